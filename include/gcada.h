@@ -295,6 +295,89 @@ gcada_status gcada_innovation_norms_noalloc(const float *fresh_dev, const float 
                                             long long p, long long ld, double *lhs_dev,
                                             void *cuda_stream, char *errbuf, size_t errbuf_len);
 
+/*
+ * Matrix operators of the server's side of a wide model's iteration, for callers that hold their own matrices: an
+ * update orthogonalised by Newton-Schulz steps (and the optimiser step of a weight matrix that uses it), and
+ * matrices in microscaled 4-bit floating point (quantisation, read-back, product), the form of an upload that
+ * costs a quarter of the bits.  (The paper has no counterpart of them.)
+ *
+ * Common to all: they need no context.  Pointers are device memory of the CURRENT device, matrices are row-major
+ * with a row stride in elements (>= their columns; any alignment that the element type has, 16 bytes is fastest).
+ * `type` is GCADA_COMPUTE_FP32 (float) or GCADA_COMPUTE_BF16.  The work is enqueued on cuda_stream (cudaStream_t
+ * as void*, NULL = legacy default stream), is asynchronous, allocates nothing, and may be captured into a graph.
+ * A work area belongs to one call at a time: two calls whose kernels may overlap (other streams, replays of two
+ * graphs) need two; its contents need no preparation and mean nothing afterwards.  status_dev: a device word of
+ * the caller's, or NULL; a kernel whose bounded wait gave up sets it to non-zero (the outputs are then undefined)
+ * and nothing clears it.  Sizes of zero are no error: nothing is done.  On failure a message is written to errbuf
+ * (if non-NULL, errbuf_len bytes), nothing has been enqueued by a call that returns GCADA_EINVAL, and nothing
+ * throws or aborts.
+ */
+
+/* How the products of an orthogonalisation are formed.  Both keep the iterate in 22 bits and accumulate in fp32.
+ * FULL: operands of 22 bits, the accuracy of fp32 arithmetic (three tensor-core products for one).
+ * HALF: operands of 11 bits; the result is within about 2e-3 of its norm, below the rounding to bfloat16. */
+#define GCADA_PRECISION_FULL 0
+#define GCADA_PRECISION_HALF 1
+
+/*
+ * o = the matrix g (batch of them: stride_g, stride_o elements apart; stride_g may be 0) after `steps` steps of
+ *     X_0 = g / (||g||_F + eps),  X_{j+1} = a X_j + (b A_j + c A_j^2) X_j,  A_j = X_j X_j^T
+ * which drive the singular values towards one.  coef = {a, b, c} (host; NULL: 3.4445, -4.7750, 2.0315, for which
+ * five steps take singular values above 0.01 of the norm to between 0.68 and 1.21).  The iterates' singular values
+ * have to stay below 7.  A matrix of zeros gives zeros; one that holds an infinity or NaN gives NaN.  o may be g.
+ * GCADA_EINVAL unless 0 <= steps <= 100, |a|, |b|, |c| <= 16, 1e-30 <= eps <= 1e30, rows, cols <= 2^20, batch <=
+ * 65535, the results do not overlap, and work_dev is 256-byte aligned with at least the bytes that
+ * gcada_orthogonalize_work gives.
+ */
+gcada_status gcada_orthogonalize_work(int batch, int rows, int cols, size_t *bytes);
+gcada_status gcada_orthogonalize(const void *g_dev, void *o_dev, int type, int batch, int rows, int cols,
+                                 long long ld_g, long long stride_g, long long ld_o, long long stride_o,
+                                 int precision, int steps, const double *coef, double eps, void *work_dev,
+                                 size_t work_bytes, int *status_dev, void *cuda_stream, char *errbuf,
+                                 size_t errbuf_len);
+
+/*
+ * One optimiser step of a weight matrix w (rows x cols), in place:
+ *     m <- beta m + (1 - beta) g           (the weighting of Eq. 8a)
+ *     u  = nesterov ? beta m + (1 - beta) g : m
+ *     w <- (1 - lr weight_decay) w - lr scale o,   o = u orthogonalised as above
+ * m is float; w and g have their own types.  The work area is that of gcada_orthogonalize with batch 1.
+ * GCADA_EINVAL as there, and unless 0 <= beta < 1 and lr, weight_decay, scale are finite (at most 1e30).
+ */
+gcada_status gcada_muon_update(void *w_dev, int w_type, float *m_dev, const void *g_dev, int g_type, int rows,
+                               int cols, long long ld_w, long long ld_m, long long ld_g, double lr, double beta,
+                               int nesterov, double weight_decay, double scale, int precision, int steps,
+                               const double *coef, double eps, void *work_dev, size_t work_bytes, int *status_dev,
+                               void *cuda_stream, char *errbuf, size_t errbuf_len);
+
+/*
+ * Microscaled 4-bit matrices.  32 consecutive elements of a row share a scale 2^e, e = floor(log2(largest
+ * magnitude)) - 2 within [-127, 127]; each element is x / 2^e rounded to nearest (ties to even) on the E2M1 values
+ * +-{0, 0.5, 1, 1.5, 2, 3, 4, 6}, beyond 6 to 6.  A block with an infinity or NaN reads back as NaN.
+ * codes: two to a byte, the even column in the low half; a row has ceil(cols / 32) * 16 bytes (zero codes behind
+ * the end).  scales: bytes e + 127 (0xFF: NaN) in tiles of 128 rows x 256 columns, 1024 bytes each, tile
+ * (row / 128) * ceil(cols / 256) + column / 256; inside a tile byte
+ *     (column % 256 / 128) * 512 + (row % 32) * 16 + (row % 128 / 32) * 4 + column % 128 / 32;
+ * bytes of rows and blocks behind the end are zero.  Both arrays are 16-byte aligned; gcada_mx_size gives their
+ * bytes.  At most 2^22 rows and 2^25 columns.
+ * gcada_mx_quantize: x is rows x cols; with `transpose` the 4-bit matrix is x^T (cols x rows, blocks run down x's
+ * columns).  gcada_mx_dequantize: the values of a rows x cols 4-bit matrix, exact in both types unless they leave
+ * the type's range.
+ */
+gcada_status gcada_mx_size(long long rows, long long cols, size_t *code_bytes, size_t *scale_bytes);
+gcada_status gcada_mx_quantize(const void *x_dev, int type, long long rows, long long cols, long long ld,
+                               int transpose, void *codes_dev, void *scales_dev, void *cuda_stream, char *errbuf,
+                               size_t errbuf_len);
+gcada_status gcada_mx_dequantize(const void *codes_dev, const void *scales_dev, long long rows, long long cols,
+                                 void *x_dev, int type, long long ld, void *cuda_stream, char *errbuf,
+                                 size_t errbuf_len);
+/* d = alpha a b^T + bias + beta d: a is m x k, b is n x k in 4-bit form, d m x n; bias (float, n values) may be
+ * NULL; with beta = 0 d is not read.  The elements' products are exact and summed in fp32.  GCADA_EINVAL if k = 0. */
+gcada_status gcada_mx_gemm(const void *a_codes, const void *a_scales, long long m, const void *b_codes,
+                           const void *b_scales, long long n, long long k, void *d_dev, int type, long long ld,
+                           double alpha, double beta, const float *bias_dev, int *status_dev, void *cuda_stream,
+                           char *errbuf, size_t errbuf_len);
+
 /* Measurement aid: enqueue the gradient kernel(s) of the current iteration `reps` times back to back on the
  * stream, bracketed by ONE pair of CUDA events, and return the mean device time per repetition in
  * milliseconds (per-launch event brackets, as GCADA_OPT_TIMING uses, add the launch gaps of each bracket to

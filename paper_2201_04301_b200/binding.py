@@ -65,6 +65,18 @@ SIGNATURES = {
     "gcada_get_launch_count": (C.c_int, [_VP, _ULLP]),
     "gcada_get_kernel_times": (C.c_int, [_VP, C.POINTER(C.c_double), C.POINTER(C.c_int)]),
     "gcada_innovation_norms_noalloc": (C.c_int, [_VP, _VP, C.c_int, _LL, _LL, _VP, _VP, C.c_char_p, C.c_size_t]),
+    "gcada_orthogonalize_work": (C.c_int, [C.c_int, C.c_int, C.c_int, C.POINTER(C.c_size_t)]),
+    "gcada_orthogonalize": (C.c_int, [_VP, _VP] + [C.c_int] * 4 + [_LL] * 4 + [C.c_int] * 2 +
+                            [C.POINTER(C.c_double), C.c_double, _VP, C.c_size_t, _VP, _VP, C.c_char_p, C.c_size_t]),
+    "gcada_muon_update": (C.c_int, [_VP, C.c_int, _VP, _VP, C.c_int, C.c_int, C.c_int, _LL, _LL, _LL, C.c_double,
+                                    C.c_double, C.c_int, C.c_double, C.c_double, C.c_int, C.c_int,
+                                    C.POINTER(C.c_double), C.c_double, _VP, C.c_size_t, _VP, _VP, C.c_char_p,
+                                    C.c_size_t]),
+    "gcada_mx_size": (C.c_int, [_LL, _LL, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]),
+    "gcada_mx_quantize": (C.c_int, [_VP, C.c_int, _LL, _LL, _LL, C.c_int, _VP, _VP, _VP, C.c_char_p, C.c_size_t]),
+    "gcada_mx_dequantize": (C.c_int, [_VP, _VP, _LL, _LL, _VP, C.c_int, _LL, _VP, C.c_char_p, C.c_size_t]),
+    "gcada_mx_gemm": (C.c_int, [_VP, _VP, _LL, _VP, _VP, _LL, _LL, _VP, C.c_int, _LL, C.c_double, C.c_double, _VP, _VP,
+                                _VP, C.c_char_p, C.c_size_t]),
     "gcada_time_gradient": (C.c_int, [_VP, C.c_int, C.POINTER(C.c_double)]),
     "gcada_time_empty_chain": (C.c_int, [_VP, C.c_int, C.POINTER(C.c_double)]),
     "gcada_eval_loss": (C.c_int, [_VP, _LL, _LL, C.POINTER(C.c_double)]),
@@ -314,6 +326,257 @@ def innovation_norms_noalloc(fresh, stale, lhs_out, stream=None):
                                             int(fresh.stride(0)), _VP(lhs_out.data_ptr()), _VP(raw or 0), buf, 256)
     if st != OK:
         raise GCadaError(st, buf.value.decode())
+
+
+# ---------------------------------------------------------------------------
+# Matrix operators (gcada_orthogonalize, gcada_muon_update, gcada_mx_*).  Tensors live on one CUDA device, which
+# need not be the current one; their last dimension is contiguous.  stream: a torch.cuda.Stream, a raw cudaStream_t
+# integer, or None for torch's current stream of that device.
+# ---------------------------------------------------------------------------
+PRECISIONS = {"full": 0, "half": 1}
+MUON_COEF = (3.4445, -4.7750, 2.0315)
+_status_words = {}
+
+
+def _compute_type(t, what):
+    kind = {"torch.float32": COMPUTE_FP32, "torch.bfloat16": COMPUTE_BF16}.get(str(t.dtype))
+    if kind is None:
+        raise ValueError("%s must be float32 or bfloat16, not %s" % (what, t.dtype))
+    return kind
+
+
+def _matrix(t, what, dims=(2,)):
+    """Checks a row-major device matrix; its row stride."""
+    if not t.is_cuda:
+        raise ValueError("%s must be a CUDA tensor" % what)
+    if t.dim() not in dims:
+        raise ValueError("%s must have %s dimensions, not %d" % (what, " or ".join(map(str, dims)), t.dim()))
+    if t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError("%s: the last dimension must be contiguous" % what)
+    rows, cols = t.shape[-2:]
+    if rows > 1 and cols and t.stride(-2) < cols:
+        raise ValueError("%s: rows overlap" % what)
+    return int(t.stride(-2)) if rows > 1 else int(cols)
+
+
+class _Launch:
+    """The device, stream, status word and message buffer of one operator call."""
+
+    def __init__(self, first, others, stream):
+        import torch
+        self.torch, self.device = torch, first.device
+        for t in others:
+            if t is not None and t.device != first.device:
+                raise ValueError("tensors on different devices: %s and %s" % (first.device, t.device))
+        self.lib = load()
+        self.guard = torch.cuda.device(first.device)
+        current = torch.cuda.current_stream(first.device)
+        self.raw = current.cuda_stream if stream is None else int(getattr(stream, "cuda_stream", stream))
+        # memory taken from torch's allocator belongs to the current stream; a call on another one says so
+        self.other = None if self.raw == current.cuda_stream else (
+            stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(self.raw, first.device))
+        self.buf = C.create_string_buffer(256)
+
+    def hold(self, *tensors):
+        if self.other is not None:
+            for t in tensors:
+                t.record_stream(self.other)
+
+    def fresh(self, *shape, dtype):
+        t = self.torch.empty(*shape, dtype=dtype, device=self.device)
+        if self.other is not None:  # the caching allocator may hand out memory that the current stream still uses
+            self.other.wait_stream(self.torch.cuda.current_stream(self.device))
+            t.record_stream(self.other)
+        return t
+
+    def status(self):
+        w = _status_words.get(self.device.index)
+        if w is None:
+            if self.torch.cuda.is_current_stream_capturing():
+                return None   # a word made now would belong to the graph being captured
+            w = _status_words[self.device.index] = self.torch.zeros(1, dtype=self.torch.int32, device=self.device)
+            self.torch.cuda.current_stream(self.device).synchronize()
+        return _VP(w.data_ptr())
+
+    def check(self, st):
+        if st != OK:
+            raise GCadaError(st, self.buf.value.decode())
+
+
+def check_operators(device=None):
+    """Waits for the device and raises (GCADA_ETIMEOUT) if a kernel of the matrix operators ever gave up a wait
+    there since the last check."""
+    import torch
+    index = torch.cuda.current_device() if device is None else torch.device(device).index
+    torch.cuda.synchronize(index)
+    w = _status_words.get(index)
+    if w is not None and int(w.item()):
+        w.zero_()
+        raise GCadaError(ETIMEOUT, "a bounded device-side wait of a matrix operator gave up")
+
+
+def _steps(steps, coef, eps, precision, narrow):
+    if precision is None:
+        precision = "half" if narrow else "full"
+    if precision not in PRECISIONS:
+        raise ValueError("precision must be 'full' or 'half', not %r" % (precision,))
+    if len(coef) != 3:
+        raise ValueError("coef must hold three values")
+    return PRECISIONS[precision], int(steps), (C.c_double * 3)(*[float(v) for v in coef]), float(eps)
+
+
+def _ns_work(run, batch, rows, cols, work):
+    n = C.c_size_t()
+    st = run.lib.gcada_orthogonalize_work(batch, rows, cols, C.byref(n))
+    if st != OK:
+        raise GCadaError(st, "matrix sizes out of range")
+    if work is None:
+        work = run.fresh(max(1, n.value), dtype=run.torch.uint8)
+    elif work.device != run.device or not work.is_contiguous():
+        raise ValueError("work must be a contiguous tensor on the same device")
+    return work, _VP(work.data_ptr()), work.numel() * work.element_size()
+
+
+def orthogonalize(g, out=None, steps=5, coef=MUON_COEF, eps=1e-7, precision=None, work=None, stream=None):
+    """`g` ([rows, cols] or [batch, rows, cols], float32 or bfloat16) after `steps` Newton-Schulz steps: a matrix of
+    the same singular vectors whose singular values are near one.  See gcada_orthogonalize.  `precision`: "full" or
+    "half", by default "full" for float32 and "half" for bfloat16.  `out` may be `g`.  `work`: a tensor of at least
+    orthogonalize_work(g) bytes to use as the work area, by default taken from torch's allocator."""
+    kind = _compute_type(g, "g")
+    ld_g = _matrix(g, "g", (2, 3))
+    run = _Launch(g, (out, work), stream)
+    if out is None:
+        out = run.fresh(g.shape, dtype=g.dtype)
+    if out.shape != g.shape or out.dtype != g.dtype:
+        raise ValueError("out must have g's shape and type")
+    ld_o = _matrix(out, "out", (2, 3))
+    rows, cols = g.shape[-2:]
+    batch = g.shape[0] if g.dim() == 3 else 1
+    stride_g, stride_o = (int(t.stride(0)) if t.dim() == 3 and batch > 1 else 0 for t in (g, out))
+    precision, steps, coef, eps = _steps(steps, coef, eps, precision, kind == COMPUTE_BF16)
+    with run.guard:
+        work, ptr, size = _ns_work(run, batch, rows, cols, work)
+        run.check(run.lib.gcada_orthogonalize(_VP(g.data_ptr()), _VP(out.data_ptr()), kind, batch, rows, cols, ld_g,
+                                              stride_g, ld_o, stride_o, precision, steps, coef, eps, ptr, size,
+                                              run.status(), _VP(run.raw), run.buf, 256))
+    run.hold(g, out)
+    return out
+
+
+def orthogonalize_work(g):
+    """Bytes of the work area that orthogonalize(g) or muon_update(w=g) needs."""
+    n = C.c_size_t()
+    rows, cols = g.shape[-2:]
+    st = load().gcada_orthogonalize_work(g.shape[0] if g.dim() == 3 else 1, rows, cols, C.byref(n))
+    if st != OK:
+        raise GCadaError(st, "matrix sizes out of range")
+    return n.value
+
+
+def muon_update(w, m, g, lr, beta=0.95, nesterov=True, weight_decay=0.0, scale=None, steps=5, coef=MUON_COEF,
+                eps=1e-7, precision=None, work=None, stream=None):
+    """One optimiser step of the weight matrix `w`, in place with its momentum `m` (float32); `g` is the gradient.
+    See gcada_muon_update.  `scale`: by default sqrt(max(1, rows / cols)).  `precision`: by default "full" for
+    float32 weights and "half" for bfloat16 ones."""
+    w_kind, g_kind = _compute_type(w, "w"), _compute_type(g, "g")
+    ld = [_matrix(t, n) for t, n in ((w, "w"), (m, "m"), (g, "g"))]
+    if str(m.dtype) != "torch.float32":
+        raise ValueError("m must be float32")
+    if m.shape != w.shape or g.shape != w.shape:
+        raise ValueError("w, m and g must have the same shape")
+    run = _Launch(w, (m, g, work), stream)
+    rows, cols = w.shape
+    if scale is None:
+        scale = max(1.0, rows / max(1, cols)) ** 0.5
+    precision, steps, coef, eps = _steps(steps, coef, eps, precision, w_kind == COMPUTE_BF16)
+    with run.guard:
+        work, ptr, size = _ns_work(run, 1, rows, cols, work)
+        run.check(run.lib.gcada_muon_update(_VP(w.data_ptr()), w_kind, _VP(m.data_ptr()), _VP(g.data_ptr()), g_kind,
+                                            rows, cols, *ld, float(lr), float(beta), int(bool(nesterov)),
+                                            float(weight_decay), float(scale), precision, steps, coef, eps, ptr, size,
+                                            run.status(), _VP(run.raw), run.buf, 256))
+    run.hold(w, m, g)
+
+
+class MxMatrix:
+    """A rows x cols matrix in microscaled 4-bit floating point (layout: include/gcada.h).  `codes`, `scales`: uint8
+    CUDA tensors of the sizes that gcada_mx_size gives, any shape, contiguous."""
+
+    def __init__(self, rows, cols, codes, scales):
+        self.rows, self.cols, self.codes, self.scales = int(rows), int(cols), codes, scales
+        n, s = C.c_size_t(), C.c_size_t()
+        st = load().gcada_mx_size(self.rows, self.cols, C.byref(n), C.byref(s))
+        if st != OK:
+            raise GCadaError(st, "matrix sizes out of range")
+        for t, want, name in ((codes, n.value, "codes"), (scales, s.value, "scales")):
+            if not t.is_cuda or str(t.dtype) != "torch.uint8" or not t.is_contiguous() or t.numel() != want:
+                raise ValueError("%s of a %d x %d matrix must be a contiguous CUDA tensor of %d bytes"
+                                 % (name, self.rows, self.cols, want))
+        if codes.device != scales.device:
+            raise ValueError("codes and scales on different devices")
+
+    def dequantize(self, dtype=None, out=None, stream=None):
+        """The values as a float32 (default) or bfloat16 tensor.  See gcada_mx_dequantize."""
+        run = _Launch(self.codes, (out,), stream)
+        if out is None:
+            out = run.fresh(self.rows, self.cols, dtype=dtype or run.torch.float32)
+        if tuple(out.shape) != (self.rows, self.cols) or (dtype is not None and out.dtype != dtype):
+            raise ValueError("out must be a %d x %d matrix of the type asked for" % (self.rows, self.cols))
+        ld = _matrix(out, "out")
+        with run.guard:
+            run.check(run.lib.gcada_mx_dequantize(_VP(self.codes.data_ptr()), _VP(self.scales.data_ptr()), self.rows,
+                                                  self.cols, _VP(out.data_ptr()), _compute_type(out, "out"), ld,
+                                                  _VP(run.raw), run.buf, 256))
+        run.hold(self.codes, self.scales, out)
+        return out
+
+
+def mx_quantize(x, transpose=False, out=None, stream=None):
+    """`x` (float32 or bfloat16 [rows, cols]), or with `transpose` its transpose, as an MxMatrix.  See
+    gcada_mx_quantize.  `out`: an MxMatrix of the result's shape to fill."""
+    kind, ld = _compute_type(x, "x"), _matrix(x, "x")
+    rows, cols = x.shape
+    shape = (cols, rows) if transpose else (rows, cols)
+    run = _Launch(x, () if out is None else (out.codes,), stream)
+    if out is None:
+        n, s = C.c_size_t(), C.c_size_t()
+        st = run.lib.gcada_mx_size(*shape, C.byref(n), C.byref(s))
+        if st != OK:
+            raise GCadaError(st, "matrix sizes out of range")
+        out = MxMatrix(*shape, run.fresh(n.value, dtype=run.torch.uint8), run.fresh(s.value, dtype=run.torch.uint8))
+    elif (out.rows, out.cols) != shape:
+        raise ValueError("out must be %d x %d" % shape)
+    with run.guard:
+        run.check(run.lib.gcada_mx_quantize(_VP(x.data_ptr()), kind, rows, cols, ld, int(bool(transpose)),
+                                            _VP(out.codes.data_ptr()), _VP(out.scales.data_ptr()), _VP(run.raw),
+                                            run.buf, 256))
+    run.hold(x, out.codes, out.scales)
+    return out
+
+
+def mx_gemm(a, b, out=None, dtype=None, alpha=1.0, beta=0.0, bias=None, stream=None):
+    """alpha a b^T + bias + beta out for MxMatrix operands a (m x k) and b (n x k), as a float32 (default) or bfloat16
+    tensor.  See gcada_mx_gemm.  `bias`: float32, n values."""
+    if a.cols != b.cols:
+        raise ValueError("a has %d columns and b %d" % (a.cols, b.cols))
+    run = _Launch(a.codes, (b.codes, out, bias), stream)
+    if out is None:
+        if beta != 0:
+            raise ValueError("beta needs out")
+        out = run.fresh(a.rows, b.rows, dtype=dtype or run.torch.float32)
+    if tuple(out.shape) != (a.rows, b.rows) or (dtype is not None and out.dtype != dtype):
+        raise ValueError("out must be a %d x %d matrix of the type asked for" % (a.rows, b.rows))
+    if bias is not None and (str(bias.dtype) != "torch.float32" or bias.numel() != b.rows or not bias.is_contiguous()):
+        raise ValueError("bias must hold %d contiguous float32 values" % b.rows)
+    ld = _matrix(out, "out")
+    with run.guard:
+        run.check(run.lib.gcada_mx_gemm(_VP(a.codes.data_ptr()), _VP(a.scales.data_ptr()), a.rows,
+                                        _VP(b.codes.data_ptr()), _VP(b.scales.data_ptr()), b.rows, a.cols,
+                                        _VP(out.data_ptr()), _compute_type(out, "out"), ld, float(alpha), float(beta),
+                                        _VP(bias.data_ptr()) if bias is not None else None, run.status(),
+                                        _VP(run.raw), run.buf, 256))
+    run.hold(a.codes, a.scales, b.codes, b.scales, out, *(() if bias is None else (bias,)))
+    return out
 
 
 def from_workload(w, stream=None, options=None, smoothness=None, c_d=None, schedule=None, delay_law=None):

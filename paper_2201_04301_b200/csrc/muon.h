@@ -1,0 +1,31 @@
+// Newton-Schulz orthogonalisation and the optimiser step built on it (see muon.cu).
+#pragma once
+#include <cuda_runtime.h>
+#include <stddef.h>
+
+namespace gcada {
+
+struct NsProblem {
+  int batch, rows, cols;
+  const void* g;        // float or bf16, row stride ld_g, matrix stride stride_g
+  long long ld_g, stride_g;
+  int g_bf16;
+  float* m = nullptr;   // momentum (one matrix), moved first; the matrix orthogonalised is then the momentum or,
+  long long ld_m = 0;   // with nesterov, its look-ahead (1 - beta) g + beta m
+  double beta = 0;
+  int nesterov = 0;
+  void* o;              // result, float or bf16
+  long long ld_o, stride_o;
+  int o_bf16;
+  int w_update = 0;     // 1: o <- decay * o - step * result
+  double decay = 1, step = 0;
+  int steps;
+  double coef[3];
+  double eps;
+  int full;             // 1: products of hi / lo pairs (fp32 accuracy), 0: of the hi parts
+  int* err = nullptr;   // device error word, or null
+};
+size_t ns_work_bytes(int batch, int rows, int cols);
+cudaError_t ns_run(const NsProblem& p, void* work, cudaStream_t st, const char** why, int* launches);
+
+}  // namespace gcada

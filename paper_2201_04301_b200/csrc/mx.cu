@@ -1,0 +1,518 @@
+// Microscaled 4-bit floating point (MXFP4): quantisation, read-back and product.
+//
+// A block of 32 consecutive elements of a row shares the scale 2^e, e = floor(log2(largest magnitude)) - 2 clamped
+// to [-127, 127], so that the largest element lands in [4, 8); each element is x / 2^e rounded to nearest even on
+// {0, .5, 1, 1.5, 2, 3, 4, 6}, magnitudes above 6 becoming 6.  A block of zeros has e = -127; a block that holds an
+// infinity or NaN has the NaN scale (0xFF) and reads back, and multiplies, as NaN.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp4.h>
+#include <atomic>
+
+#include "../../include/gcada.h"
+#include "common.cuh"
+#include "mx.h"
+#include "tc.cuh"
+
+namespace gcada {
+namespace {
+
+// ----------------------------------------------------------------- elements
+__device__ __forceinline__ uint32_t scale_code(float top) {  // biased exponent of the block's scale
+  const uint32_t e = __float_as_uint(top) >> 23;             // top >= 0 or NaN; subnormal: 0
+  return (e & 255u) == 255u ? 255u : (e > 2u ? e - 2u : 0u);
+}
+__device__ __forceinline__ float inverse_scale(uint32_t code) {  // 2^(127 - code); codes up to 252 or 255
+  return __uint_as_float((code == 255u ? 127u : 254u - code) << 23);
+}
+__device__ __forceinline__ float scale_value(uint32_t code) {
+  return code == 255u ? __uint_as_float(0x7fffffffu) : (code ? __uint_as_float(code << 23) : __uint_as_float(0x400000u));
+}
+// Eight elements (already divided by the scale) as eight codes, the first in the lowest half byte.
+__device__ __forceinline__ uint32_t codes8(const float (&f)[8]) {
+  uint32_t w = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    w |= (uint32_t)__nv_cvt_float2_to_fp4x2(make_float2(f[2 * j], f[2 * j + 1]), __NV_E2M1, cudaRoundNearest) << (8 * j);
+  return w;
+}
+__device__ __forceinline__ float2 values2(uint32_t byte) {
+  const __half2_raw h = __nv_cvt_fp4x2_to_halfraw2((__nv_fp4x2_storage_t)byte, __NV_E2M1);
+  return __half22float2(*reinterpret_cast<const __half2*>(&h));
+}
+// fmaxf drops NaN: the largest magnitude of a block keeps it instead (as bits: NaN is above infinity)
+__device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, long long n, float (&f)[8]) {
+  if (n >= 8 && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+    if (sizeof(T) == 4) {
+      const float4 x = *reinterpret_cast<const float4*>(p), y = *(reinterpret_cast<const float4*>(p) + 1);
+      f[0] = x.x; f[1] = x.y; f[2] = x.z; f[3] = x.w; f[4] = y.x; f[5] = y.y; f[6] = y.z; f[7] = y.w;
+    } else {
+      const uint4 x = *reinterpret_cast<const uint4*>(p);
+      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = j < n ? (float)p[j] : 0.f;
+  }
+}
+
+// One warp: a row's 256 columns, eight per lane; four lanes share a block.  Rows run to the end of the last row
+// tile (their scales are zeroed).
+template <typename T>
+__global__ void __launch_bounds__(256) mx_quantize_kernel(const T* __restrict__ x, long long ld, const MxView q) {
+  const int lane = threadIdx.x & 31;
+  const long long row_end = (q.rows + 127) / 128 * 128, units = row_end * q.col_tiles;
+  for (long long u = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); u < units; u += (long long)gridDim.x * 8) {
+    const long long r = u / q.col_tiles, ct = u - r * q.col_tiles, c = ct * 256 + lane * 8;
+    float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (r < q.rows && c < q.cols) load8(x + r * ld + c, q.cols - c, f);
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = max(top, abs_bits(f[j]));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const uint32_t sc = scale_code(__uint_as_float(top));
+    const float inv = inverse_scale(sc);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] *= inv;
+    if (r < q.rows && c < q.pitch * 2) *reinterpret_cast<uint32_t*>(q.codes + r * q.pitch + c / 2) = codes8(f);
+    // four blocks' scales are one word of a tile
+    uint32_t word = sc << (8 * ((lane >> 2) & 3));
+    word |= __shfl_xor_sync(0xffffffffu, word, 4);
+    word |= __shfl_xor_sync(0xffffffffu, word, 8);
+    if ((lane & 15) == 0) {
+      const int rr = (int)(r & 127);
+      *reinterpret_cast<uint32_t*>(q.scales + ((r >> 7) * q.col_tiles + ct) * 1024 + (lane >> 4) * 512 + (rr & 31) * 16 +
+                                   (rr >> 5) * 4) = word;
+    }
+  }
+}
+
+// Transposed source: x is [q.cols][q.rows], blocks run down its columns.  A CTA takes 64 columns (rows of the
+// result) x 256 rows; warp w the block of 32 rows w, two columns per lane; codes and scales leave through shared
+// memory so that a result row's 128 bytes are written together.
+template <typename T>
+__global__ void __launch_bounds__(256) mx_quantize_t_kernel(const T* __restrict__ x, long long ld, const MxView q) {
+  __shared__ __align__(16) uint4 codes_sm[64][9];  // [row][block], padded
+  __shared__ uint32_t scale_sm[64][2];
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const long long ct = blockIdx.x, r0 = (long long)blockIdx.y * 64, k0 = ct * 256 + w * 32, r = r0 + 2 * lane;
+  float v[2][32];
+  const bool pair = (reinterpret_cast<uintptr_t>(x) & (2 * sizeof(T) - 1)) == 0 && (ld & 1) == 0 && r + 1 < q.rows;
+#pragma unroll
+  for (int j = 0; j < 32; ++j) {
+    v[0][j] = v[1][j] = 0.f;
+    if (k0 + j < q.cols) {
+      const T* p = x + (k0 + j) * ld + r;
+      if (pair) {
+        if (sizeof(T) == 4) {
+          const float2 t = *reinterpret_cast<const float2*>(p);
+          v[0][j] = t.x;
+          v[1][j] = t.y;
+        } else {
+          const uint32_t t = *reinterpret_cast<const uint32_t*>(p);
+          v[0][j] = __uint_as_float(t << 16);
+          v[1][j] = __uint_as_float(t & 0xffff0000u);
+        }
+      } else {
+        if (r < q.rows) v[0][j] = (float)p[0];
+        if (r + 1 < q.rows) v[1][j] = (float)p[1];
+      }
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) top = max(top, abs_bits(v[h][j]));
+    const uint32_t sc = scale_code(__uint_as_float(top));
+    const float inv = inverse_scale(sc);
+    uint32_t c[4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      float f[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] = v[h][8 * g + j] * inv;
+      c[g] = codes8(f);
+    }
+    codes_sm[2 * lane + h][w] = make_uint4(c[0], c[1], c[2], c[3]);
+    reinterpret_cast<unsigned char*>(scale_sm[2 * lane + h])[w] = (unsigned char)sc;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 64 * 8; i += 256) {
+    const int rr = i >> 3, b = i & 7;
+    const long long at = ct * 128 + b * 16;
+    if (r0 + rr < q.rows && at < q.pitch) *reinterpret_cast<uint4*>(q.codes + (r0 + rr) * q.pitch + at) = codes_sm[rr][b];
+  }
+  if (threadIdx.x < 128) {  // rows behind the end have zero elements, hence zero scales
+    const int rr = threadIdx.x >> 1, half = threadIdx.x & 1;
+    const long long row = r0 + rr;
+    const int in = (int)(row & 127);
+    *reinterpret_cast<uint32_t*>(q.scales + ((row >> 7) * q.col_tiles + ct) * 1024 + half * 512 + (in & 31) * 16 +
+                                 (in >> 5) * 4) = scale_sm[rr][half];
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) mx_dequantize_kernel(const MxView q, T* __restrict__ out, long long ld) {
+  const int lane = threadIdx.x & 31;
+  const long long units = q.rows * q.col_tiles;
+  for (long long u = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); u < units; u += (long long)gridDim.x * 8) {
+    const long long r = u / q.col_tiles, ct = u - r * q.col_tiles, c = ct * 256 + lane * 8;
+    if (c >= q.cols) continue;
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(q.codes + r * q.pitch + c / 2);
+    const int rr = (int)(r & 127);
+    const float s = scale_value(q.scales[((r >> 7) * q.col_tiles + ct) * 1024 + (lane >> 4) * 512 + (rr & 31) * 16 +
+                                         (rr >> 5) * 4 + ((lane >> 2) & 3)]);
+    float f[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 t = values2((w >> (8 * j)) & 255u);
+      f[2 * j] = t.x * s;
+      f[2 * j + 1] = t.y * s;
+    }
+    T* o = out + r * ld + c;
+    if (c + 8 <= q.cols && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+      if (sizeof(T) == 4) {
+        *reinterpret_cast<float4*>(o) = make_float4(f[0], f[1], f[2], f[3]);
+        *(reinterpret_cast<float4*>(o) + 1) = make_float4(f[4], f[5], f[6], f[7]);
+      } else {
+        uint32_t p[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const __nv_bfloat162 t = __floats2bfloat162_rn(f[2 * j], f[2 * j + 1]);
+          p[j] = *reinterpret_cast<const uint32_t*>(&t);
+        }
+        *reinterpret_cast<uint4*>(o) = make_uint4(p[0], p[1], p[2], p[3]);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (c + j < q.cols) o[j] = (T)f[j];
+    }
+  }
+}
+
+// ----------------------------------------------------------------- product
+// Persistent CTAs over 128 x BN tiles of D, K in steps of 256: warp 0 copies the operands' codes (128-byte rows,
+// 128-byte swizzle) and scales into a ring of stages, warp 1 copies a stage's scales into tensor memory and issues
+// the block-scaled products (64 K values each), eight warps write the result.
+constexpr int BM = 128, KB = 256;
+constexpr int STAGES = 4;
+constexpr int EPI_WARPS = 8;
+constexpr int THREADS = 64 + 32 * EPI_WARPS;
+
+template <int BN>
+struct MxTile {
+  static constexpr int ACC = BN == 256 ? 1 : 2;           // accumulators in tensor memory
+  static constexpr int NB = BN < 128 ? 1 : BN / 128;      // row tiles of B's scales that a tile touches
+  static constexpr int CODE_BYTES = (BM + BN) * (KB / 2);
+  static constexpr int STAGE_BYTES = CODE_BYTES + (1 + NB) * 1024;
+  static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + 1024;
+  static constexpr int SF_COL = ACC * BN;                 // first tensor-memory column of the scales
+  static constexpr int SF_COLS = 8 + 8 * NB;              // per stage: A 2 x 4, B 2 x 4 NB
+  static constexpr int TMEM_COLS = SF_COL + STAGES * SF_COLS <= 256 ? 256 : 512;
+  static_assert(SF_COL + STAGES * SF_COLS <= 512, "tensor memory");
+  static_assert(STAGE_BYTES % 1024 == 0, "swizzle atoms");
+};
+
+__device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* tm, int c0, int c1, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(
+          smem_u32(dst)),
+      "l"(tm), "r"(smem_u32(bar)), "r"(c0), "r"(c1)
+      : "memory");
+}
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                   smem_u32(dst)),
+               "l"(src), "r"(bytes), "r"(smem_u32(bar))
+               : "memory");
+}
+// 512 bytes of scales (32 rows x 16 bytes, no swizzle; groups of 8 rows 128 bytes apart) into four columns of
+// tensor memory, the same for every quadrant of lanes.
+__device__ __forceinline__ void tc_copy_scales(uint32_t taddr, uint32_t smem_addr) {
+  const uint64_t desc = (uint64_t)((smem_addr & 0x3FFFFu) >> 4) | ((uint64_t)(128 >> 4) << 32) | (1ull << 46);
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void tc_mma_mxf4(uint32_t tmem_c, uint64_t da, uint64_t db, uint32_t idesc, uint32_t sfa,
+                                            uint32_t sfb, uint32_t accum) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+      :
+      : "r"(tmem_c), "l"(da), "l"(db), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accum)
+      : "memory");
+}
+
+template <int BN>
+__global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_constant__ CUtensorMap tmA,
+                                                             const __grid_constant__ CUtensorMap tmB, const MxGemm p) {
+  using T = MxTile<BN>;
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  __shared__ uint64_t full_bar[STAGES], empty_bar[STAGES], tfull_bar[2], tempty_bar[2];
+  __shared__ uint32_t tmem_base_sm;
+  unsigned char* tiles = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int M = (int)p.a.rows, N = (int)p.b.rows;
+  const int tiles_m = (M + BM - 1) / BM, tiles_n = (N + BN - 1) / BN, total = tiles_m * tiles_n;
+  const int nkb = (int)p.a.col_tiles;
+  const int n_local = (int)blockIdx.x < total ? (total - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x : 0;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(&full_bar[s], 1);
+      mbar_init(&empty_bar[s], 1);
+    }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(&tfull_bar[s], 1);
+      mbar_init(&tempty_bar[s], EPI_WARPS);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_sm)),
+                 "r"((uint32_t)T::TMEM_COLS)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = tmem_base_sm;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      bool ok = true;
+      int it = 0;
+      const long long b_tiles = (p.b.rows + 127) / 128;
+      for (int i = 0; i < n_local && ok; ++i) {
+        const int u = (int)blockIdx.x + i * (int)gridDim.x, mt = u / tiles_n, nt = u - mt * tiles_n;
+        const long long bt = (long long)nt * BN / 128;
+        const int nb = b_tiles - bt < T::NB ? (int)(b_tiles - bt) : T::NB;
+        for (int kb = 0; kb < nkb; ++kb, ++it) {
+          const int s = it % STAGES;
+          ok = mbar_spin_bounded(&empty_bar[s], (uint32_t)(((it / STAGES) & 1) ^ 1));
+          if (!ok) break;
+          unsigned char* sa = tiles + (size_t)s * T::STAGE_BYTES;
+          mbar_expect_tx(&full_bar[s], T::CODE_BYTES + (1 + nb) * 1024);
+          tma_load_2d(sa, &tmA, kb * (KB / 2), mt * BM, &full_bar[s]);
+          tma_load_2d(sa + BM * (KB / 2), &tmB, kb * (KB / 2), nt * BN, &full_bar[s]);
+          bulk_load(sa + T::CODE_BYTES, p.a.scales + ((long long)mt * p.a.col_tiles + kb) * 1024, 1024, &full_bar[s]);
+          for (int j = 0; j < nb; ++j)
+            bulk_load(sa + T::CODE_BYTES + (1 + j) * 1024, p.b.scales + ((bt + j) * p.b.col_tiles + kb) * 1024, 1024,
+                      &full_bar[s]);
+        }
+      }
+      if (!ok) raise_error(p.err);
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      // E2M1 operands (1 at bits 7 and 10), E8M0 scales (bit 23); bits 29 / 4: which pair of a column's four scale
+      // bytes an instruction's two blocks take
+      constexpr uint32_t IDESC = (1u << 7) | (1u << 10) | ((uint32_t)(BN >> 3) << 17) | (1u << 23) | ((uint32_t)(BM >> 4) << 24);
+      bool ok = true;
+      int it = 0;
+      for (int i = 0; i < n_local && ok; ++i) {
+        const int slot = i % T::ACC;
+        const int u = (int)blockIdx.x + i * (int)gridDim.x, nt = u % tiles_n;
+        ok = mbar_spin_bounded(&tempty_bar[slot], (uint32_t)(((i / T::ACC) & 1) ^ 1));
+        if (!ok) break;
+        tc_fence_after();
+        for (int kb = 0; kb < nkb && ok; ++kb, ++it) {
+          const int s = it % STAGES;
+          ok = mbar_spin_bounded(&full_bar[s], (uint32_t)((it / STAGES) & 1));
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t sa = smem_u32(tiles + (size_t)s * T::STAGE_BYTES);
+          const uint32_t sf = tmem_base + (uint32_t)(T::SF_COL + s * T::SF_COLS);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            tc_copy_scales(sf + h * 4, sa + T::CODE_BYTES + h * 512);
+#pragma unroll
+            for (int j = 0; j < T::NB; ++j)
+              tc_copy_scales(sf + 8 + h * 4 * T::NB + j * 4, sa + T::CODE_BYTES + (1 + j) * 1024 + h * 512);
+          }
+          const uint64_t da = make_desc(sa), db = make_desc(sa + BM * (KB / 2));
+          // a tile narrower than a scale tile starts at one of its groups of 32 rows = one of the four columns
+          const uint32_t sub = BN < 128 ? (uint32_t)((nt * BN & 127) >> 5) : 0u;
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk) {
+            const uint32_t id = (uint32_t)(kk & 1) * 2u;
+            tc_mma_mxf4(tmem_base + (uint32_t)(slot * BN), da + (uint64_t)(kk * 2), db + (uint64_t)(kk * 2),
+                        IDESC | (id << 29) | (id << 4), sf + (kk >> 1) * 4, sf + 8 + (kk >> 1) * 4 * T::NB + sub,
+                        (kb | kk) != 0 ? 1u : 0u);
+          }
+          tc_commit(&empty_bar[s]);
+        }
+        if (ok) tc_commit(&tfull_bar[slot]);
+      }
+      if (!ok) raise_error(p.err);
+    }
+  } else {
+    const int quad = warp & 3, half = (warp - 2) >> 2;
+    bool ok = true;
+    for (int i = 0; i < n_local; ++i) {
+      const int slot = i % T::ACC;
+      const int u = (int)blockIdx.x + i * (int)gridDim.x, mt = u / tiles_n, nt = u - mt * tiles_n;
+      const int m = mt * BM + quad * 32 + lane;
+      if (ok) {
+        ok = mbar_wait_bounded(&tfull_bar[slot], (uint32_t)((i / T::ACC) & 1));
+        ok = __all_sync(0xffffffffu, ok);
+      }
+      if (!ok) continue;
+      tc_fence_after();
+      const uint32_t tbase = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(slot * BN);
+      for (int c = half * (BN / 2); c < (half + 1) * (BN / 2); c += 32) {
+        uint32_t v[32];
+        tc_ld32_issue(tbase + (uint32_t)c, v);
+        tc_ld_wait();
+        const int n0 = nt * BN + c;
+        if (m >= M || n0 >= N) continue;
+#pragma unroll
+        for (int j = 0; j < 32; j += 8) {
+          const int n = n0 + j;
+          if (n >= N) break;
+          float f[8];
+#pragma unroll
+          for (int t = 0; t < 8; ++t) {
+            f[t] = nkb ? p.alpha * __uint_as_float(v[j + t]) : 0.f;
+            if (p.bias && n + t < N) f[t] += p.bias[n + t];
+          }
+          if (!p.d_bf16) {
+            float* o = static_cast<float*>(p.d) + (long long)m * p.ld + n;
+            if (n + 8 <= N && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+#pragma unroll
+              for (int t = 0; t < 8; t += 4) {
+                if (p.beta != 0.f) {
+                  const float4 d = *reinterpret_cast<const float4*>(o + t);
+                  f[t] += p.beta * d.x; f[t + 1] += p.beta * d.y; f[t + 2] += p.beta * d.z; f[t + 3] += p.beta * d.w;
+                }
+                *reinterpret_cast<float4*>(o + t) = make_float4(f[t], f[t + 1], f[t + 2], f[t + 3]);
+              }
+            } else {
+#pragma unroll
+              for (int t = 0; t < 8; ++t)
+                if (n + t < N) o[t] = p.beta != 0.f ? f[t] + p.beta * o[t] : f[t];
+            }
+          } else {
+            __nv_bfloat16* o = static_cast<__nv_bfloat16*>(p.d) + (long long)m * p.ld + n;
+            if (p.beta != 0.f) {
+#pragma unroll
+              for (int t = 0; t < 8; ++t)
+                if (n + t < N) f[t] += p.beta * __bfloat162float(o[t]);
+            }
+            if (n + 8 <= N && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+              uint32_t w[4];
+#pragma unroll
+              for (int t = 0; t < 4; ++t) {
+                const __nv_bfloat162 b2 = __floats2bfloat162_rn(f[2 * t], f[2 * t + 1]);
+                w[t] = *reinterpret_cast<const uint32_t*>(&b2);
+              }
+              *reinterpret_cast<uint4*>(o) = make_uint4(w[0], w[1], w[2], w[3]);
+            } else {
+#pragma unroll
+              for (int t = 0; t < 8; ++t)
+                if (n + t < N) o[t] = __float2bfloat16_rn(f[t]);
+            }
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&tempty_bar[slot]);
+    }
+    if (!ok && lane == 0) raise_error(p.err);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)T::TMEM_COLS)
+                 : "memory");
+  }
+}
+
+// ----------------------------------------------------------------- host
+// codes as bytes [rows][pitch]; boxes of 128 bytes (256 elements) x box_rows, 128-byte swizzle, zero fill outside.
+bool make_map_codes(CUtensorMap* tm, const MxView& v, int box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[2] = {(cuuint64_t)mx_pitch(v.cols), (cuuint64_t)v.rows};
+  cuuint64_t strides[1] = {(cuuint64_t)v.pitch};
+  cuuint32_t box[2] = {128, (cuuint32_t)box_rows};
+  cuuint32_t es[2] = {1, 1};
+  return fn(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, v.codes, dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+cudaError_t set_attributes() {
+  const cudaFuncAttribute at = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  cudaError_t e = cudaFuncSetAttribute(mx_gemm_kernel<256>, at, MxTile<256>::SMEM_BYTES);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(mx_gemm_kernel<64>, at, MxTile<64>::SMEM_BYTES);
+  return e;
+}
+
+template <int BN>
+cudaError_t launch_mx_gemm(const MxGemm& p, int sms, cudaStream_t st, const char** why) {
+  CUtensorMap ta, tb;
+  if (!make_map_codes(&ta, p.a, BM) || !make_map_codes(&tb, p.b, BN))
+    return *why = "tensor map creation failed for this shape", cudaErrorInvalidValue;
+  const long long units = ((p.a.rows + BM - 1) / BM) * ((p.b.rows + BN - 1) / BN);
+  const int ctas = (int)(units < sms ? units : sms);
+  mx_gemm_kernel<BN><<<ctas, THREADS, MxTile<BN>::SMEM_BYTES, st>>>(ta, tb, p);
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) *why = "kernel launch";
+  return e;
+}
+
+}  // namespace
+
+cudaError_t mx_quantize(const void* x, int bf16, long long ld, int transpose, const MxView& q, cudaStream_t st) {
+  if (transpose) {
+    const dim3 grid((unsigned)q.col_tiles, (unsigned)((q.rows + 127) / 128 * 2));
+    if (bf16)
+      mx_quantize_t_kernel<<<grid, 256, 0, st>>>(static_cast<const __nv_bfloat16*>(x), ld, q);
+    else
+      mx_quantize_t_kernel<<<grid, 256, 0, st>>>(static_cast<const float*>(x), ld, q);
+  } else {
+    const long long want = ((q.rows + 127) / 128 * 128 * q.col_tiles + 7) / 8;
+    const int blocks = (int)(want < 148 * 16 ? want : 148 * 16);
+    if (bf16)
+      mx_quantize_kernel<<<blocks, 256, 0, st>>>(static_cast<const __nv_bfloat16*>(x), ld, q);
+    else
+      mx_quantize_kernel<<<blocks, 256, 0, st>>>(static_cast<const float*>(x), ld, q);
+  }
+  return cudaGetLastError();
+}
+
+cudaError_t mx_dequantize(const MxView& q, void* out, int bf16, long long ld, cudaStream_t st) {
+  const long long want = (q.rows * q.col_tiles + 7) / 8;
+  const int blocks = (int)(want < 148 * 16 ? want : 148 * 16);
+  if (bf16)
+    mx_dequantize_kernel<<<blocks, 256, 0, st>>>(q, static_cast<__nv_bfloat16*>(out), ld);
+  else
+    mx_dequantize_kernel<<<blocks, 256, 0, st>>>(q, static_cast<float*>(out), ld);
+  return cudaGetLastError();
+}
+
+cudaError_t mx_gemm(const MxGemm& p, cudaStream_t st, const char** why) {
+  *why = "";
+  static std::atomic<int> known[MAX_DEVICES];
+  int sms = 0;
+  cudaError_t e = device_ready(known, set_attributes, &sms, why);
+  if (e != cudaSuccess) return e;
+  // wide tiles once they fill the machine
+  const long long wide = ((p.a.rows + 127) / 128) * ((p.b.rows + 255) / 256);
+  if (wide >= sms) return launch_mx_gemm<256>(p, sms, st, why);
+  return launch_mx_gemm<64>(p, sms, st, why);
+}
+
+}  // namespace gcada
