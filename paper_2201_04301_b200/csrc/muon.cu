@@ -13,8 +13,8 @@
 //     result's norm; with X kept in 11 bits 2e-2 / 4e-2 / 1.4e-3; in bf16 2e-1 / 3e-1 / 1.3e-2.)
 //   - precision FULL: each product is lo*hi' + hi*lo' + hi*hi' (the smallest terms first), which is fp32 accuracy
 //     (simulated 4e-7 .. 8e-6 of the result's norm on the same spectra, fp32 arithmetic itself 6e-6 .. 3e-5).
-// A and b A + c A^2 are symmetric: only tiles that touch the upper triangle are computed, each element is written
-// to both places, and the polynomial can be read as either operand.
+// A and b A + c A^2 are symmetric: only blocks on and above the diagonal are computed and stored.  An operand block
+// below it is copied from its mirror image and multiplied as the transposed (MN-major) operand that it then is.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>
@@ -29,16 +29,18 @@
 namespace gcada {
 namespace {
 
-constexpr int BM = 128, BN = 256, BK = 64;
+constexpr int TR = 128, BK = 64;                       // rows of an operand block; K values of a stage
 constexpr int BLK_BYTES = 64 * BK * 2;                 // one copy box: 64 x 64 fp16
-constexpr int STAGE_BYTES = (BM + BN) * BK * 2;        // 48 KiB
-constexpr int STAGES = 4;
+constexpr int OP_BYTES = TR * BK * 2;                  // one operand block: 16 KiB
+constexpr int STAGE_BYTES = 2 * OP_BYTES;
+constexpr int STAGES = 6;                              // even: a stage of hi parts is followed by its lo parts
 constexpr int EPI_WARPS = 8;
 constexpr int THREADS = 64 + 32 * EPI_WARPS;
 constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + 1024;
+constexpr int CHUNK = 4;                               // FULL: stage pairs summed in tensor memory before the sum
+                                                       // moves to registers
 constexpr float SCALE = 1024.f;                        // stored value = SCALE * matrix element
 constexpr float INV_SCALE = 1.f / 1024.f;
-constexpr uint32_t IDESC = (1u << 4) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);  // fp16 operands, fp32 sum
 constexpr int NORM_BLOCKS = 296;                       // partial sums of a matrix's squared norm
 
 enum { OUT_SPLIT = 0, OUT_F32 = 1, OUT_BF16 = 2, OUT_UPDATE_F32 = 3, OUT_UPDATE_BF16 = 4 };
@@ -47,16 +49,21 @@ enum { OUT_SPLIT = 0, OUT_F32 = 1, OUT_BF16 = 2, OUT_UPDATE_F32 = 3, OUT_UPDATE_
 // iterate is then SCALE * X_j / rho_j with powers of two rho_0 ~ ||X_0||, rho_{j+1} = min(1, rho_j g), g >= |a|: an
 // iterate that small grows by |a| a step.  For every other matrix all rho are 1.
 constexpr int MAX_STEPS = 100;
-enum { RHO_NONE = 0, RHO_POLY = 1, RHO_APPLY = 2, RHO_LAST = 3 };
+enum { PROD_GRAM = 0, PROD_POLY = 1, PROD_APPLY = 2, PROD_LAST = 3 };
 
 struct NsGemm {
   int M, N, K, batch;
+  int prod;              // PROD_*
   int a_mn, b_mn;        // the operand's M / N index is the contiguous one of its array
-  int sym;               // the result is symmetric (M == N)
-  int terms;             // 1: hi*hi, 3: lo*hi + hi*lo + hi*hi
-  float c_src, c_acc;    // value = c_src * src + c_acc * accumulator, times factors of the iterate's own scale rho:
-  int rho_mode;          // RHO_*
-  const float* rho;      // [batch][MAX_STEPS + 1]; entry `step_no` is that of the iterate the step starts from
+  int sym;               // the result is symmetric (M == N): only its upper blocks of 2^sym_log rows are written
+  int a_sym, b_sym;      // so is the operand: a block below the diagonal is read as the transpose of its mirror image
+  int sym_log;           // 7 or 8 (8 wherever a pair of CTAs takes part)
+  int split;             // CTAs of a cluster that share a tile's K range
+  float c_src, c_acc;    // value = c_src * src + c_acc * accumulator, times powers of rho
+  float diag;            // symmetric results: added on the diagonal (see ns_run on the shifted form)
+  float c_src_shift;     // PROD_APPLY / PROD_LAST in the shifted form: added to c_src
+  float c_src_plain;     // PROD_POLY in the shifted form: c_src where the form does not apply
+  const float* rho;      // [batch][MAX_STEPS + 1]; entry step_no is that of the iterate the step starts from
   int step_no;
   const __half* src;     // [batch][2][.][ld_src] hi / lo planes, or null
   long long ld_src, src_plane;
@@ -70,69 +77,212 @@ struct NsGemm {
   int* err;
 };
 
-// Tiles of 128 x 256; of a symmetric result only those with an element on or above the diagonal: row mt starts at
-// column tile mt / 2.
-__device__ __forceinline__ void tile_of(int u, int tiles_m, int tiles_n, int sym, int& mt, int& nt) {
+// Square tiles; of a symmetric result only those in the upper blocks of 2^g tiles (g = 0 or 1).
+__device__ __forceinline__ void tile_of(int u, int tiles_n, int sym, int g, int& mt, int& nt) {
   if (!sym) {
     mt = u / tiles_n;
     nt = u - mt * tiles_n;
     return;
   }
-  for (mt = 0; mt < tiles_m; ++mt) {
-    const int w = tiles_n - mt / 2;
+  for (mt = 0;; ++mt) {
+    const int w = tiles_n - (mt >> g << g);
     if (u < w) break;
     u -= w;
   }
-  nt = mt / 2 + u;
+  nt = (mt >> g << g) + u;
 }
-__host__ __device__ inline int tile_count(int tiles_m, int tiles_n, int sym) {
+__host__ __device__ inline int tile_count(int tiles_m, int tiles_n, int sym, int g) {
   if (!sym) return tiles_m * tiles_n;
   int n = 0;
-  for (int mt = 0; mt < tiles_m; ++mt) n += tiles_n - mt / 2;
+  for (int mt = 0; mt < tiles_m; ++mt) n += tiles_n - (mt >> g << g);
   return n;
 }
 
-__device__ __forceinline__ void tc_mma_f16(uint32_t tmem_c, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accum) {
-  tc_mma_bf16(tmem_c, da, db, idesc, accum);  // kind::f16 covers both 16-bit types; the descriptor says which
+// Eight 32-bit words at once: a thread's 32 bytes are one whole sector of the memory system.
+struct Words8 {
+  uint32_t w[8];
+};
+__device__ __forceinline__ Words8 load32(const void* p) {
+  Words8 r;
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]),
+                 "=r"(r.w[7])
+               : "l"(p));
+  return r;
+}
+__device__ __forceinline__ void store32(void* p, const uint32_t (&w)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+               "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
+__device__ __forceinline__ uint32_t pack_half2(float x, float y) {
+  const __half2 h = __floats2half2_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float2 unpack_half2(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+
+// What an epilogue thread needs for the tile at hand.
+struct RowCtx {
+  int m;
+  float c_src, c_acc, diag;
+  const __half* src;  // row m
+  __half* dst;        // matrix
+  void* user;         // row m
+};
+__device__ __forceinline__ RowCtx row_ctx(const NsGemm& a, int b, int m) {
+  RowCtx r;
+  r.m = m;
+  const float* rho = a.rho + (long long)b * (MAX_STEPS + 1) + a.step_no;
+  const float r0 = rho[0];
+  const bool plain = r0 == 1.f;
+  r.c_src = a.c_src;
+  r.c_acc = a.c_acc;
+  r.diag = plain ? a.diag : 0.f;
+  if (a.prod == PROD_POLY) {
+    const float k = r0 * r0;
+    if (!plain) r.c_src = a.c_src_plain;
+    r.c_src *= k;
+    r.c_acc *= k * k;
+  } else if (a.prod != PROD_GRAM) {
+    const float k = a.prod == PROD_APPLY ? r0 / rho[1] : r0;
+    if (plain) r.c_src += a.c_src_shift;
+    r.c_src *= k;
+    r.c_acc *= k;
+  }
+  r.src = a.src ? a.src + (long long)b * 2 * a.src_plane + (long long)m * a.ld_src : nullptr;
+  r.dst = a.dst + (long long)b * 2 * a.dst_plane;
+  const long long o = (long long)b * a.user_stride + (long long)m * a.ld_user;
+  r.user = a.out == OUT_F32 || a.out == OUT_UPDATE_F32 ? (void*)(static_cast<float*>(a.user) + o)
+                                                        : (void*)(static_cast<__nv_bfloat16*>(a.user) + o);
+  return r;
 }
 
-// v[0..7] += or -> helpers on eight consecutive columns
-__device__ __forceinline__ void load_split8(const __half* hi, const __half* lo, float (&f)[8]) {
-  const uint4 h = *reinterpret_cast<const uint4*>(hi), l = *reinterpret_cast<const uint4*>(lo);
-  const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, lw[4] = {l.x, l.y, l.z, l.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&hw[i]));
-    const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&lw[i]));
-    f[2 * i] = a.x + b.x;
-    f[2 * i + 1] = a.y + b.y;
-  }
+// Sixteen columns from n of row r.m (in range; n is a multiple of 16, columns from a.N on are padding or absent).
+struct Src16 {
+  Words8 hi, lo;
+};
+__device__ __forceinline__ Src16 load_src16(const NsGemm& a, const RowCtx& r, int n) {
+  Src16 s;
+  s.hi = load32(r.src + n);
+  s.lo = load32(r.src + a.src_plane + n);
+  return s;
 }
-__device__ __forceinline__ void split8(const float (&f)[8], uint4& h, uint4& l) {
-  uint32_t hw[4], lw[4];
+// Whether a thread has anything to do with the columns from n: below the diagonal blocks nothing is kept.
+__device__ __forceinline__ bool wanted(const NsGemm& a, int m, int n) {
+  return n < a.N && !(a.sym && (m >> a.sym_log) > (n >> a.sym_log));
+}
+__device__ __forceinline__ void finish16(const NsGemm& a, const RowCtx& r, int n, float (&f)[16], const Src16& s) {
+  const int m = r.m;
+  if (r.src) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __half2 a = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
-    const float2 b = __half22float2(a);
-    const __half2 c = __floats2half2_rn(f[2 * i] - b.x, f[2 * i + 1] - b.y);
-    hw[i] = *reinterpret_cast<const uint32_t*>(&a);
-    lw[i] = *reinterpret_cast<const uint32_t*>(&c);
+    for (int j = 0; j < 8; ++j) {
+      const float2 h = unpack_half2(s.hi.w[j]), l = unpack_half2(s.lo.w[j]);
+      f[2 * j] = r.c_src * (h.x + l.x) + r.c_acc * f[2 * j];
+      f[2 * j + 1] = r.c_src * (h.y + l.y) + r.c_acc * f[2 * j + 1];
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) f[j] = r.c_acc * f[j];
   }
-  h = make_uint4(hw[0], hw[1], hw[2], hw[3]);
-  l = make_uint4(lw[0], lw[1], lw[2], lw[3]);
+  if (a.out == OUT_SPLIT) {
+    if (a.sym && m >= n && m < n + 16) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j)
+        if (n + j == m) f[j] += r.diag;
+    }
+    uint32_t h[8], l[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      h[j] = pack_half2(f[2 * j], f[2 * j + 1]);
+      const float2 b = unpack_half2(h[j]);
+      l[j] = pack_half2(f[2 * j] - b.x, f[2 * j + 1] - b.y);
+    }
+    __half* o = r.dst + (long long)m * a.ld_dst + n;
+    store32(o, h);
+    if (a.write_lo) store32(o + a.dst_plane, l);
+  } else if (a.out == OUT_F32 || a.out == OUT_UPDATE_F32) {
+    float* o = static_cast<float*>(r.user) + n;
+    const bool upd = a.out == OUT_UPDATE_F32;
+    if (n + 16 <= a.N && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+      float4 p[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (upd) p[j] = *reinterpret_cast<const float4*>(o + 4 * j);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float4 w = make_float4(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]);
+        if (upd)
+          w = make_float4(a.decay * p[j].x - a.step * w.x, a.decay * p[j].y - a.step * w.y,
+                          a.decay * p[j].z - a.step * w.z, a.decay * p[j].w - a.step * w.w);
+        *reinterpret_cast<float4*>(o + 4 * j) = w;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 16; ++j)
+        if (n + j < a.N) o[j] = upd ? a.decay * o[j] - a.step * f[j] : f[j];
+    }
+  } else {
+    __nv_bfloat16* o = static_cast<__nv_bfloat16*>(r.user) + n;
+    const bool upd = a.out == OUT_UPDATE_BF16;
+    if (n + 16 <= a.N && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+      uint4* o4 = reinterpret_cast<uint4*>(o);
+      if (upd) {
+        const uint4 p = o4[0], q = o4[1];
+        const uint32_t pw[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          f[j] = a.decay * __uint_as_float(j & 1 ? pw[j >> 1] & 0xffff0000u : pw[j >> 1] << 16) - a.step * f[j];
+      }
+      uint32_t w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const __nv_bfloat162 t = __floats2bfloat162_rn(f[2 * j], f[2 * j + 1]);
+        w[j] = *reinterpret_cast<const uint32_t*>(&t);
+      }
+      o4[0] = make_uint4(w[0], w[1], w[2], w[3]);
+      o4[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 16; ++j)
+        if (n + j < a.N) o[j] = __float2bfloat16_rn(upd ? a.decay * __bfloat162float(o[j]) - a.step * f[j] : f[j]);
+    }
+  }
 }
 
+// One product.  Warp 0 copies operand blocks (128 rows or columns x 64 K values) into a ring of stages, warp 1
+// issues the tcgen05 products into one of two accumulators, eight warps finish the other one.
+//   PAIR: the two CTAs of a cluster work on one 256 x 256 tile (cta_group::2): each holds 128 rows of A, 128 of the
+//         256 columns of B and 128 rows of the result, so a stage of 32 KiB feeds 512 cycles of the tensor core: 64
+//         bytes a cycle, what an SM can take from L2.  (A single CTA's 128 x 256 tile needs 94.)
+//   else: a CTA has its own 128 x 128 tile and, when there are fewer tiles than SMs, shares its K range with the
+//         other CTAs of its cluster: each leaves its partial tile in shared memory and adds up (in rank order) the
+//         columns that fall to it.
+// FULL: stages alternate between hi and lo parts, three products for each pair; the sum of CHUNK pairs moves to
+// registers, because the tensor cores cut (not round) each partial sum.
+template <bool PAIR, bool FULL>
 __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_constant__ CUtensorMap tmA,
                                                              const __grid_constant__ CUtensorMap tmB, const NsGemm a) {
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   __shared__ uint64_t full_bar[STAGES], empty_bar[STAGES], tfull_bar[2], tempty_bar[2];
   __shared__ uint32_t tmem_base_sm;
+  constexpr int TILE = PAIR ? 256 : 128;
+  constexpr int WCOLS = TILE / 2;                // columns of an epilogue warp
+  constexpr uint32_t TMEM_COLS = 2 * TILE;
   unsigned char* tiles = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int tiles_m = (a.M + BM - 1) / BM, tiles_n = (a.N + BN - 1) / BN;
-  const int per = tile_count(tiles_m, tiles_n, a.sym), total = per * a.batch;
-  const int nkb = (a.K + BK - 1) / BK, steps = nkb * a.terms;
-  const int n_local = (int)blockIdx.x < total ? (total - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x : 0;
+  const int csize = PAIR ? 2 : a.split;
+  const int rank = csize > 1 ? (int)cluster_rank() : 0;
+  const int first = (int)blockIdx.x / csize, stride = (int)gridDim.x / csize;
+  const int tiles_m = (a.M + TILE - 1) / TILE, tiles_n = (a.N + TILE - 1) / TILE;
+  const int g_tiles = PAIR ? 0 : a.sym_log - 7;  // log2 of the tiles in a symmetric block
+  const int per = tile_count(tiles_m, tiles_n, a.sym, g_tiles), total = per * a.batch;
+  const int n_local = first < total ? (total - first + stride - 1) / stride : 0;
+  const int kb_all = (a.K + BK - 1) / BK;
+  // this CTA's K blocks
+  const int kb0 = PAIR ? 0 : (int)((long long)kb_all * rank / csize);
+  const int kb1 = PAIR ? kb_all : (int)((long long)kb_all * (rank + 1) / csize);
+  const int nkb = kb1 - kb0;
+  const int chunks = FULL ? (nkb + CHUNK - 1) / CHUNK : 1;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {
@@ -141,76 +291,105 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
     }
     for (int s = 0; s < 2; ++s) {
       mbar_init(&tfull_bar[s], 1);
-      mbar_init(&tempty_bar[s], EPI_WARPS);
+      mbar_init(&tempty_bar[s], PAIR ? 2 * EPI_WARPS : EPI_WARPS);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_sm)),
-                 "r"(512u)
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
+  if (warp == 1) tmem_alloc<PAIR>(&tmem_base_sm, TMEM_COLS);
   tc_fence_before();
   __syncthreads();
+  if (PAIR) cluster_sync();  // the peer's barriers exist
   tc_fence_after();
   const uint32_t tmem_base = tmem_base_sm;
+  pdl_launch_dependents();
+  pdl_wait();
 
   if (warp == 0) {
     if (lane == 0) {
       bool ok = true;
       int it = 0;
       for (int i = 0; i < n_local && ok; ++i) {
-        const int u = (int)blockIdx.x + i * (int)gridDim.x, b = u / per;
+        const int u = first + i * stride, b = u / per;
         int mt, nt;
-        tile_of(u - b * per, tiles_m, tiles_n, a.sym, mt, nt);
-        for (int s0 = 0; s0 < steps; ++s0, ++it) {
-          const int t = a.terms == 1 ? 2 : s0 / nkb, kc = (a.terms == 1 ? s0 : s0 - t * nkb) * BK;
-          const int zA = 2 * b + (t == 0 ? 1 : 0), zB = 2 * b + (t == 1 ? 1 : 0);  // plane 0 = hi, 1 = lo
-          const int s = it % STAGES;
-          ok = mbar_spin_bounded(&empty_bar[s], (uint32_t)(((it / STAGES) & 1) ^ 1));
-          if (!ok) break;
-          unsigned char* sa = tiles + (size_t)s * STAGE_BYTES;
-          mbar_expect_tx(&full_bar[s], STAGE_BYTES);
+        tile_of(u - b * per, tiles_n, a.sym, g_tiles, mt, nt);
+        const int rA = PAIR ? mt * 256 + rank * 128 : mt * 128, rB = PAIR ? nt * 256 + rank * 128 : nt * 128;
+        for (int kb = kb0; kb < kb1 && ok; ++kb) {
+          const int kblk = kb * BK >> a.sym_log;
+          const bool mnA = a.a_mn || (a.a_sym && kblk < rA >> a.sym_log), mnB = a.b_mn || (a.b_sym && kblk < rB >> a.sym_log);
 #pragma unroll
-          for (int j = 0; j < BM / 64; ++j) {
-            const int r = mt * BM + j * 64;
-            tma_load_3d(sa + j * BLK_BYTES, &tmA, a.a_mn ? r : kc, a.a_mn ? kc : r, zA, &full_bar[s]);
-          }
+          for (int t = 0; t < (FULL ? 2 : 1); ++t, ++it) {  // plane 0 = hi, 1 = lo
+            const int s = it % STAGES, kc = kb * BK, z = 2 * b + t;
+            ok = mbar_spin_bounded(&empty_bar[s], (uint32_t)(((it / STAGES) & 1) ^ 1));
+            if (!ok) break;
+            unsigned char* sa = tiles + (size_t)s * STAGE_BYTES;
+            if (!PAIR || rank == 0) mbar_expect_tx(&full_bar[s], PAIR ? 2 * STAGE_BYTES : STAGE_BYTES);
+            // a pair's copies are all counted by its first CTA, whose thread issues the products
+            const uint32_t bar = PAIR ? cluster_map(smem_u32(&full_bar[s]), 0) : smem_u32(&full_bar[s]);
 #pragma unroll
-          for (int j = 0; j < BN / 64; ++j) {
-            const int r = nt * BN + j * 64;
-            tma_load_3d(sa + BM * BK * 2 + j * BLK_BYTES, &tmB, a.b_mn ? r : kc, a.b_mn ? kc : r, zB, &full_bar[s]);
+            for (int j = 0; j < 2; ++j) {
+              const int r = rA + j * 64;
+              tma_load_3d_to<PAIR>(sa + j * BLK_BYTES, &tmA, mnA ? r : kc, mnA ? kc : r, z, bar);
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const int r = rB + j * 64;
+              tma_load_3d_to<PAIR>(sa + OP_BYTES + j * BLK_BYTES, &tmB, mnB ? r : kc, mnB ? kc : r, z, bar);
+            }
           }
         }
       }
       if (!ok) raise_error(a.err);
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      const uint32_t idesc = IDESC | (a.a_mn ? 1u << 15 : 0u) | (a.b_mn ? 1u << 16 : 0u);
-      const uint64_t ka = a.a_mn ? 128u : 2u, kb = a.b_mn ? 128u : 2u;  // descriptor step of 16 K values
+    if (lane == 0 && (!PAIR || rank == 0)) {
+      // fp16 operands, fp32 sum
+      constexpr uint32_t IDESC = (1u << 4) | ((uint32_t)(TILE >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24);
       bool ok = true;
-      int it = 0;
+      int it = 0, acc_no = 0;
       for (int i = 0; i < n_local && ok; ++i) {
-        const int slot = i & 1;
-        ok = mbar_spin_bounded(&tempty_bar[slot], (uint32_t)(((i >> 1) & 1) ^ 1));
-        if (!ok) break;
-        tc_fence_after();
-        for (int s0 = 0; s0 < steps && ok; ++s0, ++it) {
-          const int s = it % STAGES;
-          ok = mbar_spin_bounded(&full_bar[s], (uint32_t)((it / STAGES) & 1));
+        const int u = first + i * stride, b = u / per;
+        int mt, nt;
+        tile_of(u - b * per, tiles_n, a.sym, g_tiles, mt, nt);
+        const int blkA = mt * TILE >> a.sym_log, blkB = nt * TILE >> a.sym_log;
+        for (int c = 0; c < chunks && ok; ++c, ++acc_no) {
+          const int slot = acc_no & 1;
+          ok = mbar_spin_bounded(&tempty_bar[slot], (uint32_t)(((acc_no >> 1) & 1) ^ 1));
           if (!ok) break;
           tc_fence_after();
-          const uint32_t sa = smem_u32(tiles + (size_t)s * STAGE_BYTES);
-          const uint64_t da = a.a_mn ? make_desc_mn(sa) : make_desc(sa);
-          const uint64_t db = a.b_mn ? make_desc_mn(sa + BM * BK * 2) : make_desc(sa + BM * BK * 2);
+          const uint32_t d = tmem_base + (uint32_t)(slot * TILE);
+          const int n = FULL ? (c == chunks - 1 ? nkb - c * CHUNK : CHUNK) : nkb;
+          for (int kb = 0; kb < n && ok; ++kb) {
+            const int kblk = (kb0 + c * CHUNK + kb) * BK >> a.sym_log;
+            const bool mnA = a.a_mn || (a.a_sym && kblk < blkA), mnB = a.b_mn || (a.b_sym && kblk < blkB);
+            const uint32_t idesc = IDESC | (mnA ? 1u << 15 : 0u) | (mnB ? 1u << 16 : 0u);
+            const uint64_t ka = mnA ? 128u : 2u, kk_b = mnB ? 128u : 2u;  // descriptor step of 16 K values
+            uint64_t da[2], db[2];
+            int st[2];
 #pragma unroll
-          for (int kk = 0; kk < BK / 16; ++kk)
-            tc_mma_f16(tmem_base + (uint32_t)(slot * BN), da + kk * ka, db + kk * kb, idesc, (s0 | kk) != 0 ? 1u : 0u);
-          tc_commit(&empty_bar[s]);
+            for (int t = 0; t < (FULL ? 2 : 1); ++t, ++it) {
+              const int s = it % STAGES;
+              st[t] = s;
+              ok = ok && mbar_spin_bounded(&full_bar[s], (uint32_t)((it / STAGES) & 1));
+              const uint32_t sa = smem_u32(tiles + (size_t)s * STAGE_BYTES);
+              da[t] = mnA ? make_desc_mn(sa) : make_desc(sa);
+              db[t] = mnB ? make_desc_mn(sa + OP_BYTES) : make_desc(sa + OP_BYTES);
+            }
+            if (!ok) break;
+            tc_fence_after();
+            if (FULL) {  // the smallest products first
+#pragma unroll
+              for (int kk = 0; kk < BK / 16; ++kk) tc_mma<PAIR>(d, da[1] + kk * ka, db[0] + kk * kk_b, idesc, (kb | kk) != 0 ? 1u : 0u);
+#pragma unroll
+              for (int kk = 0; kk < BK / 16; ++kk) tc_mma<PAIR>(d, da[0] + kk * ka, db[1] + kk * kk_b, idesc, 1u);
+              tc_commit_to<PAIR>(&empty_bar[st[1]]);
+            }
+#pragma unroll
+            for (int kk = 0; kk < BK / 16; ++kk)
+              tc_mma<PAIR>(d, da[0] + kk * ka, db[0] + kk * kk_b, idesc, FULL || (kb | kk) != 0 ? 1u : 0u);
+            tc_commit_to<PAIR>(&empty_bar[st[0]]);
+          }
+          if (ok) tc_commit_to<PAIR>(&tfull_bar[slot]);
         }
-        if (ok) tc_commit(&tfull_bar[slot]);
       }
       if (!ok) raise_error(a.err);
     }
@@ -218,134 +397,135 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
     // epilogue: warp w may touch TMEM lanes 32*(w%4) .. +31; the two warps of a quadrant split the columns
     const int quad = warp & 3, half = (warp - 2) >> 2;
     bool ok = true;
+    int acc_no = 0;
     for (int i = 0; i < n_local; ++i) {
-      const int slot = i & 1;
-      const int u = (int)blockIdx.x + i * (int)gridDim.x, b = u / per;
+      const int u = first + i * stride, b = u / per;
       int mt, nt;
-      tile_of(u - b * per, tiles_m, tiles_n, a.sym, mt, nt);
-      const int m = mt * BM + quad * 32 + lane;
-      if (ok) {
-        ok = mbar_wait_bounded(&tfull_bar[slot], (uint32_t)((i >> 1) & 1));
-        ok = __all_sync(0xffffffffu, ok);
-      }
-      if (!ok) continue;
-      tc_fence_after();
-      const uint32_t tbase = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(slot * BN);
-      const __half* src = a.src ? a.src + (long long)b * 2 * a.src_plane + (long long)m * a.ld_src : nullptr;
-      __half* dst = a.dst + (long long)b * 2 * a.dst_plane;
-      float c_src = a.c_src, c_acc = a.c_acc;
-      if (a.rho_mode != RHO_NONE) {
-        const float* r = a.rho + (long long)b * (MAX_STEPS + 1) + a.step_no;
-        const float r0 = r[0], k = a.rho_mode == RHO_APPLY ? r0 / r[1] : (a.rho_mode == RHO_LAST ? r0 : r0 * r0);
-        c_src *= k;
-        c_acc *= a.rho_mode == RHO_POLY ? k * k : k;
-      }
-      auto chunk = [&](const uint32_t (&v)[32], int c) {
-        const int n0 = nt * BN + c;
-        if (m >= a.M || n0 >= a.N) return;
+      tile_of(u - b * per, tiles_n, a.sym, g_tiles, mt, nt);
+      const int m = mt * TILE + (PAIR ? rank * 128 : 0) + quad * 32 + lane;
+      const int c0 = half * WCOLS, n0 = nt * TILE + c0;
+      const bool row_ok = m < a.M;
+      RowCtx r{};
+      if (row_ok) r = row_ctx(a, b, m);
+      const bool direct = PAIR || csize == 1;
+      // the linear term's values do not depend on the products: those of the next 32 columns are always on their way
+      // (not with FULL, whose sums fill the registers)
+      Src16 next[2];
+      auto fetch = [&](int q) {
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int n = n0 + 8 * g;
-          if (n >= a.N) break;
-          float f[8];
-          if (src) {
-            load_split8(src + n, src + a.src_plane + n, f);
+        for (int h = 0; h < 2; ++h)
+          if (direct && row_ok && r.src && wanted(a, m, n0 + q + 16 * h)) next[h] = load_src16(a, r, n0 + q + 16 * h);
+      };
+      auto finish = [&](const float* v, int q) {
+        Src16 now[2];
+        if (!FULL) {
+          now[0] = next[0];
+          now[1] = next[1];
+          if (q + 32 < WCOLS) fetch(q + 32);
+        }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] = c_src * f[j] + c_acc * __uint_as_float(v[8 * g + j]);
-          } else {
+        for (int h = 0; h < 2; ++h) {
+          if (row_ok && wanted(a, m, n0 + q + 16 * h)) {
+            if (FULL && r.src) now[h] = load_src16(a, r, n0 + q + 16 * h);
+            float f[16];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] = c_acc * __uint_as_float(v[8 * g + j]);
-          }
-          if (a.out == OUT_SPLIT) {
-            uint4 h, l;
-            split8(f, h, l);
-            if (!a.sym) {
-              *reinterpret_cast<uint4*>(dst + (long long)m * a.ld_dst + n) = h;
-              if (a.write_lo) *reinterpret_cast<uint4*>(dst + a.dst_plane + (long long)m * a.ld_dst + n) = l;
-            } else {
-              const __half* h8 = reinterpret_cast<const __half*>(&h);
-              const __half* l8 = reinterpret_cast<const __half*>(&l);
-              if (n >= m) {
-                *reinterpret_cast<uint4*>(dst + (long long)m * a.ld_dst + n) = h;
-                if (a.write_lo) *reinterpret_cast<uint4*>(dst + a.dst_plane + (long long)m * a.ld_dst + n) = l;
-              }
-#pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                if (n + j >= a.N || n + j < m) continue;  // below the diagonal: the mirrored element is written
-                if (n < m) {
-                  dst[(long long)m * a.ld_dst + n + j] = h8[j];
-                  if (a.write_lo) dst[a.dst_plane + (long long)m * a.ld_dst + n + j] = l8[j];
-                }
-                if (n + j > m) {
-                  dst[(long long)(n + j) * a.ld_dst + m] = h8[j];
-                  if (a.write_lo) dst[a.dst_plane + (long long)(n + j) * a.ld_dst + m] = l8[j];
-                }
-              }
-            }
-          } else if (a.out == OUT_F32 || a.out == OUT_UPDATE_F32) {
-            float* o = static_cast<float*>(a.user) + (long long)b * a.user_stride + (long long)m * a.ld_user + n;
-            const bool upd = a.out == OUT_UPDATE_F32;
-            if (n + 8 <= a.N && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
-#pragma unroll
-              for (int j = 0; j < 8; j += 4) {
-                float4 w = make_float4(f[j], f[j + 1], f[j + 2], f[j + 3]);
-                if (upd) {
-                  const float4 p = *reinterpret_cast<const float4*>(o + j);
-                  w = make_float4(a.decay * p.x - a.step * w.x, a.decay * p.y - a.step * w.y,
-                                  a.decay * p.z - a.step * w.z, a.decay * p.w - a.step * w.w);
-                }
-                *reinterpret_cast<float4*>(o + j) = w;
-              }
-            } else {
-#pragma unroll
-              for (int j = 0; j < 8; ++j)
-                if (n + j < a.N) o[j] = upd ? a.decay * o[j] - a.step * f[j] : f[j];
-            }
-          } else {
-            __nv_bfloat16* o =
-                static_cast<__nv_bfloat16*>(a.user) + (long long)b * a.user_stride + (long long)m * a.ld_user + n;
-            const bool upd = a.out == OUT_UPDATE_BF16;
-            if (n + 8 <= a.N && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
-              if (upd) {
-                const uint4 p = *reinterpret_cast<const uint4*>(o);
-                const uint32_t pw[4] = {p.x, p.y, p.z, p.w};
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                  f[j] = a.decay * __uint_as_float(j & 1 ? pw[j >> 1] & 0xffff0000u : pw[j >> 1] << 16) - a.step * f[j];
-              }
-              uint32_t w[4];
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const __nv_bfloat162 t = __floats2bfloat162_rn(f[2 * j], f[2 * j + 1]);
-                w[j] = *reinterpret_cast<const uint32_t*>(&t);
-              }
-              *reinterpret_cast<uint4*>(o) = make_uint4(w[0], w[1], w[2], w[3]);
-            } else {
-#pragma unroll
-              for (int j = 0; j < 8; ++j)
-                if (n + j < a.N)
-                  o[j] = __float2bfloat16_rn(upd ? a.decay * __bfloat162float(o[j]) - a.step * f[j] : f[j]);
-            }
+            for (int j = 0; j < 16; ++j) f[j] = v[16 * h + j];
+            finish16(a, r, n0 + q + 16 * h, f, now[h]);
           }
         }
       };
-      for (int c = half * (BN / 2); c < (half + 1) * (BN / 2); c += 32) {
-        uint32_t v[32];
-        tc_ld32_issue(tbase + (uint32_t)c, v);
-        tc_ld_wait();
-        chunk(v, c);
+      if (!FULL) fetch(0);
+      float sum[FULL ? WCOLS : 1];
+      for (int c = 0; c < chunks; ++c, ++acc_no) {
+        const int slot = acc_no & 1;
+        if (ok) {
+          ok = mbar_wait_bounded(&tfull_bar[slot], (uint32_t)((acc_no >> 1) & 1));
+          ok = __all_sync(0xffffffffu, ok);
+        }
+        if (!ok) continue;
+        tc_fence_after();
+        const uint32_t tbase = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(slot * TILE + c0);
+#pragma unroll
+        for (int q = 0; q < WCOLS; q += 32) {
+          uint32_t v[32];
+          tc_ld32_issue(tbase + (uint32_t)q, v);
+          tc_ld_wait();
+          if (FULL) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) sum[q + j] = (c == 0 ? 0.f : sum[q + j]) + __uint_as_float(v[j]);
+          } else if (!direct) {
+            float* part = reinterpret_cast<float*>(tiles) + (size_t)(c0 + q) * TR + quad * 32 + lane;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) part[j * TR] = __uint_as_float(v[j]);
+          } else {
+            float f[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]);
+            finish(f, q);
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if (PAIR)
+            mbar_arrive_cluster(cluster_map(smem_u32(&tempty_bar[slot]), 0));
+          else
+            mbar_arrive(&tempty_bar[slot]);
+        }
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&tempty_bar[slot]);
+      if (FULL && ok) {
+        if (!direct) {
+          float* part = reinterpret_cast<float*>(tiles) + (size_t)c0 * TR + quad * 32 + lane;
+#pragma unroll
+          for (int j = 0; j < WCOLS; ++j) part[j * TR] = sum[FULL ? j : 0];
+        } else {
+#pragma unroll
+          for (int q = 0; q < WCOLS; q += 32) finish(sum + (FULL ? q : 0), q);
+        }
+      }
     }
     if (!ok && lane == 0) raise_error(a.err);
   }
+  if (!PAIR && csize > 1) {
+    // one tile per cluster: the partial tiles are complete (every stage has been consumed before they were written)
+    __syncwarp();
+    cluster_sync();
+    if (warp >= 2) {
+      const int quad = warp & 3, half = (warp - 2) >> 2;
+      const int b = first / per;
+      int mt, nt;
+      tile_of(first - b * per, tiles_n, a.sym, g_tiles, mt, nt);
+      // this CTA's columns, 16 at a time, dealt to the two warps of a quadrant
+      const int m = mt * TILE + quad * 32 + lane, mine = TILE / csize;
+      if (m < a.M) {
+        const RowCtx r = row_ctx(a, b, m);
+        for (int c = rank * mine + half * 16; c < (rank + 1) * mine; c += 32) {
+          const int n = nt * TILE + c;
+          if (!wanted(a, m, n)) continue;
+          Src16 s;
+          if (r.src) s = load_src16(a, r, n);
+          float f[16];
+#pragma unroll
+          for (int j = 0; j < 16; ++j) f[j] = 0.f;
+          for (int p = 0; p < csize; ++p) {
+            const uint32_t from = cluster_map(smem_u32(tiles), (uint32_t)p) + (uint32_t)((c * TR + quad * 32 + lane) * 4);
+            float x[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) x[j] = cluster_load(from + (uint32_t)(j * TR * 4));
+#pragma unroll
+            for (int j = 0; j < 16; ++j) f[j] += x[j];
+          }
+          finish16(a, r, n, f, s);
+        }
+      }
+    }
+  }
   tc_fence_before();
   __syncthreads();
+  if (csize > 1) cluster_sync();  // nobody reads this CTA's shared or tensor memory any more
   if (warp == 1) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
+    tmem_dealloc<PAIR>(tmem_base, TMEM_COLS);
   }
 }
 
@@ -410,6 +590,20 @@ __device__ __forceinline__ void source8(const NsSource& s, int b, int r, int c, 
 #pragma unroll
     for (int j = 0; j < 8; ++j) f[j] = s.nesterov ? s.omb * f[j] + s.beta * m[j] : m[j];
   }
+}
+
+__device__ __forceinline__ void split8(const float (&f)[8], uint4& h, uint4& l) {
+  uint32_t hw[4], lw[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __half2 a = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+    const float2 b = __half22float2(a);
+    const __half2 c = __floats2half2_rn(f[2 * i] - b.x, f[2 * i + 1] - b.y);
+    hw[i] = *reinterpret_cast<const uint32_t*>(&a);
+    lw[i] = *reinterpret_cast<const uint32_t*>(&c);
+  }
+  h = make_uint4(hw[0], hw[1], hw[2], hw[3]);
+  l = make_uint4(lw[0], lw[1], lw[2], lw[3]);
 }
 
 // Squared Frobenius norm in doubles, NORM_BLOCKS partial sums per matrix (fixed order: bitwise reproducible).
@@ -506,9 +700,9 @@ NsLayout layout(int batch, int rows, int cols) {
   NsLayout L{};
   L.r = rows < cols ? rows : cols;
   L.c = rows < cols ? cols : rows;
-  L.ld_x = (cols + 7) / 8 * 8;
+  L.ld_x = (cols + 15) / 16 * 16;  // rows of whole 32-byte sectors
   L.plane_x = L.ld_x * rows;
-  L.ld_s = (L.r + 7) / 8 * 8;
+  L.ld_s = (L.r + 15) / 16 * 16;
   L.plane_s = L.ld_s * L.r;
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -527,15 +721,67 @@ NsLayout layout(int batch, int rows, int cols) {
 }
 
 cudaError_t set_attributes() {
-  return cudaFuncSetAttribute(ns_gemm_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
+  const cudaFuncAttribute at = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  cudaError_t e = cudaFuncSetAttribute(ns_gemm_kernel<true, true>, at, SMEM_BYTES);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<true, false>, at, SMEM_BYTES);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<false, true>, at, SMEM_BYTES);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<false, false>, at, SMEM_BYTES);
+  return e;
 }
 
-cudaError_t launch_ns_gemm(const CUtensorMap& ta, const CUtensorMap& tb, const NsGemm& a, int sms, cudaStream_t st) {
-  const long long units =
-      (long long)tile_count((a.M + BM - 1) / BM, (a.N + BN - 1) / BN, a.sym) * a.batch;
-  const int ctas = (int)(units < sms ? units : sms);
-  ns_gemm_kernel<<<ctas, THREADS, SMEM_BYTES, st>>>(ta, tb, a);
-  return cudaGetLastError();
+template <bool PAIR, bool FULL>
+cudaError_t launch_shape(const CUtensorMap& ta, const CUtensorMap& tb, const NsGemm& a, int ctas, cudaStream_t st) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)ctas);
+  cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = SMEM_BYTES;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = PAIR ? 2 : (unsigned)a.split;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = PAIR || a.split > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, ns_gemm_kernel<PAIR, FULL>, ta, tb, a);
+}
+
+// A K block costs a CTA the same 32 KiB from L2 in either shape (about 512 cycles), so the shape is the one with
+// fewer K blocks in sequence; `ramp` is what filling and draining a tile costs, in K blocks.
+struct Shape {
+  bool pair;
+  int split, ctas;
+};
+Shape choose_shape(int M, int N, int K, int sym, int batch, int sms) {
+  const int kb = (K + BK - 1) / BK;
+  auto tiles = [&](int t, int g) { return (long long)tile_count((M + t - 1) / t, (N + t - 1) / t, sym, g) * batch; };
+  const long long pairs = tiles(256, 0), singles = tiles(128, 0);
+  const int ramp_pair = 10, ramp_single = 6;
+  Shape s{false, 1, 0};
+  long long cost = (singles + sms - 1) / sms * kb + ramp_single;
+  for (int k = 2; k <= 8 && singles * k <= sms && kb >= 2 * k; k *= 2) {
+    const long long c = (kb + k - 1) / k + ramp_single + 2;
+    if (c < cost) {
+      cost = c;
+      s.split = k;
+    }
+  }
+  if ((pairs + sms / 2 - 1) / (sms / 2) * kb + ramp_pair < cost) s.pair = true;
+  return s;
+}
+
+cudaError_t launch_ns_gemm(const CUtensorMap& ta, const CUtensorMap& tb, NsGemm a, const Shape& s, int full, int sms,
+                           cudaStream_t st) {
+  const int t = s.pair ? 256 : 128;
+  const long long tiles =
+      (long long)tile_count((a.M + t - 1) / t, (a.N + t - 1) / t, a.sym, s.pair ? 0 : a.sym_log - 7) * a.batch;
+  // (a symmetric result kept in blocks of 256 has a few tiles of 128 more than the choice counted: no split then)
+  a.split = tiles * s.split <= sms ? s.split : 1;
+  const long long room = s.pair ? sms / 2 : sms, want = tiles * (s.pair ? 1 : a.split);
+  const int ctas = (int)(want < room ? want : room) * (s.pair ? 2 : 1);
+  if (s.pair) return full ? launch_shape<true, true>(ta, tb, a, ctas, st) : launch_shape<true, false>(ta, tb, a, ctas, st);
+  return full ? launch_shape<false, true>(ta, tb, a, ctas, st) : launch_shape<false, false>(ta, tb, a, ctas, st);
 }
 
 }  // namespace
@@ -600,54 +846,72 @@ cudaError_t ns_run(const NsProblem& p, void* work, cudaStream_t st, const char**
   f.src_plane = L.plane_x;
   f.err = p.err;
   f.rho = rho;
+  const Shape gram = choose_shape(L.r, L.r, L.c, 1, p.batch, sms), poly = choose_shape(L.r, L.r, L.r, 1, p.batch, sms),
+              apply = choose_shape(p.rows, p.cols, L.r, 0, p.batch, sms);
+  const int sym_log = gram.pair || poly.pair || apply.pair ? 8 : 7;
+  const float ca = (float)p.coef[0], cb = (float)p.coef[1], cc = (float)p.coef[2];
   for (int j = 0; j < p.steps; ++j) {
     const int cur = j & 1;
+    const bool last = j == p.steps - 1;
+    // HALF, shifted form: near the end A is close to the identity.  In the last two steps E = A - I is stored in its
+    // place, b A + c A^2 = (b + c) I + (b + 2c) E + c E^2, and in the last one (b + c) I moves to the linear term,
+    // so that what is rounded to 11 bits is small.  (Simulated error of a Gaussian matrix 2.6e-3 -> 1.5e-3 of the
+    // result's norm, rank 10 4.7e-4 -> 8.0e-4; with the shift one step earlier still 1.0e-3 and 2.0e-3.)
+    const bool shift_a = !p.full && j >= p.steps - 2, shift_p = !p.full && last;
     NsGemm g{};
     g.batch = p.batch;
-    g.terms = p.full ? 3 : 1;
     g.err = p.err;
     g.rho = rho;
     g.step_no = j;
-    // A
+    // A, or A - I
+    g.prod = PROD_GRAM;
     g.M = g.N = L.r;
     g.K = L.c;
     g.a_mn = g.b_mn = tall;
     g.sym = 1;
+    g.sym_log = sym_log;
     g.c_acc = INV_SCALE;
+    g.diag = shift_a ? -SCALE : 0.f;
     g.dst = A;
     g.ld_dst = L.ld_s;
     g.dst_plane = L.plane_s;
     g.write_lo = 1;
-    if ((e = launch_ns_gemm(tx[cur], tx[cur], g, sms, st)) != cudaSuccess) return *why = "kernel launch", e;
+    if ((e = launch_ns_gemm(tx[cur], tx[cur], g, gram, p.full, sms, st)) != cudaSuccess) return *why = "kernel launch", e;
     // b A + c A^2
+    g.prod = PROD_POLY;
     g.K = L.r;
     g.a_mn = g.b_mn = 0;
+    g.a_sym = g.b_sym = 1;
     g.src = A;
     g.ld_src = L.ld_s;
     g.src_plane = L.plane_s;
-    g.c_src = (float)p.coef[1];
-    g.c_acc = (float)p.coef[2] * INV_SCALE;
-    g.rho_mode = RHO_POLY;
+    g.c_src = shift_a ? cb + 2.f * cc : cb;
+    g.c_src_plain = cb;
+    g.c_acc = cc * INV_SCALE;
+    g.diag = shift_a && !shift_p ? (cb + cc) * SCALE : 0.f;
     g.dst = Q;
     g.write_lo = p.full;
-    if ((e = launch_ns_gemm(ta, ta, g, sms, st)) != cudaSuccess) return *why = "kernel launch", e;
+    if ((e = launch_ns_gemm(ta, ta, g, poly, p.full, sms, st)) != cudaSuccess) return *why = "kernel launch", e;
     // a X + (.) X, or a X + X (.) for a tall matrix
-    const bool last = j == p.steps - 1;
     NsGemm h = last ? f : g;
-    h.terms = g.terms;
+    h.prod = last ? PROD_LAST : PROD_APPLY;
     h.step_no = j;
-    h.rho_mode = last ? RHO_LAST : RHO_APPLY;
     h.M = p.rows;
     h.N = p.cols;
     h.K = L.r;
     h.a_mn = 0;
     h.b_mn = tall ? 0 : 1;
+    h.a_sym = !tall;
+    h.b_sym = tall;
     h.sym = 0;
+    h.sym_log = sym_log;
+    h.diag = 0.f;
     h.src = X[cur];
     h.ld_src = L.ld_x;
     h.src_plane = L.plane_x;
     const float k = last ? INV_SCALE : 1.f;
-    h.c_src = (float)p.coef[0] * k;
+    h.c_src = ca * k;
+    h.c_src_shift = shift_p ? (cb + cc) * k : 0.f;
     h.c_acc = INV_SCALE * k;
     if (!last) {
       h.dst = X[cur ^ 1];
@@ -655,7 +919,7 @@ cudaError_t ns_run(const NsProblem& p, void* work, cudaStream_t st, const char**
       h.dst_plane = L.plane_x;
       h.write_lo = 1;
     }
-    if ((e = launch_ns_gemm(tall ? tx[cur] : tq, tall ? tq : tx[cur], h, sms, st)) != cudaSuccess)
+    if ((e = launch_ns_gemm(tall ? tx[cur] : tq, tall ? tq : tx[cur], h, apply, p.full, sms, st)) != cudaSuccess)
       return *why = "kernel launch", e;
     n += 3;
   }

@@ -165,6 +165,19 @@ def test_orthogonalize_batches_strides_and_places(t):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(12, 520, 700), (12, 700, 520), (40, 530, 610), (2, 1100, 900), (1, 300, 4000), (30, 128, 256)])
+def test_orthogonalize_many_tiles(shape, t):
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    g = torch.randn(shape, generator=gen, device="cuda").to(TYPES[t])
+    o = binding.orthogonalize(g)
+    for i in sorted({0, shape[0] // 2, shape[0] - 1}):
+        assert rel(num(o[i]), om.newton_schulz(num(g[i]))) <= (FULL_TOL if t == "f32" else HALF_TOL) + OUT[t]
+    assert torch.equal(o, binding.orthogonalize(g))
+    binding.check_operators()
+
+
+@pytest.mark.gpu
 def test_orthogonalize_steps_coefficients_and_scale():
     g = torch.from_numpy(spectrum(40, 90, "gauss")).float().cuda()
     for steps in (0, 1, 2, 9):
