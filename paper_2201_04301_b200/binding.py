@@ -335,72 +335,82 @@ def innovation_norms_noalloc(fresh, stale, lhs_out, stream=None):
 # ---------------------------------------------------------------------------
 PRECISIONS = {"full": 0, "half": 1}
 MUON_COEF = (3.4445, -4.7750, 2.0315)
-_status_words = {}
+_status_words = {}   # device index -> an int32 tensor that a kernel whose bounded wait gave up makes non-zero
 
 
 def _compute_type(t, what):
-    kind = {"torch.float32": COMPUTE_FP32, "torch.bfloat16": COMPUTE_BF16}.get(str(t.dtype))
-    if kind is None:
-        raise ValueError("%s must be float32 or bfloat16, not %s" % (what, t.dtype))
-    return kind
+    import torch
+    if t.dtype is torch.float32:
+        return COMPUTE_FP32
+    if t.dtype is torch.bfloat16:
+        return COMPUTE_BF16
+    raise ValueError("%s must be float32 or bfloat16, not %s" % (what, t.dtype))
 
 
 def _matrix(t, what, dims=(2,)):
     """Checks a row-major device matrix; its row stride."""
+    shape, stride = t.shape, t.stride()
     if not t.is_cuda:
         raise ValueError("%s must be a CUDA tensor" % what)
-    if t.dim() not in dims:
-        raise ValueError("%s must have %s dimensions, not %d" % (what, " or ".join(map(str, dims)), t.dim()))
-    if t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1:
+    if len(shape) not in dims:
+        raise ValueError("%s must have %s dimensions, not %d" % (what, " or ".join(map(str, dims)), len(shape)))
+    rows, cols = shape[-2:]
+    if cols > 1 and stride[-1] != 1:
         raise ValueError("%s: the last dimension must be contiguous" % what)
-    rows, cols = t.shape[-2:]
-    if rows > 1 and cols and t.stride(-2) < cols:
+    if rows <= 1:
+        return cols
+    if stride[-2] < cols:
         raise ValueError("%s: rows overlap" % what)
-    return int(t.stride(-2)) if rows > 1 else int(cols)
+    return stride[-2]
 
 
 class _Launch:
-    """The device, stream, status word and message buffer of one operator call."""
+    """Device, stream and message buffer of one operator call on `first`'s device."""
 
     def __init__(self, first, others, stream):
         import torch
-        self.torch, self.device = torch, first.device
+        self.torch, self.device, self.lib = torch, first.device, _lib or load()
         for t in others:
-            if t is not None and t.device != first.device:
-                raise ValueError("tensors on different devices: %s and %s" % (first.device, t.device))
-        self.lib = load()
-        self.guard = torch.cuda.device(first.device)
-        current = torch.cuda.current_stream(first.device)
-        self.raw = current.cuda_stream if stream is None else int(getattr(stream, "cuda_stream", stream))
-        # memory taken from torch's allocator belongs to the current stream; a call on another one says so
-        self.other = None if self.raw == current.cuda_stream else (
-            stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(self.raw, first.device))
-        self.buf = C.create_string_buffer(256)
-
-    def hold(self, *tensors):
-        if self.other is not None:
-            for t in tensors:
-                t.record_stream(self.other)
+            if t is not None and t.device != self.device:
+                raise ValueError("tensors on different devices: %s and %s" % (self.device, t.device))
+        self.index = self.device.index
+        current = torch._C._cuda_getCurrentRawStream(self.index)
+        self.raw, self.other = current, None
+        if stream is not None:
+            self.raw = int(getattr(stream, "cuda_stream", stream))
+            if self.raw != current:
+                # memory taken from torch's allocator belongs to the current stream; a call on another one says so
+                self.other = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(self.raw, self.device)
 
     def fresh(self, *shape, dtype):
-        t = self.torch.empty(*shape, dtype=dtype, device=self.device)
+        t = self.torch.empty(shape, dtype=dtype, device=self.device)
         if self.other is not None:  # the caching allocator may hand out memory that the current stream still uses
             self.other.wait_stream(self.torch.cuda.current_stream(self.device))
             t.record_stream(self.other)
         return t
 
     def status(self):
-        w = _status_words.get(self.device.index)
+        w = _status_words.get(self.index)
         if w is None:
             if self.torch.cuda.is_current_stream_capturing():
                 return None   # a word made now would belong to the graph being captured
-            w = _status_words[self.device.index] = self.torch.zeros(1, dtype=self.torch.int32, device=self.device)
+            w = _status_words[self.index] = self.torch.zeros(1, dtype=self.torch.int32, device=self.device)
             self.torch.cuda.current_stream(self.device).synchronize()
-        return _VP(w.data_ptr())
+        return w.data_ptr()
 
-    def check(self, st):
+    def call(self, fn, args, tensors):
+        buf = C.create_string_buffer(256)
+        if self.torch._C._cuda_getDevice() == self.index:
+            st = fn(*args, self.raw, buf, 256)
+        else:
+            with self.torch.cuda.device(self.index):
+                st = fn(*args, self.raw, buf, 256)
         if st != OK:
-            raise GCadaError(st, self.buf.value.decode())
+            raise GCadaError(st, buf.value.decode())
+        if self.other is not None:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(self.other)
 
 
 def check_operators(device=None):
@@ -415,26 +425,38 @@ def check_operators(device=None):
         raise GCadaError(ETIMEOUT, "a bounded device-side wait of a matrix operator gave up")
 
 
+_coef_arrays = {}
+
+
 def _steps(steps, coef, eps, precision, narrow):
     if precision is None:
         precision = "half" if narrow else "full"
     if precision not in PRECISIONS:
         raise ValueError("precision must be 'full' or 'half', not %r" % (precision,))
-    if len(coef) != 3:
-        raise ValueError("coef must hold three values")
-    return PRECISIONS[precision], int(steps), (C.c_double * 3)(*[float(v) for v in coef]), float(eps)
+    array = _coef_arrays.get(coef) if type(coef) is tuple else None
+    if array is None:
+        if len(coef) != 3:
+            raise ValueError("coef must hold three values")
+        array = (C.c_double * 3)(*[float(v) for v in coef])
+        if coef == MUON_COEF:
+            _coef_arrays[MUON_COEF] = array
+    return PRECISIONS[precision], int(steps), array, float(eps)
+
+
+def _work_bytes(lib, batch, rows, cols):
+    n = C.c_size_t()
+    st = lib.gcada_orthogonalize_work(batch, rows, cols, C.byref(n))
+    if st != OK:
+        raise GCadaError(st, "matrix sizes out of range")
+    return n.value
 
 
 def _ns_work(run, batch, rows, cols, work):
-    n = C.c_size_t()
-    st = run.lib.gcada_orthogonalize_work(batch, rows, cols, C.byref(n))
-    if st != OK:
-        raise GCadaError(st, "matrix sizes out of range")
     if work is None:
-        work = run.fresh(max(1, n.value), dtype=run.torch.uint8)
-    elif work.device != run.device or not work.is_contiguous():
-        raise ValueError("work must be a contiguous tensor on the same device")
-    return work, _VP(work.data_ptr()), work.numel() * work.element_size()
+        work = run.fresh(max(1, _work_bytes(run.lib, batch, rows, cols)), dtype=run.torch.uint8)
+    elif not work.is_contiguous():
+        raise ValueError("work must be contiguous")
+    return work, work.data_ptr(), work.numel() * work.element_size()
 
 
 def orthogonalize(g, out=None, steps=5, coef=MUON_COEF, eps=1e-7, precision=None, work=None, stream=None):
@@ -442,35 +464,28 @@ def orthogonalize(g, out=None, steps=5, coef=MUON_COEF, eps=1e-7, precision=None
     the same singular vectors whose singular values are near one.  See gcada_orthogonalize.  `precision`: "full" or
     "half", by default "full" for float32 and "half" for bfloat16.  `out` may be `g`.  `work`: a tensor of at least
     orthogonalize_work(g) bytes to use as the work area, by default taken from torch's allocator."""
-    kind = _compute_type(g, "g")
-    ld_g = _matrix(g, "g", (2, 3))
+    kind, ld_g = _compute_type(g, "g"), _matrix(g, "g", (2, 3))
     run = _Launch(g, (out, work), stream)
+    shape = g.shape
     if out is None:
-        out = run.fresh(g.shape, dtype=g.dtype)
-    if out.shape != g.shape or out.dtype != g.dtype:
+        out = run.fresh(*shape, dtype=g.dtype)
+    elif out.shape != shape or out.dtype != g.dtype:
         raise ValueError("out must have g's shape and type")
     ld_o = _matrix(out, "out", (2, 3))
-    rows, cols = g.shape[-2:]
-    batch = g.shape[0] if g.dim() == 3 else 1
-    stride_g, stride_o = (int(t.stride(0)) if t.dim() == 3 and batch > 1 else 0 for t in (g, out))
+    rows, cols = shape[-2:]
+    batch, stride_g, stride_o = (shape[0], g.stride(0), out.stride(0)) if len(shape) == 3 else (1, 0, 0)
     precision, steps, coef, eps = _steps(steps, coef, eps, precision, kind == COMPUTE_BF16)
-    with run.guard:
-        work, ptr, size = _ns_work(run, batch, rows, cols, work)
-        run.check(run.lib.gcada_orthogonalize(_VP(g.data_ptr()), _VP(out.data_ptr()), kind, batch, rows, cols, ld_g,
-                                              stride_g, ld_o, stride_o, precision, steps, coef, eps, ptr, size,
-                                              run.status(), _VP(run.raw), run.buf, 256))
-    run.hold(g, out)
+    work, ptr, size = _ns_work(run, batch, rows, cols, work)
+    run.call(run.lib.gcada_orthogonalize,
+             (g.data_ptr(), out.data_ptr(), kind, batch, rows, cols, ld_g, stride_g, ld_o, stride_o, precision, steps,
+              coef, eps, ptr, size, run.status()), (g, out, work))
     return out
 
 
 def orthogonalize_work(g):
     """Bytes of the work area that orthogonalize(g) or muon_update(w=g) needs."""
-    n = C.c_size_t()
     rows, cols = g.shape[-2:]
-    st = load().gcada_orthogonalize_work(g.shape[0] if g.dim() == 3 else 1, rows, cols, C.byref(n))
-    if st != OK:
-        raise GCadaError(st, "matrix sizes out of range")
-    return n.value
+    return _work_bytes(load(), g.shape[0] if g.dim() == 3 else 1, rows, cols)
 
 
 def muon_update(w, m, g, lr, beta=0.95, nesterov=True, weight_decay=0.0, scale=None, steps=5, coef=MUON_COEF,
@@ -479,23 +494,29 @@ def muon_update(w, m, g, lr, beta=0.95, nesterov=True, weight_decay=0.0, scale=N
     See gcada_muon_update.  `scale`: by default sqrt(max(1, rows / cols)).  `precision`: by default "full" for
     float32 weights and "half" for bfloat16 ones."""
     w_kind, g_kind = _compute_type(w, "w"), _compute_type(g, "g")
-    ld = [_matrix(t, n) for t, n in ((w, "w"), (m, "m"), (g, "g"))]
-    if str(m.dtype) != "torch.float32":
+    ld_w, ld_m, ld_g = _matrix(w, "w"), _matrix(m, "m"), _matrix(g, "g")
+    if _compute_type(m, "m") != COMPUTE_FP32:
         raise ValueError("m must be float32")
+    rows, cols = w.shape
     if m.shape != w.shape or g.shape != w.shape:
         raise ValueError("w, m and g must have the same shape")
     run = _Launch(w, (m, g, work), stream)
-    rows, cols = w.shape
     if scale is None:
         scale = max(1.0, rows / max(1, cols)) ** 0.5
     precision, steps, coef, eps = _steps(steps, coef, eps, precision, w_kind == COMPUTE_BF16)
-    with run.guard:
-        work, ptr, size = _ns_work(run, 1, rows, cols, work)
-        run.check(run.lib.gcada_muon_update(_VP(w.data_ptr()), w_kind, _VP(m.data_ptr()), _VP(g.data_ptr()), g_kind,
-                                            rows, cols, *ld, float(lr), float(beta), int(bool(nesterov)),
-                                            float(weight_decay), float(scale), precision, steps, coef, eps, ptr, size,
-                                            run.status(), _VP(run.raw), run.buf, 256))
-    run.hold(w, m, g)
+    work, ptr, size = _ns_work(run, 1, rows, cols, work)
+    run.call(run.lib.gcada_muon_update,
+             (w.data_ptr(), w_kind, m.data_ptr(), g.data_ptr(), g_kind, rows, cols, ld_w, ld_m, ld_g, float(lr),
+              float(beta), int(bool(nesterov)), float(weight_decay), float(scale), precision, steps, coef, eps, ptr,
+              size, run.status()), (w, m, g, work))
+
+
+def _mx_bytes(rows, cols):
+    n, s = C.c_size_t(), C.c_size_t()
+    st = (_lib or load()).gcada_mx_size(rows, cols, C.byref(n), C.byref(s))
+    if st != OK:
+        raise GCadaError(st, "matrix sizes out of range")
+    return n.value, s.value
 
 
 class MxMatrix:
@@ -504,11 +525,7 @@ class MxMatrix:
 
     def __init__(self, rows, cols, codes, scales):
         self.rows, self.cols, self.codes, self.scales = int(rows), int(cols), codes, scales
-        n, s = C.c_size_t(), C.c_size_t()
-        st = load().gcada_mx_size(self.rows, self.cols, C.byref(n), C.byref(s))
-        if st != OK:
-            raise GCadaError(st, "matrix sizes out of range")
-        for t, want, name in ((codes, n.value, "codes"), (scales, s.value, "scales")):
+        for t, want, name in zip((codes, scales), _mx_bytes(self.rows, self.cols), ("codes", "scales")):
             if not t.is_cuda or str(t.dtype) != "torch.uint8" or not t.is_contiguous() or t.numel() != want:
                 raise ValueError("%s of a %d x %d matrix must be a contiguous CUDA tensor of %d bytes"
                                  % (name, self.rows, self.cols, want))
@@ -520,14 +537,12 @@ class MxMatrix:
         run = _Launch(self.codes, (out,), stream)
         if out is None:
             out = run.fresh(self.rows, self.cols, dtype=dtype or run.torch.float32)
-        if tuple(out.shape) != (self.rows, self.cols) or (dtype is not None and out.dtype != dtype):
+        elif tuple(out.shape) != (self.rows, self.cols) or (dtype is not None and out.dtype != dtype):
             raise ValueError("out must be a %d x %d matrix of the type asked for" % (self.rows, self.cols))
         ld = _matrix(out, "out")
-        with run.guard:
-            run.check(run.lib.gcada_mx_dequantize(_VP(self.codes.data_ptr()), _VP(self.scales.data_ptr()), self.rows,
-                                                  self.cols, _VP(out.data_ptr()), _compute_type(out, "out"), ld,
-                                                  _VP(run.raw), run.buf, 256))
-        run.hold(self.codes, self.scales, out)
+        run.call(run.lib.gcada_mx_dequantize,
+                 (self.codes.data_ptr(), self.scales.data_ptr(), self.rows, self.cols, out.data_ptr(),
+                  _compute_type(out, "out"), ld), (self.codes, self.scales, out))
         return out
 
 
@@ -539,18 +554,15 @@ def mx_quantize(x, transpose=False, out=None, stream=None):
     shape = (cols, rows) if transpose else (rows, cols)
     run = _Launch(x, () if out is None else (out.codes,), stream)
     if out is None:
-        n, s = C.c_size_t(), C.c_size_t()
-        st = run.lib.gcada_mx_size(*shape, C.byref(n), C.byref(s))
-        if st != OK:
-            raise GCadaError(st, "matrix sizes out of range")
-        out = MxMatrix(*shape, run.fresh(n.value, dtype=run.torch.uint8), run.fresh(s.value, dtype=run.torch.uint8))
+        n, s = _mx_bytes(*shape)
+        out = MxMatrix.__new__(MxMatrix)
+        out.rows, out.cols = shape
+        out.codes, out.scales = run.fresh(n, dtype=run.torch.uint8), run.fresh(s, dtype=run.torch.uint8)
     elif (out.rows, out.cols) != shape:
         raise ValueError("out must be %d x %d" % shape)
-    with run.guard:
-        run.check(run.lib.gcada_mx_quantize(_VP(x.data_ptr()), kind, rows, cols, ld, int(bool(transpose)),
-                                            _VP(out.codes.data_ptr()), _VP(out.scales.data_ptr()), _VP(run.raw),
-                                            run.buf, 256))
-    run.hold(x, out.codes, out.scales)
+    run.call(run.lib.gcada_mx_quantize,
+             (x.data_ptr(), kind, rows, cols, ld, 1 if transpose else 0, out.codes.data_ptr(), out.scales.data_ptr()),
+             (x, out.codes, out.scales))
     return out
 
 
@@ -564,18 +576,16 @@ def mx_gemm(a, b, out=None, dtype=None, alpha=1.0, beta=0.0, bias=None, stream=N
         if beta != 0:
             raise ValueError("beta needs out")
         out = run.fresh(a.rows, b.rows, dtype=dtype or run.torch.float32)
-    if tuple(out.shape) != (a.rows, b.rows) or (dtype is not None and out.dtype != dtype):
+    elif tuple(out.shape) != (a.rows, b.rows) or (dtype is not None and out.dtype != dtype):
         raise ValueError("out must be a %d x %d matrix of the type asked for" % (a.rows, b.rows))
     if bias is not None and (str(bias.dtype) != "torch.float32" or bias.numel() != b.rows or not bias.is_contiguous()):
         raise ValueError("bias must hold %d contiguous float32 values" % b.rows)
     ld = _matrix(out, "out")
-    with run.guard:
-        run.check(run.lib.gcada_mx_gemm(_VP(a.codes.data_ptr()), _VP(a.scales.data_ptr()), a.rows,
-                                        _VP(b.codes.data_ptr()), _VP(b.scales.data_ptr()), b.rows, a.cols,
-                                        _VP(out.data_ptr()), _compute_type(out, "out"), ld, float(alpha), float(beta),
-                                        _VP(bias.data_ptr()) if bias is not None else None, run.status(),
-                                        _VP(run.raw), run.buf, 256))
-    run.hold(a.codes, a.scales, b.codes, b.scales, out, *(() if bias is None else (bias,)))
+    run.call(run.lib.gcada_mx_gemm,
+             (a.codes.data_ptr(), a.scales.data_ptr(), a.rows, b.codes.data_ptr(), b.scales.data_ptr(), b.rows, a.cols,
+              out.data_ptr(), _compute_type(out, "out"), ld, float(alpha), float(beta),
+              None if bias is None else bias.data_ptr(), run.status()),
+             (a.codes, a.scales, b.codes, b.scales, out, bias))
     return out
 
 

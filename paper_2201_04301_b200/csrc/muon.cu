@@ -495,11 +495,11 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
       const int b = first / per;
       int mt, nt;
       tile_of(first - b * per, tiles_n, a.sym, g_tiles, mt, nt);
-      // this CTA's columns, 16 at a time, dealt to the two warps of a quadrant
-      const int m = mt * TILE + quad * 32 + lane, mine = TILE / csize;
+      // columns are dealt out 16 at a time: to the CTAs, then to the two warps of a quadrant
+      const int m = mt * TILE + quad * 32 + lane;
       if (m < a.M) {
         const RowCtx r = row_ctx(a, b, m);
-        for (int c = rank * mine + half * 16; c < (rank + 1) * mine; c += 32) {
+        for (int c = 16 * (rank + half * csize); c < TILE; c += 32 * csize) {
           const int n = nt * TILE + c;
           if (!wanted(a, m, n)) continue;
           Src16 s;
@@ -530,17 +530,6 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
 }
 
 // ----------------------------------------------------------------- source: a matrix, or the momentum's look-ahead
-struct NsSource {
-  const void* g;  // float or bf16, row stride ld, matrix stride
-  long long ld, stride;
-  int bf16;
-  float* m;       // momentum (row stride ld_m), or null: the matrix itself
-  long long ld_m, m_stride;
-  float beta, omb;
-  int nesterov;
-  int rows, cols;
-};
-
 template <typename T>
 __device__ __forceinline__ void load8(const T* p, int n, float (&f)[8]) {
   if (n == 8 && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
@@ -726,6 +715,7 @@ cudaError_t set_attributes() {
   if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<true, false>, at, SMEM_BYTES);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<false, true>, at, SMEM_BYTES);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<false, false>, at, SMEM_BYTES);
+  if (e == cudaSuccess) e = ns_cluster_set_attributes();
   return e;
 }
 
@@ -751,23 +741,24 @@ cudaError_t launch_shape(const CUtensorMap& ta, const CUtensorMap& tb, const NsG
 // fewer K blocks in sequence; `ramp` is what filling and draining a tile costs, in K blocks.
 struct Shape {
   bool pair;
-  int split, ctas;
+  int split;
 };
-Shape choose_shape(int M, int N, int K, int sym, int batch, int sms) {
+Shape choose_shape(int M, int N, int K, int sym, int g, int batch, int full, int sms) {
   const int kb = (K + BK - 1) / BK;
-  auto tiles = [&](int t, int g) { return (long long)tile_count((M + t - 1) / t, (N + t - 1) / t, sym, g) * batch; };
-  const long long pairs = tiles(256, 0), singles = tiles(128, 0);
-  const int ramp_pair = 10, ramp_single = 6;
-  Shape s{false, 1, 0};
-  long long cost = (singles + sms - 1) / sms * kb + ramp_single;
-  for (int k = 2; k <= 8 && singles * k <= sms && kb >= 2 * k; k *= 2) {
-    const long long c = (kb + k - 1) / k + ramp_single + 2;
+  auto tiles = [&](int t, int gt) { return (long long)tile_count((M + t - 1) / t, (N + t - 1) / t, sym, gt) * batch; };
+  const long long pairs = tiles(256, 0), singles = tiles(128, g);
+  // FULL: 64 KiB and three products a block; a pair's products (1536 cycles) then outlast its copies (1024)
+  const int kb_pair = full ? 3 : 1, kb_single = full ? 2 : 1, ramp_pair = 10, ramp_single = 6;
+  Shape s{false, 1};
+  long long cost = (singles + sms - 1) / sms * kb * kb_single + ramp_single;
+  for (int k = 2; k <= 8 && singles * k <= sms && kb >= 2 * k; ++k) {
+    const long long c = (kb + k - 1) / k * kb_single + ramp_single + 2;
     if (c < cost) {
       cost = c;
       s.split = k;
     }
   }
-  if ((pairs + sms / 2 - 1) / (sms / 2) * kb + ramp_pair < cost) s.pair = true;
+  if ((pairs + sms / 2 - 1) / (sms / 2) * kb * kb_pair + ramp_pair < cost) s = Shape{true, 1};
   return s;
 }
 
@@ -776,8 +767,7 @@ cudaError_t launch_ns_gemm(const CUtensorMap& ta, const CUtensorMap& tb, NsGemm 
   const int t = s.pair ? 256 : 128;
   const long long tiles =
       (long long)tile_count((a.M + t - 1) / t, (a.N + t - 1) / t, a.sym, s.pair ? 0 : a.sym_log - 7) * a.batch;
-  // (a symmetric result kept in blocks of 256 has a few tiles of 128 more than the choice counted: no split then)
-  a.split = tiles * s.split <= sms ? s.split : 1;
+  a.split = s.split;
   const long long room = s.pair ? sms / 2 : sms, want = tiles * (s.pair ? 1 : a.split);
   const int ctas = (int)(want < room ? want : room) * (s.pair ? 2 : 1);
   if (s.pair) return full ? launch_shape<true, true>(ta, tb, a, ctas, st) : launch_shape<true, false>(ta, tb, a, ctas, st);
@@ -786,7 +776,9 @@ cudaError_t launch_ns_gemm(const CUtensorMap& ta, const CUtensorMap& tb, NsGemm 
 
 }  // namespace
 
-size_t ns_work_bytes(int batch, int rows, int cols) { return layout(batch, rows, cols).bytes; }
+size_t ns_work_bytes(int batch, int rows, int cols) {
+  return ns_cluster_size(rows, cols, nullptr) ? 256 : layout(batch, rows, cols).bytes;
+}
 
 // Everything an orthogonalisation enqueues.  `why` names the step that failed.
 cudaError_t ns_run(const NsProblem& p, void* work, cudaStream_t st, const char** why, int* launches) {
@@ -795,6 +787,25 @@ cudaError_t ns_run(const NsProblem& p, void* work, cudaStream_t st, const char**
   int sms = 0;
   cudaError_t e = device_ready(known, set_attributes, &sms, why);
   if (e != cudaSuccess) return e;
+  NsSource s{};
+  s.g = p.g;
+  s.ld = p.ld_g;
+  s.stride = p.stride_g;
+  s.bf16 = p.g_bf16;
+  s.m = p.m;
+  s.ld_m = p.ld_m;
+  s.beta = (float)p.beta;
+  s.omb = (float)(1.0 - p.beta);
+  s.nesterov = p.nesterov;
+  s.rows = p.rows;
+  s.cols = p.cols;
+  const NsSink sink{p.o, p.ld_o, p.stride_o, p.o_bf16, p.w_update, (float)p.decay, (float)p.step};
+  if (ns_cluster_size(p.rows, p.cols, nullptr)) {
+    const float coef[3] = {(float)p.coef[0], (float)p.coef[1], (float)p.coef[2]};
+    if ((e = launch_ns_cluster(s, sink, p.batch, coef, p.steps, p.eps, st)) != cudaSuccess) *why = "kernel launch";
+    if (launches) *launches = 1;
+    return e;
+  }
   const NsLayout L = layout(p.batch, p.rows, p.cols);
   char* base = static_cast<char*>(work);
   double* part = reinterpret_cast<double*>(base + L.part);
@@ -808,18 +819,6 @@ cudaError_t ns_run(const NsProblem& p, void* work, cudaStream_t st, const char**
   for (int i = 0; i < 2 && ok; ++i) ok = make_map_f16(&tx[i], X[i], p.cols, p.rows, 2LL * p.batch, L.ld_x, L.plane_x);
   if (!ok) return *why = "tensor map creation failed for this shape", cudaErrorInvalidValue;
 
-  NsSource s{};
-  s.g = p.g;
-  s.ld = p.ld_g;
-  s.stride = p.stride_g;
-  s.bf16 = p.g_bf16;
-  s.m = p.m;
-  s.ld_m = p.ld_m;
-  s.beta = (float)p.beta;
-  s.omb = (float)(1.0 - p.beta);
-  s.nesterov = p.nesterov;
-  s.rows = p.rows;
-  s.cols = p.cols;
   const long long chunks = (long long)((p.cols + 7) / 8) * p.rows;
   const long long want = (chunks + 255) / 256;
   const int nb = (int)(want < NORM_BLOCKS ? want : NORM_BLOCKS);
@@ -836,19 +835,26 @@ cudaError_t ns_run(const NsProblem& p, void* work, cudaStream_t st, const char**
   f.batch = p.batch;
   f.M = p.rows;
   f.N = p.cols;
-  f.out = p.w_update ? (p.o_bf16 ? OUT_UPDATE_BF16 : OUT_UPDATE_F32) : (p.o_bf16 ? OUT_BF16 : OUT_F32);
-  f.user = p.o;
-  f.ld_user = p.ld_o;
-  f.user_stride = p.stride_o;
-  f.decay = (float)p.decay;
-  f.step = (float)p.step;
+  f.out = sink.update ? (sink.bf16 ? OUT_UPDATE_BF16 : OUT_UPDATE_F32) : (sink.bf16 ? OUT_BF16 : OUT_F32);
+  f.user = sink.o;
+  f.ld_user = sink.ld;
+  f.user_stride = sink.stride;
+  f.decay = sink.decay;
+  f.step = sink.step;
   f.ld_src = L.ld_x;
   f.src_plane = L.plane_x;
   f.err = p.err;
   f.rho = rho;
-  const Shape gram = choose_shape(L.r, L.r, L.c, 1, p.batch, sms), poly = choose_shape(L.r, L.r, L.r, 1, p.batch, sms),
-              apply = choose_shape(p.rows, p.cols, L.r, 0, p.batch, sms);
-  const int sym_log = gram.pair || poly.pair || apply.pair ? 8 : 7;
+  Shape gram, poly, apply;
+  int sym_log = 7;
+  for (;;) {  // a pair of CTAs anywhere asks for symmetric blocks of 256 everywhere, which changes the other counts
+    const int g = sym_log - 7;
+    gram = choose_shape(L.r, L.r, L.c, 1, g, p.batch, p.full, sms);
+    poly = choose_shape(L.r, L.r, L.r, 1, g, p.batch, p.full, sms);
+    apply = choose_shape(p.rows, p.cols, L.r, 0, g, p.batch, p.full, sms);
+    if (sym_log == 8 || !(gram.pair || poly.pair || apply.pair)) break;
+    sym_log = 8;
+  }
   const float ca = (float)p.coef[0], cb = (float)p.coef[1], cc = (float)p.coef[2];
   for (int j = 0; j < p.steps; ++j) {
     const int cur = j & 1;

@@ -25,6 +25,31 @@ struct NsProblem {
   int full;             // 1: products of hi / lo pairs (fp32 accuracy), 0: of the hi parts
   int* err = nullptr;   // device error word, or null
 };
+// The matrix that is orthogonalised: g itself, or with m the momentum or its look-ahead.
+struct NsSource {
+  const void* g;  // float or bf16, row stride ld, matrix stride
+  long long ld, stride;
+  int bf16;
+  float* m;       // momentum (row stride ld_m), or null
+  long long ld_m, m_stride;
+  float beta, omb;
+  int nesterov;
+  int rows, cols;
+};
+// Where the result goes: o <- x, or o <- decay * o - step * x.
+struct NsSink {
+  void* o;        // float or bf16, row stride ld, matrix stride
+  long long ld, stride;
+  int bf16, update;
+  float decay, step;
+};
+
+// Narrow matrices, whole iterations on chip (muon_cluster.cu).  cluster_size: CTAs per matrix, 0 = not this way.
+int ns_cluster_size(int rows, int cols, size_t* smem_bytes);
+cudaError_t ns_cluster_set_attributes();
+cudaError_t launch_ns_cluster(const NsSource& s, const NsSink& o, int batch, const float coef[3], int steps, double eps,
+                              cudaStream_t st);
+
 size_t ns_work_bytes(int batch, int rows, int cols);
 cudaError_t ns_run(const NsProblem& p, void* work, cudaStream_t st, const char** why, int* launches);
 
