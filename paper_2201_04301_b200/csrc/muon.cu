@@ -751,7 +751,7 @@ Shape choose_shape(int M, int N, int K, int sym, int g, int batch, int full, int
   const int kb_pair = full ? 3 : 1, kb_single = full ? 2 : 1, ramp_pair = 10, ramp_single = 6;
   Shape s{false, 1};
   long long cost = (singles + sms - 1) / sms * kb * kb_single + ramp_single;
-  for (int k = 2; k <= 8 && singles * k <= sms && kb >= 2 * k; ++k) {
+  for (int k = 2; k <= 8 && singles <= max_clusters(k, sms) && kb >= 2 * k; ++k) {
     const long long c = (kb + k - 1) / k * kb_single + ramp_single + 2;
     if (c < cost) {
       cost = c;
@@ -777,7 +777,7 @@ cudaError_t launch_ns_gemm(const CUtensorMap& ta, const CUtensorMap& tb, NsGemm 
 }  // namespace
 
 size_t ns_work_bytes(int batch, int rows, int cols) {
-  return ns_cluster_size(rows, cols, nullptr) ? 256 : layout(batch, rows, cols).bytes;
+  return ns_fits_cluster(rows, cols) ? 256 : layout(batch, rows, cols).bytes;
 }
 
 // Everything an orthogonalisation enqueues.  `why` names the step that failed.
@@ -800,7 +800,7 @@ cudaError_t ns_run(const NsProblem& p, void* work, cudaStream_t st, const char**
   s.rows = p.rows;
   s.cols = p.cols;
   const NsSink sink{p.o, p.ld_o, p.stride_o, p.o_bf16, p.w_update, (float)p.decay, (float)p.step};
-  if (ns_cluster_size(p.rows, p.cols, nullptr)) {
+  if (ns_fits_cluster(p.rows, p.cols)) {
     const float coef[3] = {(float)p.coef[0], (float)p.coef[1], (float)p.coef[2]};
     if ((e = launch_ns_cluster(s, sink, p.batch, coef, p.steps, p.eps, st)) != cudaSuccess) *why = "kernel launch";
     if (launches) *launches = 1;

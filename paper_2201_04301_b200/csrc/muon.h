@@ -44,8 +44,8 @@ struct NsSink {
   float decay, step;
 };
 
-// Narrow matrices, whole iterations on chip (muon_cluster.cu).  cluster_size: CTAs per matrix, 0 = not this way.
-int ns_cluster_size(int rows, int cols, size_t* smem_bytes);
+// Narrow matrices, all steps on chip (muon_cluster.cu).
+bool ns_fits_cluster(int rows, int cols);
 cudaError_t ns_cluster_set_attributes();
 cudaError_t launch_ns_cluster(const NsSource& s, const NsSink& o, int batch, const float coef[3], int steps, double eps,
                               cudaStream_t st);

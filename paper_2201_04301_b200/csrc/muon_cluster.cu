@@ -1,11 +1,11 @@
 // Newton-Schulz steps of a narrow matrix (short side up to 64) in one launch: the long side is dealt out to the CTAs
 // of a thread-block cluster, which keep their slices of X in shared memory for all steps, in fp32 throughout.
 //
-// A step: every CTA forms its slice's share of A = X X^T, one cluster barrier, every CTA adds up all shares (read
-// through distributed shared memory, in rank order: bitwise reproducible), forms b A + c A^2 for itself and applies
-// it to its slice.  Shares are double-buffered, so one barrier a step is enough.  Bound: latency - each phase is
-// some hundred cycles of FMAs between barriers.  As separate tensor-core launches the same steps cost 4 to 5 us per
-// product however small it is (10 x 200: 76 us, 64 x 512: 98 us).
+// A step: every CTA forms its slice's share of A = X X^T; cluster barrier; every CTA adds up its part of A from all
+// shares (through distributed shared memory, in rank order: bitwise reproducible) and hands it to all; cluster
+// barrier; every CTA forms b A + c A^2 for itself and applies it to its slice.  Bound: latency - each phase is some
+// hundred to some thousand cycles of FMAs between barriers.  As separate tensor-core launches the same steps cost
+// 4 to 5 us per product however small it is.
 #include <cuda_bf16.h>
 
 #include "common.cuh"
@@ -17,6 +17,7 @@ namespace {
 
 constexpr int NC_THREADS = 512;
 constexpr int NC_MAX_R = 64;
+static_assert(NC_MAX_R <= 64, "the tiles of A fit the smallest block that they are given");
 constexpr int NC_MAX_SMEM = 220 * 1024;
 
 struct NcArgs {
@@ -27,53 +28,66 @@ struct NcArgs {
   double eps;
 };
 
-__device__ __forceinline__ float cluster_load_f32(uint32_t base, uint32_t rank, int index) {
-  return cluster_load(cluster_map(base, rank) + 4u * (uint32_t)index);
+// A thread's place in a symmetric product: a 4 x 4 tile on or above the diagonal, whose sum 2^lk neighbouring lanes
+// share (all of a warp's lanes take part in every exchange).
+struct SymPlace {
+  int ti, tj, part, lk;
+  bool on;
+};
+__device__ SymPlace sym_place(int nt, int K) {
+  const int tiles = nt * (nt + 1) / 2;
+  SymPlace p;
+  p.lk = 0;
+  while (p.lk < 5 && (tiles << (p.lk + 1)) <= (int)blockDim.x && (4 << p.lk) <= K) ++p.lk;
+  const int tile = (int)threadIdx.x >> p.lk;
+  p.part = (int)threadIdx.x & ((1 << p.lk) - 1);
+  p.on = tile < tiles;
+  p.ti = 0;
+  int u = p.on ? tile : 0;
+  while (u >= nt - p.ti) u -= nt - p.ti++;
+  p.tj = p.ti + u;
+  return p;
 }
 
-// out[i][j] (symmetric, n x n in rows of rp) = sum over k < K of M[k][i] M[k][j] (M in rows of rp) times s_acc, plus
-// s_src * add[i][j].  4 x 4 values a thread; `kp` neighbouring lanes share the sum over k.
-__device__ void symmetric_product(const float* M, int K, int rp, float* out, const float* add, float s_src, float s_acc) {
-  const int nt = rp >> 2, tiles = nt * (nt + 1) / 2;
-  int kp = 1;
-  while (kp < 32 && tiles * kp * 2 <= NC_THREADS && kp * 4 <= K) kp *= 2;
-  for (int base = 0; base < tiles * kp; base += NC_THREADS) {
-    const int id = base + (int)threadIdx.x, tile = id / kp, part = id % kp;
-    const bool on = tile < tiles;
-    int ti = 0, tj = 0;
-    if (on) {
-      int u = tile;
-      while (u >= nt - ti) u -= nt - ti, ++ti;
-      tj = ti + u;
-    }
-    float acc[4][4] = {};
-    if (on) {
+// out[i][j] (symmetric, in rows of rp) = s_acc * sum over k < K of M[k][i] M[k][j] + s_src * add[i][j].
+__device__ __forceinline__ void symmetric_product(const SymPlace& p, const float* M, int K, int rp, float* out, const float* add,
+                                                  float s_src, float s_acc) {
+  float acc[4][4] = {};
+  if (p.on) {
+    const float* mi = M + 4 * p.ti;
+    const float* mj = M + 4 * p.tj;
 #pragma unroll 4
-      for (int k = part; k < K; k += kp) {
-        const float4 x = *reinterpret_cast<const float4*>(M + k * rp + 4 * ti), y = *reinterpret_cast<const float4*>(M + k * rp + 4 * tj);
-        const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+    for (int k = p.part; k < K; k += 1 << p.lk) {
+      const float4 x = *reinterpret_cast<const float4*>(mi + k * rp), y = *reinterpret_cast<const float4*>(mj + k * rp);
+      const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) acc[i][j] += xs[i] * ys[j];
+        for (int j = 0; j < 4; ++j) acc[i][j] += xs[i] * ys[j];
+    }
+  }
+  for (int o = 1; o < 1 << p.lk; o *= 2) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j] += __shfl_xor_sync(0xffffffffu, acc[i][j], o);
+  }
+  if (p.on && p.part == 0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int at = (4 * p.ti + i) * rp + 4 * p.tj;
+      float4 v = make_float4(s_acc * acc[i][0], s_acc * acc[i][1], s_acc * acc[i][2], s_acc * acc[i][3]);
+      if (add) {
+        const float4 w = *reinterpret_cast<const float4*>(add + at);
+        v = make_float4(v.x + s_src * w.x, v.y + s_src * w.y, v.z + s_src * w.z, v.w + s_src * w.w);
       }
+      *reinterpret_cast<float4*>(out + at) = v;
+      acc[i][0] = v.x; acc[i][1] = v.y; acc[i][2] = v.z; acc[i][3] = v.w;
     }
-    for (int o = 1; o < kp; o *= 2) {
+    if (p.ti != p.tj) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] += __shfl_xor_sync(0xffffffffu, acc[i][j], o);
-    }
-    if (on && part == 0) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int p = (4 * ti + i) * rp + 4 * tj + j;
-          const float v = s_acc * acc[i][j] + (add ? s_src * add[p] : 0.f);
-          out[p] = v;
-          out[(4 * tj + j) * rp + 4 * ti + i] = v;
-        }
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<float4*>(out + (4 * p.tj + j) * rp + 4 * p.ti) = make_float4(acc[0][j], acc[1][j], acc[2][j], acc[3][j]);
     }
   }
 }
@@ -85,19 +99,19 @@ __global__ void __launch_bounds__(NC_THREADS, 1) ns_cluster_kernel(const NsSourc
   const int rp = n.rp, sq = rp * rp;
   float* X = sm;                       // [csp][rp]: X transposed, element (i, k) at k * rp + i
   float* Y = X + (size_t)n.csp * rp;   // the next iterate
-  float* part[2] = {Y + (size_t)n.csp * rp, Y + (size_t)n.csp * rp + sq};  // this CTA's share of A
-  float* A = part[1] + sq;
+  float* A = Y + (size_t)n.csp * rp;
   float* Q = A + sq;
+  float* part = Q + sq;                // clusters: this CTA's share of A
   const int b = blockIdx.x / n.csize, rank = n.csize > 1 ? (int)cluster_rank() : 0;
   const int k0 = rank * n.cs, kn = max(0, min(n.cs, n.c - k0));
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, threads = blockDim.x;
 
   // the slice, momentum moved on the way; squares in doubles
-  for (int e = tid; e < n.csp * rp; e += NC_THREADS) X[e] = 0.f;
+  for (int e = tid; e < n.csp * rp; e += threads) X[e] = 0.f;
   __syncthreads();
   const int count = kn * n.r;
   double ss = 0.0;
-  for (int e = tid; e < count; e += NC_THREADS) {
+  for (int e = tid; e < count; e += threads) {
     const int major = n.tall ? n.r : kn, q = e / major, w = e - q * major;
     const int i = n.tall ? w : q, k = n.tall ? q : w;
     const long long row = n.tall ? k0 + k : i, col = n.tall ? i : k0 + k;
@@ -129,36 +143,47 @@ __global__ void __launch_bounds__(NC_THREADS, 1) ns_cluster_kernel(const NsSourc
     ss = scratch[0];
   }
   const double norm = sqrt(ss) + n.eps;
-  for (int e = tid; e < n.csp * rp; e += NC_THREADS) X[e] = (float)((double)X[e] / norm);
+  for (int e = tid; e < n.csp * rp; e += threads) X[e] = (float)((double)X[e] / norm);
   __syncthreads();
 
   const int nt = rp >> 2, kgroups = (kn + 3) >> 2, items = kgroups * nt;
-  int kp = 1;  // lanes that share an item's sum over j
-  while (kp < 16 && items * kp * 2 <= NC_THREADS && kp * 2 <= nt) kp *= 2;
+  int lk = 0;  // 2^lk lanes share an item's sum over j
+  while (lk < 4 && (items << (lk + 1)) <= threads && (2 << lk) <= nt) ++lk;
+  const SymPlace gram = sym_place(nt, kn), poly = sym_place(nt, n.r);
+  const int e0 = (sq >> 2) * rank / n.csize, e1 = (sq >> 2) * (rank + 1) / n.csize;
   for (int step = 0; step < n.steps; ++step) {
-    float* mine = n.csize > 1 ? part[step & 1] : A;
-    symmetric_product(X, kn, rp, mine, nullptr, 0.f, 1.f);
+    symmetric_product(gram, X, kn, rp, n.csize > 1 ? part : A, nullptr, 0.f, 1.f);
     if (n.csize > 1) {
+      // each CTA adds up its part of the matrix and hands it to all
       cluster_sync();
-      const uint32_t from = smem_u32(mine);
-      for (int e = tid; e < sq; e += NC_THREADS) {
-        float v = 0.f;
-        for (int p = 0; p < n.csize; ++p) v += cluster_load_f32(from, (uint32_t)p, e);
-        A[e] = v;
+      for (int e = e0 + tid; e < e1; e += threads) {
+        float4 v[8];
+#pragma unroll
+        for (int p = 0; p < 8; ++p)
+          if (p < n.csize) v[p] = cluster_load4(cluster_map(smem_u32(part + 4 * e), (uint32_t)p));
+        float4 t = v[0];
+#pragma unroll
+        for (int p = 1; p < 8; ++p)
+          if (p < n.csize) t = make_float4(t.x + v[p].x, t.y + v[p].y, t.z + v[p].z, t.w + v[p].w);
+#pragma unroll
+        for (int p = 0; p < 8; ++p)
+          if (p < n.csize) cluster_store4(cluster_map(smem_u32(A + 4 * e), (uint32_t)p), t);
       }
+      cluster_sync();
+    } else {
+      __syncthreads();
     }
-    __syncthreads();
-    symmetric_product(A, n.r, rp, Q, A, n.b, n.cc);
+    symmetric_product(poly, A, n.r, rp, Q, A, n.b, n.cc);
     __syncthreads();
     // Y = a X + X Q: 4 columns of the slice x 4 rows a thread
-    for (int base = 0; base < items * kp; base += NC_THREADS) {
-      const int id = base + tid, item = id / kp, p = id % kp;
+    for (int base = 0; base < items << lk; base += threads) {
+      const int id = base + tid, item = id >> lk, p = id & ((1 << lk) - 1);
       const bool on = item < items;
       const int kg = on ? item / nt : 0, ti = on ? item - kg * nt : 0;
       const float* x = X + (size_t)kg * 4 * rp;
       float acc[4][4] = {};
       if (on) {
-        for (int j = 4 * p; j < rp; j += 4 * kp) {
+        for (int j = 4 * p; j < rp; j += 4 << lk) {
           float4 xv[4], qv[4];
 #pragma unroll
           for (int t = 0; t < 4; ++t) {
@@ -178,7 +203,7 @@ __global__ void __launch_bounds__(NC_THREADS, 1) ns_cluster_kernel(const NsSourc
           }
         }
       }
-      for (int w = 1; w < kp; w *= 2) {
+      for (int w = 1; w < 1 << lk; w *= 2) {
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -199,7 +224,7 @@ __global__ void __launch_bounds__(NC_THREADS, 1) ns_cluster_kernel(const NsSourc
     Y = t;
   }
 
-  for (int e = tid; e < count; e += NC_THREADS) {
+  for (int e = tid; e < count; e += threads) {
     const int major = n.tall ? n.r : kn, q = e / major, w = e - q * major;
     const int i = n.tall ? w : q, k = n.tall ? q : w;
     const long long row = n.tall ? k0 + k : i, col = n.tall ? i : k0 + k;
@@ -216,8 +241,10 @@ __global__ void __launch_bounds__(NC_THREADS, 1) ns_cluster_kernel(const NsSourc
   if (n.csize > 1) cluster_sync();  // the others have read this CTA's last share
 }
 
-// CTAs for a matrix: enough for its slices to fit, and more while a CTA's products outweigh a wider barrier.
-NcArgs plan(int rows, int cols, size_t* bytes) {
+// CTAs for a matrix.  One is fastest only while a barrier costs more than the work (16 x 16: 13 us with one, 15 with
+// eight; 16 x 64: equal); from there on eight (10 x 200: 20 and 18 us, 64 x 200: 116 and 43), but no more than let
+// all matrices of a batch run at once, and enough for the slices to fit.
+NcArgs plan(int batch, int rows, int cols, size_t* bytes) {
   NcArgs n{};
   n.tall = rows > cols;
   n.r = n.tall ? cols : rows;
@@ -225,25 +252,25 @@ NcArgs plan(int rows, int cols, size_t* bytes) {
   if (n.r > NC_MAX_R) return n;
   const int q = (n.r + 3) / 4;
   n.rp = 4 * (q | 1);
-  for (int cs = 1; cs <= 8; cs *= 2) {
+  int want = (long long)n.rp * n.c <= 1200 ? 1 : 8;
+  while (want > 1 && batch * want > 128) want /= 2;
+  for (int cs = want; cs <= 8; cs *= 2) {
     n.cs = (n.c + cs - 1) / cs;
     n.csp = (n.cs + 3) / 4 * 4;
-    *bytes = sizeof(float) * ((size_t)2 * n.csp * n.rp + (size_t)4 * n.rp * n.rp);
-    n.csize = 0;
-    if (*bytes > NC_MAX_SMEM) continue;
+    const double size = sizeof(float) * ((double)2 * n.csp * n.rp + (double)(cs > 1 ? 3 : 2) * n.rp * n.rp);
+    if (size > NC_MAX_SMEM) continue;
+    *bytes = (size_t)size;
     n.csize = cs;
-    if ((long long)n.rp * n.rp * n.cs <= 64 * 1024) break;
+    break;
   }
   return n;
 }
 
 }  // namespace
 
-int ns_cluster_size(int rows, int cols, size_t* smem_bytes) {
+bool ns_fits_cluster(int rows, int cols) {
   size_t bytes = 0;
-  const NcArgs n = plan(rows, cols, &bytes);
-  if (smem_bytes) *smem_bytes = bytes;
-  return n.csize;
+  return plan(1, rows, cols, &bytes).csize != 0;
 }
 
 cudaError_t ns_cluster_set_attributes() {
@@ -253,7 +280,7 @@ cudaError_t ns_cluster_set_attributes() {
 cudaError_t launch_ns_cluster(const NsSource& s, const NsSink& o, int batch, const float coef[3], int steps, double eps,
                               cudaStream_t st) {
   size_t bytes = 0;
-  NcArgs n = plan(s.rows, s.cols, &bytes);
+  NcArgs n = plan(batch, s.rows, s.cols, &bytes);
   n.steps = steps;
   n.a = coef[0];
   n.b = coef[1];
@@ -261,7 +288,10 @@ cudaError_t launch_ns_cluster(const NsSource& s, const NsSink& o, int batch, con
   n.eps = eps;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(batch * n.csize));
-  cfg.blockDim = dim3(NC_THREADS);
+  // a thread at least for every 4 x 4 tile of A (153 at most: a symmetric product is one pass), and as many as the
+  // slice's own tiles keep busy
+  const int nt = n.rp >> 2, tiles = nt * (nt + 1) / 2, items = (n.csp >> 2) * nt, want = tiles > items ? tiles : items;
+  cfg.blockDim = dim3((unsigned)(want <= 64 ? 128 : want <= 192 ? 256 : NC_THREADS));
   cfg.dynamicSmemBytes = bytes;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];

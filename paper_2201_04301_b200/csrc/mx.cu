@@ -101,7 +101,7 @@ __global__ void __launch_bounds__(256) mx_quantize_t_kernel(const T* __restrict_
   __shared__ __align__(16) uint4 codes_sm[64][9];  // [row][block], padded
   __shared__ uint32_t scale_sm[64][2];
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  const long long ct = blockIdx.x, r0 = (long long)blockIdx.y * 64, k0 = ct * 256 + w * 32, r = r0 + 2 * lane;
+  const long long strips = (q.rows + 127) / 128 * 2, ct = blockIdx.x / strips, r0 = (blockIdx.x - ct * strips) * 64, k0 = ct * 256 + w * 32, r = r0 + 2 * lane;
   float v[2][32];
   const bool pair = (reinterpret_cast<uintptr_t>(x) & (2 * sizeof(T) - 1)) == 0 && (ld & 1) == 0 && r + 1 < q.rows;
 #pragma unroll
@@ -199,71 +199,141 @@ __global__ void __launch_bounds__(256) mx_dequantize_kernel(const MxView q, T* _
 }
 
 // ----------------------------------------------------------------- product
-// Persistent CTAs over 128 x BN tiles of D, K in steps of 256: warp 0 copies the operands' codes (128-byte rows,
-// 128-byte swizzle) and scales into a ring of stages, warp 1 copies a stage's scales into tensor memory and issues
-// the block-scaled products (64 K values each), eight warps write the result.
+// Warp 0 copies the operands' codes (128-byte rows of 256 elements, 128-byte swizzle) and scales into a ring of
+// stages, warp 1 copies a stage's scales into tensor memory and issues the block-scaled products (64 K values each),
+// eight warps write the result.  As in the fp16 products of muon.cu there are two shapes:
+//   PAIR: two CTAs on a 256 x 256 tile (cta_group::2), persistent.  A CTA holds 128 rows of A and of the result, 128 of
+//         the 256 columns of B, and the scales of its rows and of all columns.  The accumulator takes 256 of the 512
+//         columns of tensor memory and the stages' scales most of the rest, so there is only one: the epilogue first
+//         moves it to registers (128 a thread), which frees it for the next tile.
+//   else: a CTA on a 128 x BN tile; with fewer tiles than SMs the CTAs of a cluster share the K range and add up
+//         their partial tiles through distributed shared memory in rank order.
 constexpr int BM = 128, KB = 256;
-constexpr int STAGES = 4;
 constexpr int EPI_WARPS = 8;
 constexpr int THREADS = 64 + 32 * EPI_WARPS;
 
-template <int BN>
+template <bool PAIR, int BN>
 struct MxTile {
-  static constexpr int ACC = BN == 256 ? 1 : 2;           // accumulators in tensor memory
-  static constexpr int NB = BN < 128 ? 1 : BN / 128;      // row tiles of B's scales that a tile touches
-  static constexpr int CODE_BYTES = (BM + BN) * (KB / 2);
+  static constexpr int TM = PAIR ? 256 : 128, TN = PAIR ? 256 : BN;  // the tile
+  static constexpr int ROWS_B = PAIR ? 128 : BN;                     // rows of B that this CTA copies
+  static constexpr int NB = TN < 128 ? 1 : TN / 128;                 // row tiles of B's scales that the tile touches
+  static constexpr int ACC = PAIR ? 1 : 2;                           // accumulators in tensor memory
+  static constexpr int CODE_BYTES = (BM + ROWS_B) * (KB / 2);
   static constexpr int STAGE_BYTES = CODE_BYTES + (1 + NB) * 1024;
+  static constexpr int STAGES = PAIR || BN == 128 ? 6 : 7;
   static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + 1024;
-  static constexpr int SF_COL = ACC * BN;                 // first tensor-memory column of the scales
+  static constexpr int SF_COL = ACC * TN;                 // first tensor-memory column of the scales
   static constexpr int SF_COLS = 8 + 8 * NB;              // per stage: A 2 x 4, B 2 x 4 NB
   static constexpr int TMEM_COLS = SF_COL + STAGES * SF_COLS <= 256 ? 256 : 512;
   static_assert(SF_COL + STAGES * SF_COLS <= 512, "tensor memory");
   static_assert(STAGE_BYTES % 1024 == 0, "swizzle atoms");
+  static_assert(PAIR || BM * TN * 4 <= STAGES * STAGE_BYTES, "a partial tile lies in the stages");
+  static_assert(SMEM_BYTES <= 232448 - 1024, "shared memory");
 };
 
-__device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* tm, int c0, int c1, uint64_t* bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(
-          smem_u32(dst)),
-      "l"(tm), "r"(smem_u32(bar)), "r"(c0), "r"(c1)
-      : "memory");
-}
-__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-                   smem_u32(dst)),
-               "l"(src), "r"(bytes), "r"(smem_u32(bar))
-               : "memory");
-}
 // 512 bytes of scales (32 rows x 16 bytes, no swizzle; groups of 8 rows 128 bytes apart) into four columns of
-// tensor memory, the same for every quadrant of lanes.
+// tensor memory, the same for every quadrant of lanes; with PAIR in both CTAs.
+template <bool PAIR>
 __device__ __forceinline__ void tc_copy_scales(uint32_t taddr, uint32_t smem_addr) {
   const uint64_t desc = (uint64_t)((smem_addr & 0x3FFFFu) >> 4) | ((uint64_t)(128 >> 4) << 32) | (1ull << 46);
-  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+  if (PAIR)
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+  else
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
 }
+template <bool PAIR>
 __device__ __forceinline__ void tc_mma_mxf4(uint32_t tmem_c, uint64_t da, uint64_t db, uint32_t idesc, uint32_t sfa,
                                             uint32_t sfb, uint32_t accum) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %6, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-      :
-      : "r"(tmem_c), "l"(da), "l"(db), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accum)
-      : "memory");
+  if (PAIR)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(tmem_c),
+        "l"(da), "l"(db), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accum)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(tmem_c),
+        "l"(da), "l"(db), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accum)
+        : "memory");
 }
 
-template <int BN>
+// Sixteen sums of row m from column n on (n < N), scaled and written.
+__device__ __forceinline__ void mx_finish16(const MxGemm& p, int m, int n, float (&f)[16]) {
+  const int N = (int)p.b.rows;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) f[j] *= p.alpha;
+  if (p.bias) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+      if (n + j < N) f[j] += p.bias[n + j];
+  }
+  if (!p.d_bf16) {
+    float* o = static_cast<float*>(p.d) + (long long)m * p.ld + n;
+    if (n + 16 <= N && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+      float4* o4 = reinterpret_cast<float4*>(o);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        float4 v = make_float4(f[4 * t], f[4 * t + 1], f[4 * t + 2], f[4 * t + 3]);
+        if (p.beta != 0.f) {
+          const float4 d = o4[t];
+          v = make_float4(v.x + p.beta * d.x, v.y + p.beta * d.y, v.z + p.beta * d.z, v.w + p.beta * d.w);
+        }
+        o4[t] = v;
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < 16; ++t)
+        if (n + t < N) o[t] = p.beta != 0.f ? f[t] + p.beta * o[t] : f[t];
+    }
+  } else {
+    __nv_bfloat16* o = static_cast<__nv_bfloat16*>(p.d) + (long long)m * p.ld + n;
+    if (p.beta != 0.f) {
+#pragma unroll
+      for (int t = 0; t < 16; ++t)
+        if (n + t < N) f[t] += p.beta * __bfloat162float(o[t]);
+    }
+    if (n + 16 <= N && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+      uint32_t w[8];
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const __nv_bfloat162 b2 = __floats2bfloat162_rn(f[2 * t], f[2 * t + 1]);
+        w[t] = *reinterpret_cast<const uint32_t*>(&b2);
+      }
+      reinterpret_cast<uint4*>(o)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+      reinterpret_cast<uint4*>(o)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    } else {
+#pragma unroll
+      for (int t = 0; t < 16; ++t)
+        if (n + t < N) o[t] = __float2bfloat16_rn(f[t]);
+    }
+  }
+}
+
+template <bool PAIR, int BN>
 __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_constant__ CUtensorMap tmA,
-                                                             const __grid_constant__ CUtensorMap tmB, const MxGemm p) {
-  using T = MxTile<BN>;
+                                                             const __grid_constant__ CUtensorMap tmB,
+                                                             const __grid_constant__ CUtensorMap tmSA,
+                                                             const __grid_constant__ CUtensorMap tmSB, const MxGemm p,
+                                                             const int split) {
+  using T = MxTile<PAIR, BN>;
+  constexpr int STAGES = T::STAGES, WCOLS = T::TN / 2;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   __shared__ uint64_t full_bar[STAGES], empty_bar[STAGES], tfull_bar[2], tempty_bar[2];
   __shared__ uint32_t tmem_base_sm;
   unsigned char* tiles = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int csize = PAIR ? 2 : split;
+  const int rank = csize > 1 ? (int)cluster_rank() : 0;
+  const int first = (int)blockIdx.x / csize, stride = (int)gridDim.x / csize;
   const int M = (int)p.a.rows, N = (int)p.b.rows;
-  const int tiles_m = (M + BM - 1) / BM, tiles_n = (N + BN - 1) / BN, total = tiles_m * tiles_n;
-  const int nkb = (int)p.a.col_tiles;
-  const int n_local = (int)blockIdx.x < total ? (total - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x : 0;
+  const int tiles_m = (M + T::TM - 1) / T::TM, tiles_n = (N + T::TN - 1) / T::TN, total = tiles_m * tiles_n;
+  const int n_local = first < total ? (total - first + stride - 1) / stride : 0;
+  const int kb_all = (int)p.a.col_tiles;
+  const int kb0 = PAIR ? 0 : (int)((long long)kb_all * rank / csize);
+  const int kb1 = PAIR ? kb_all : (int)((long long)kb_all * (rank + 1) / csize);
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {
@@ -272,60 +342,59 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
     }
     for (int s = 0; s < 2; ++s) {
       mbar_init(&tfull_bar[s], 1);
-      mbar_init(&tempty_bar[s], EPI_WARPS);
+      mbar_init(&tempty_bar[s], PAIR ? 2 * EPI_WARPS : EPI_WARPS);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_sm)),
-                 "r"((uint32_t)T::TMEM_COLS)
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
+  if (warp == 1) tmem_alloc<PAIR>(&tmem_base_sm, (uint32_t)T::TMEM_COLS);
   tc_fence_before();
   __syncthreads();
+  if (PAIR) cluster_sync();  // the peer's barriers exist
   tc_fence_after();
   const uint32_t tmem_base = tmem_base_sm;
+  pdl_launch_dependents();
+  pdl_wait();
 
   if (warp == 0) {
     if (lane == 0) {
       bool ok = true;
       int it = 0;
-      const long long b_tiles = (p.b.rows + 127) / 128;
       for (int i = 0; i < n_local && ok; ++i) {
-        const int u = (int)blockIdx.x + i * (int)gridDim.x, mt = u / tiles_n, nt = u - mt * tiles_n;
-        const long long bt = (long long)nt * BN / 128;
-        const int nb = b_tiles - bt < T::NB ? (int)(b_tiles - bt) : T::NB;
-        for (int kb = 0; kb < nkb; ++kb, ++it) {
+        const int u = first + i * stride, mt = u / tiles_n, nt = u - mt * tiles_n;
+        const int rA = mt * T::TM + (PAIR ? rank * 128 : 0), rB = nt * T::TN + (PAIR ? rank * 128 : 0);
+        for (int kb = kb0; kb < kb1; ++kb, ++it) {
           const int s = it % STAGES;
           ok = mbar_spin_bounded(&empty_bar[s], (uint32_t)(((it / STAGES) & 1) ^ 1));
           if (!ok) break;
           unsigned char* sa = tiles + (size_t)s * T::STAGE_BYTES;
-          mbar_expect_tx(&full_bar[s], T::CODE_BYTES + (1 + nb) * 1024);
-          tma_load_2d(sa, &tmA, kb * (KB / 2), mt * BM, &full_bar[s]);
-          tma_load_2d(sa + BM * (KB / 2), &tmB, kb * (KB / 2), nt * BN, &full_bar[s]);
-          bulk_load(sa + T::CODE_BYTES, p.a.scales + ((long long)mt * p.a.col_tiles + kb) * 1024, 1024, &full_bar[s]);
-          for (int j = 0; j < nb; ++j)
-            bulk_load(sa + T::CODE_BYTES + (1 + j) * 1024, p.b.scales + ((bt + j) * p.b.col_tiles + kb) * 1024, 1024,
-                      &full_bar[s]);
+          if (!PAIR || rank == 0) mbar_expect_tx(&full_bar[s], (PAIR ? 2 : 1) * T::STAGE_BYTES);
+          const uint32_t bar = PAIR ? cluster_map(smem_u32(&full_bar[s]), 0) : smem_u32(&full_bar[s]);
+          tma_load_2d_to<PAIR>(sa, &tmA, kb * (KB / 2), rA, bar);
+          tma_load_2d_to<PAIR>(sa + BM * (KB / 2), &tmB, kb * (KB / 2), rB, bar);
+          // scale tiles are rows of their maps; one behind the end (its columns are not kept) arrives as zeros
+          tma_load_2d_to<PAIR>(sa + T::CODE_BYTES, &tmSA, 0, (rA >> 7) * (int)p.a.col_tiles + kb, bar);
+#pragma unroll
+          for (int j = 0; j < T::NB; ++j)
+            tma_load_2d_to<PAIR>(sa + T::CODE_BYTES + (1 + j) * 1024, &tmSB, 0, ((nt * T::TN >> 7) + j) * (int)p.b.col_tiles + kb, bar);
         }
       }
       if (!ok) raise_error(p.err);
     }
   } else if (warp == 1) {
-    if (lane == 0) {
+    if (lane == 0 && (!PAIR || rank == 0)) {
       // E2M1 operands (1 at bits 7 and 10), E8M0 scales (bit 23); bits 29 / 4: which pair of a column's four scale
       // bytes an instruction's two blocks take
-      constexpr uint32_t IDESC = (1u << 7) | (1u << 10) | ((uint32_t)(BN >> 3) << 17) | (1u << 23) | ((uint32_t)(BM >> 4) << 24);
+      constexpr uint32_t IDESC =
+          (1u << 7) | (1u << 10) | ((uint32_t)(T::TN >> 3) << 17) | (1u << 23) | ((uint32_t)(T::TM >> 4) << 24);
       bool ok = true;
       int it = 0;
       for (int i = 0; i < n_local && ok; ++i) {
         const int slot = i % T::ACC;
-        const int u = (int)blockIdx.x + i * (int)gridDim.x, nt = u % tiles_n;
+        const int u = first + i * stride, nt = u % tiles_n;
         ok = mbar_spin_bounded(&tempty_bar[slot], (uint32_t)(((i / T::ACC) & 1) ^ 1));
         if (!ok) break;
         tc_fence_after();
-        for (int kb = 0; kb < nkb && ok; ++kb, ++it) {
+        for (int kb = kb0; kb < kb1 && ok; ++kb, ++it) {
           const int s = it % STAGES;
           ok = mbar_spin_bounded(&full_bar[s], (uint32_t)((it / STAGES) & 1));
           if (!ok) break;
@@ -334,24 +403,24 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
           const uint32_t sf = tmem_base + (uint32_t)(T::SF_COL + s * T::SF_COLS);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            tc_copy_scales(sf + h * 4, sa + T::CODE_BYTES + h * 512);
+            tc_copy_scales<PAIR>(sf + h * 4, sa + T::CODE_BYTES + h * 512);
 #pragma unroll
             for (int j = 0; j < T::NB; ++j)
-              tc_copy_scales(sf + 8 + h * 4 * T::NB + j * 4, sa + T::CODE_BYTES + (1 + j) * 1024 + h * 512);
+              tc_copy_scales<PAIR>(sf + 8 + h * 4 * T::NB + j * 4, sa + T::CODE_BYTES + (1 + j) * 1024 + h * 512);
           }
           const uint64_t da = make_desc(sa), db = make_desc(sa + BM * (KB / 2));
           // a tile narrower than a scale tile starts at one of its groups of 32 rows = one of the four columns
-          const uint32_t sub = BN < 128 ? (uint32_t)((nt * BN & 127) >> 5) : 0u;
+          const uint32_t sub = T::TN < 128 ? (uint32_t)((nt * T::TN & 127) >> 5) : 0u;
 #pragma unroll
           for (int kk = 0; kk < 4; ++kk) {
             const uint32_t id = (uint32_t)(kk & 1) * 2u;
-            tc_mma_mxf4(tmem_base + (uint32_t)(slot * BN), da + (uint64_t)(kk * 2), db + (uint64_t)(kk * 2),
-                        IDESC | (id << 29) | (id << 4), sf + (kk >> 1) * 4, sf + 8 + (kk >> 1) * 4 * T::NB + sub,
-                        (kb | kk) != 0 ? 1u : 0u);
+            tc_mma_mxf4<PAIR>(tmem_base + (uint32_t)(slot * T::TN), da + (uint64_t)(kk * 2), db + (uint64_t)(kk * 2),
+                              IDESC | (id << 29) | (id << 4), sf + (kk >> 1) * 4, sf + 8 + (kk >> 1) * 4 * T::NB + sub,
+                              (kb != kb0 || kk != 0) ? 1u : 0u);
           }
-          tc_commit(&empty_bar[s]);
+          tc_commit_to<PAIR>(&empty_bar[s]);
         }
-        if (ok) tc_commit(&tfull_bar[slot]);
+        if (ok) tc_commit_to<PAIR>(&tfull_bar[slot]);
       }
       if (!ok) raise_error(p.err);
     }
@@ -360,82 +429,77 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
     bool ok = true;
     for (int i = 0; i < n_local; ++i) {
       const int slot = i % T::ACC;
-      const int u = (int)blockIdx.x + i * (int)gridDim.x, mt = u / tiles_n, nt = u - mt * tiles_n;
-      const int m = mt * BM + quad * 32 + lane;
+      const int u = first + i * stride, mt = u / tiles_n, nt = u - mt * tiles_n;
+      const int m = mt * T::TM + (PAIR ? rank * 128 : 0) + quad * 32 + lane, c0 = half * WCOLS, n0 = nt * T::TN + c0;
       if (ok) {
         ok = mbar_wait_bounded(&tfull_bar[slot], (uint32_t)((i / T::ACC) & 1));
         ok = __all_sync(0xffffffffu, ok);
       }
       if (!ok) continue;
       tc_fence_after();
-      const uint32_t tbase = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(slot * BN);
-      for (int c = half * (BN / 2); c < (half + 1) * (BN / 2); c += 32) {
-        uint32_t v[32];
-        tc_ld32_issue(tbase + (uint32_t)c, v);
-        tc_ld_wait();
-        const int n0 = nt * BN + c;
-        if (m >= M || n0 >= N) continue;
+      const uint32_t tbase = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(slot * T::TN + c0);
+      uint32_t v[WCOLS / 32][32];
 #pragma unroll
-        for (int j = 0; j < 32; j += 8) {
-          const int n = n0 + j;
-          if (n >= N) break;
-          float f[8];
+      for (int q = 0; q < WCOLS / 32; ++q) tc_ld32_issue(tbase + (uint32_t)(q * 32), v[q]);
+      tc_ld_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if (PAIR)
+          mbar_arrive_cluster(cluster_map(smem_u32(&tempty_bar[slot]), 0));
+        else
+          mbar_arrive(&tempty_bar[slot]);
+      }
+      if (!PAIR && csize > 1) {
+        float* part = reinterpret_cast<float*>(tiles) + (size_t)c0 * BM + quad * 32 + lane;
 #pragma unroll
-          for (int t = 0; t < 8; ++t) {
-            f[t] = nkb ? p.alpha * __uint_as_float(v[j + t]) : 0.f;
-            if (p.bias && n + t < N) f[t] += p.bias[n + t];
-          }
-          if (!p.d_bf16) {
-            float* o = static_cast<float*>(p.d) + (long long)m * p.ld + n;
-            if (n + 8 <= N && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+        for (int j = 0; j < WCOLS; ++j) part[j * BM] = __uint_as_float(v[j >> 5][j & 31]);
+      } else if (m < M) {
 #pragma unroll
-              for (int t = 0; t < 8; t += 4) {
-                if (p.beta != 0.f) {
-                  const float4 d = *reinterpret_cast<const float4*>(o + t);
-                  f[t] += p.beta * d.x; f[t + 1] += p.beta * d.y; f[t + 2] += p.beta * d.z; f[t + 3] += p.beta * d.w;
-                }
-                *reinterpret_cast<float4*>(o + t) = make_float4(f[t], f[t + 1], f[t + 2], f[t + 3]);
-              }
-            } else {
+        for (int j = 0; j < WCOLS; j += 16) {
+          if (n0 + j < N) {
+            float f[16];
 #pragma unroll
-              for (int t = 0; t < 8; ++t)
-                if (n + t < N) o[t] = p.beta != 0.f ? f[t] + p.beta * o[t] : f[t];
-            }
-          } else {
-            __nv_bfloat16* o = static_cast<__nv_bfloat16*>(p.d) + (long long)m * p.ld + n;
-            if (p.beta != 0.f) {
-#pragma unroll
-              for (int t = 0; t < 8; ++t)
-                if (n + t < N) f[t] += p.beta * __bfloat162float(o[t]);
-            }
-            if (n + 8 <= N && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
-              uint32_t w[4];
-#pragma unroll
-              for (int t = 0; t < 4; ++t) {
-                const __nv_bfloat162 b2 = __floats2bfloat162_rn(f[2 * t], f[2 * t + 1]);
-                w[t] = *reinterpret_cast<const uint32_t*>(&b2);
-              }
-              *reinterpret_cast<uint4*>(o) = make_uint4(w[0], w[1], w[2], w[3]);
-            } else {
-#pragma unroll
-              for (int t = 0; t < 8; ++t)
-                if (n + t < N) o[t] = __float2bfloat16_rn(f[t]);
-            }
+            for (int t = 0; t < 16; ++t) f[t] = __uint_as_float(v[j >> 5][(j & 31) + t]);
+            mx_finish16(p, m, n0 + j, f);
           }
         }
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&tempty_bar[slot]);
     }
     if (!ok && lane == 0) raise_error(p.err);
   }
+  if (!PAIR && csize > 1) {
+    // one tile per cluster; every stage had been consumed before the partial tiles were written over them
+    __syncwarp();
+    cluster_sync();
+    if (warp >= 2) {
+      const int quad = warp & 3, half = (warp - 2) >> 2, mt = first / tiles_n, nt = first - mt * tiles_n;
+      const int m = mt * T::TM + quad * 32 + lane;
+      // columns are dealt out 16 at a time: to the CTAs, then to the two warps of a quadrant
+      for (int c = 16 * (rank + half * csize); c < T::TN && m < M; c += 32 * csize) {
+        const int n = nt * T::TN + c;
+        if (n >= N) break;
+        float f[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) f[j] = 0.f;
+        for (int r = 0; r < csize; ++r) {
+          const uint32_t from = cluster_map(smem_u32(tiles), (uint32_t)r) + (uint32_t)((c * BM + quad * 32 + lane) * 4);
+          float x[16];
+#pragma unroll
+          for (int j = 0; j < 16; ++j) x[j] = cluster_load(from + (uint32_t)(j * BM * 4));
+#pragma unroll
+          for (int j = 0; j < 16; ++j) f[j] += x[j];
+        }
+        mx_finish16(p, m, n, f);
+      }
+    }
+  }
   tc_fence_before();
   __syncthreads();
+  if (csize > 1) cluster_sync();  // nobody reads this CTA's shared or tensor memory any more
   if (warp == 1) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)T::TMEM_COLS)
-                 : "memory");
+    tmem_dealloc<PAIR>(tmem_base, (uint32_t)T::TMEM_COLS);
   }
 }
 
@@ -452,23 +516,47 @@ bool make_map_codes(CUtensorMap* tm, const MxView& v, int box_rows) {
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+// scale tiles as rows of 256 words, one a box
+bool make_map_scales(CUtensorMap* tm, const MxView& v) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[2] = {256, (cuuint64_t)((v.rows + 127) / 128 * v.col_tiles)};
+  cuuint64_t strides[1] = {1024};
+  cuuint32_t box[2] = {256, 1};
+  cuuint32_t es[2] = {1, 1};
+  return fn(tm, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, v.scales, dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 
 cudaError_t set_attributes() {
   const cudaFuncAttribute at = cudaFuncAttributeMaxDynamicSharedMemorySize;
-  cudaError_t e = cudaFuncSetAttribute(mx_gemm_kernel<256>, at, MxTile<256>::SMEM_BYTES);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(mx_gemm_kernel<64>, at, MxTile<64>::SMEM_BYTES);
+  cudaError_t e = cudaFuncSetAttribute(mx_gemm_kernel<true, 256>, at, MxTile<true, 256>::SMEM_BYTES);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(mx_gemm_kernel<false, 128>, at, MxTile<false, 128>::SMEM_BYTES);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(mx_gemm_kernel<false, 64>, at, MxTile<false, 64>::SMEM_BYTES);
   return e;
 }
 
-template <int BN>
-cudaError_t launch_mx_gemm(const MxGemm& p, int sms, cudaStream_t st, const char** why) {
-  CUtensorMap ta, tb;
-  if (!make_map_codes(&ta, p.a, BM) || !make_map_codes(&tb, p.b, BN))
+template <bool PAIR, int BN>
+cudaError_t launch_shape(const MxGemm& p, int split, long long ctas, cudaStream_t st, const char** why) {
+  using T = MxTile<PAIR, BN>;
+  CUtensorMap ta, tb, sa, sb;
+  if (!make_map_codes(&ta, p.a, BM) || !make_map_codes(&tb, p.b, T::ROWS_B) || !make_map_scales(&sa, p.a) || !make_map_scales(&sb, p.b))
     return *why = "tensor map creation failed for this shape", cudaErrorInvalidValue;
-  const long long units = ((p.a.rows + BM - 1) / BM) * ((p.b.rows + BN - 1) / BN);
-  const int ctas = (int)(units < sms ? units : sms);
-  mx_gemm_kernel<BN><<<ctas, THREADS, MxTile<BN>::SMEM_BYTES, st>>>(ta, tb, p);
-  const cudaError_t e = cudaGetLastError();
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)ctas);
+  cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = T::SMEM_BYTES;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = PAIR ? 2 : (unsigned)split;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = PAIR || split > 1 ? 2 : 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, mx_gemm_kernel<PAIR, BN>, ta, tb, sa, sb, p, split);
   if (e != cudaSuccess) *why = "kernel launch";
   return e;
 }
@@ -477,7 +565,7 @@ cudaError_t launch_mx_gemm(const MxGemm& p, int sms, cudaStream_t st, const char
 
 cudaError_t mx_quantize(const void* x, int bf16, long long ld, int transpose, const MxView& q, cudaStream_t st) {
   if (transpose) {
-    const dim3 grid((unsigned)q.col_tiles, (unsigned)((q.rows + 127) / 128 * 2));
+    const dim3 grid((unsigned)((q.rows + 127) / 128 * 2 * q.col_tiles));
     if (bf16)
       mx_quantize_t_kernel<<<grid, 256, 0, st>>>(static_cast<const __nv_bfloat16*>(x), ld, q);
     else
@@ -509,10 +597,30 @@ cudaError_t mx_gemm(const MxGemm& p, cudaStream_t st, const char** why) {
   int sms = 0;
   cudaError_t e = device_ready(known, set_attributes, &sms, why);
   if (e != cudaSuccess) return e;
-  // wide tiles once they fill the machine
-  const long long wide = ((p.a.rows + 127) / 128) * ((p.b.rows + 255) / 256);
-  if (wide >= sms) return launch_mx_gemm<256>(p, sms, st, why);
-  return launch_mx_gemm<64>(p, sms, st, why);
+  // The shape whose CTAs have the least to copy in sequence: a K block costs 35 KiB in a pair, 34 and 26 KiB in the
+  // single shapes (units of 32 KiB below); `ramp` is what filling and draining costs, a cluster's sum included.
+  const int kb = (int)p.a.col_tiles;
+  auto tiles = [&](int tm, int tn) { return ((p.a.rows + tm - 1) / tm) * ((p.b.rows + tn - 1) / tn); };
+  const long long pairs = tiles(256, 256), t128 = tiles(128, 128), t64 = tiles(128, 64);
+  int bn = 256, split = 1;
+  double cost = (double)((pairs + sms / 2 - 1) / (sms / 2)) * (kb * 1.1 + 4) + 8;
+  for (int w = 128; w >= 64; w -= 64) {
+    const long long t = w == 128 ? t128 : t64;
+    const double unit = w == 128 ? 1.06 : 0.8;
+    for (int k = 1; k <= 8 && k <= kb; ++k) {
+      if (k > 1 && (t * k > sms || k * t > (long long)max_clusters(k, sms) * k)) break;
+      const double c = (k == 1 ? (double)((t + sms - 1) / sms) : 1.0) * ((kb + k - 1) / k) * unit + 6 + (k > 1 ? 3 : 0);
+      if (c < cost) {
+        cost = c;
+        bn = w;
+        split = k;
+      }
+    }
+  }
+  if (bn == 256) return launch_shape<true, 256>(p, 1, 2 * (pairs < sms / 2 ? pairs : sms / 2), st, why);
+  const long long t = bn == 128 ? t128 : t64, want = t * split, ctas = want < sms ? want : sms;
+  if (bn == 128) return launch_shape<false, 128>(p, split, ctas, st, why);
+  return launch_shape<false, 64>(p, split, ctas, st, why);
 }
 
 }  // namespace gcada

@@ -134,6 +134,14 @@ __device__ __forceinline__ float cluster_load(uint32_t addr) {
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
   return v;
 }
+__device__ __forceinline__ float4 cluster_load4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void cluster_store4(uint32_t addr, float4 v) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
 }
@@ -172,6 +180,21 @@ __device__ __forceinline__ void tma_load_3d_to(void* dst, const CUtensorMap* tm,
         "l"(tm), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
         : "memory");
 }
+template <bool PAIR>
+__device__ __forceinline__ void tma_load_2d_to(void* dst, const CUtensorMap* tm, int c0, int c1, uint32_t bar) {
+  if (PAIR)
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(
+            smem_u32(dst)),
+        "l"(tm), "r"(bar), "r"(c0), "r"(c1)
+        : "memory");
+  else
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(
+            smem_u32(dst)),
+        "l"(tm), "r"(bar), "r"(c0), "r"(c1)
+        : "memory");
+}
 // 16-bit operands, fp32 sum; with PAIR rows 0-127 of A and of the result and columns 0-127 of B are the first CTA's.
 template <bool PAIR>
 __device__ __forceinline__ void tc_mma(uint32_t tmem_c, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accum) {
@@ -208,6 +231,13 @@ __device__ __forceinline__ void raise_error(int* err) {
 }
 
 // ----------------------------------------------------------------- host
+// Clusters of `size` CTAs, one to an SM, that run at once on a B200 (cudaOccupancyMaxActiveClusters: a cluster lies
+// in one group of SMs, and the groups are not all of one size).
+inline int max_clusters(int size, int sms) {
+  static const int at_once[9] = {0, 148, 74, 45, 33, 26, 22, 15, 15};
+  return (int)((long long)at_once[size] * sms / 148);
+}
+
 // Multiprocessors of the current device; the first call on a device also checks that it runs this library's code
 // and sets the calling file's kernel attributes.  `known` is the caller's own table, 0 = not seen yet.
 constexpr int MAX_DEVICES = 64;

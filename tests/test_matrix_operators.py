@@ -315,7 +315,7 @@ def test_infinities_and_nan_take_their_block_only():
 
 
 GEMMS = [(1, 1, 1), (1, 8, 32), (3, 5, 33), (1, 300, 1000), (2, 257, 96), (8, 130, 513), (16, 64, 64), (17, 1000, 300), (64, 40, 4096),
-         (128, 128, 256), (129, 127, 257), (130, 333, 700), (300, 260, 64), (1, 4096, 128), (1500, 2100, 160)]
+         (128, 128, 256), (129, 127, 257), (130, 333, 700), (300, 260, 64), (1, 4096, 128), (1500, 2100, 160), (200, 500, 3000), (257, 1025, 2050), (2600, 2300, 1030), (4000, 5000, 300)]
 
 
 @pytest.mark.gpu
