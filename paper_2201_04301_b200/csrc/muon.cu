@@ -34,14 +34,14 @@ constexpr int BLK_BYTES = 64 * BK * 2;                 // one copy box: 64 x 64 
 constexpr int OP_BYTES = TR * BK * 2;                  // one operand block: 16 KiB
 constexpr int STAGE_BYTES = 2 * OP_BYTES;
 constexpr int STAGES = 6;                              // even: a stage of hi parts is followed by its lo parts
-constexpr int EPI_WARPS = 8;
+constexpr int EPI_WARPS = 16;                          // four to a quadrant of tensor memory's lanes
 constexpr int THREADS = 64 + 32 * EPI_WARPS;
 constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + 1024;
 constexpr int CHUNK = 4;                               // FULL: stage pairs summed in tensor memory before the sum
                                                        // moves to registers
 constexpr float SCALE = 1024.f;                        // stored value = SCALE * matrix element
 constexpr float INV_SCALE = 1.f / 1024.f;
-constexpr int NORM_BLOCKS = 296;                       // partial sums of a matrix's squared norm
+constexpr int NORM_BLOCKS = 1184;                      // partial sums of a matrix's squared norm
 
 enum { OUT_SPLIT = 0, OUT_F32 = 1, OUT_BF16 = 2, OUT_UPDATE_F32 = 3, OUT_UPDATE_BF16 = 4 };
 
@@ -171,8 +171,7 @@ __device__ __forceinline__ Src16 load_src16(const NsGemm& a, const RowCtx& r, in
 __device__ __forceinline__ bool wanted(const NsGemm& a, int m, int n) {
   return n < a.N && !(a.sym && (m >> a.sym_log) > (n >> a.sym_log));
 }
-__device__ __forceinline__ void finish16(const NsGemm& a, const RowCtx& r, int n, float (&f)[16], const Src16& s) {
-  const int m = r.m;
+__device__ __forceinline__ void combine16(const RowCtx& r, float (&f)[16], const Src16& s) {
   if (r.src) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -184,6 +183,9 @@ __device__ __forceinline__ void finish16(const NsGemm& a, const RowCtx& r, int n
 #pragma unroll
     for (int j = 0; j < 16; ++j) f[j] = r.c_acc * f[j];
   }
+}
+__device__ __forceinline__ void emit16(const NsGemm& a, const RowCtx& r, int n, float (&f)[16]) {
+  const int m = r.m;
   if (a.out == OUT_SPLIT) {
     if (a.sym && m >= n && m < n + 16) {
 #pragma unroll
@@ -266,7 +268,7 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
   __shared__ uint64_t full_bar[STAGES], empty_bar[STAGES], tfull_bar[2], tempty_bar[2];
   __shared__ uint32_t tmem_base_sm;
   constexpr int TILE = PAIR ? 256 : 128;
-  constexpr int WCOLS = TILE / 2;                // columns of an epilogue warp
+  constexpr int WCOLS = TILE / 4;                // columns of an epilogue warp
   constexpr uint32_t TMEM_COLS = 2 * TILE;
   unsigned char* tiles = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -394,8 +396,8 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
       if (!ok) raise_error(a.err);
     }
   } else {
-    // epilogue: warp w may touch TMEM lanes 32*(w%4) .. +31; the two warps of a quadrant split the columns
-    const int quad = warp & 3, half = (warp - 2) >> 2;
+    // epilogue: warp w may touch TMEM lanes 32*(w%4) .. +31; the four warps of a quadrant split the columns
+    const int quad = warp & 3, sub = (warp - 2) >> 2;
     bool ok = true;
     int acc_no = 0;
     for (int i = 0; i < n_local; ++i) {
@@ -403,38 +405,25 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
       int mt, nt;
       tile_of(u - b * per, tiles_n, a.sym, g_tiles, mt, nt);
       const int m = mt * TILE + (PAIR ? rank * 128 : 0) + quad * 32 + lane;
-      const int c0 = half * WCOLS, n0 = nt * TILE + c0;
+      const int c0 = sub * WCOLS, n0 = nt * TILE + c0;
       const bool row_ok = m < a.M;
       RowCtx r{};
       if (row_ok) r = row_ctx(a, b, m);
       const bool direct = PAIR || csize == 1;
-      // the linear term's values do not depend on the products: those of the next 32 columns are always on their way
-      // (not with FULL, whose sums fill the registers)
-      Src16 next[2];
+      // the linear term's values do not depend on the products: each group of 16 is fetched one group ahead
+      Src16 src;
       auto fetch = [&](int q) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-          if (direct && row_ok && r.src && wanted(a, m, n0 + q + 16 * h)) next[h] = load_src16(a, r, n0 + q + 16 * h);
+        if (direct && row_ok && r.src && wanted(a, m, n0 + q)) src = load_src16(a, r, n0 + q);
       };
       auto finish = [&](const float* v, int q) {
-        Src16 now[2];
-        if (!FULL) {
-          now[0] = next[0];
-          now[1] = next[1];
-          if (q + 32 < WCOLS) fetch(q + 32);
-        }
+        float f[16];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (row_ok && wanted(a, m, n0 + q + 16 * h)) {
-            if (FULL && r.src) now[h] = load_src16(a, r, n0 + q + 16 * h);
-            float f[16];
-#pragma unroll
-            for (int j = 0; j < 16; ++j) f[j] = v[16 * h + j];
-            finish16(a, r, n0 + q + 16 * h, f, now[h]);
-          }
-        }
+        for (int j = 0; j < 16; ++j) f[j] = v[j];
+        combine16(r, f, src);
+        if (q + 16 < WCOLS) fetch(q + 16);
+        if (row_ok && wanted(a, m, n0 + q)) emit16(a, r, n0 + q, f);
       };
-      if (!FULL) fetch(0);
+      fetch(0);
       float sum[FULL ? WCOLS : 1];
       for (int c = 0; c < chunks; ++c, ++acc_no) {
         const int slot = acc_no & 1;
@@ -446,21 +435,21 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
         tc_fence_after();
         const uint32_t tbase = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(slot * TILE + c0);
 #pragma unroll
-        for (int q = 0; q < WCOLS; q += 32) {
-          uint32_t v[32];
-          tc_ld32_issue(tbase + (uint32_t)q, v);
+        for (int q = 0; q < WCOLS; q += 16) {
+          uint32_t v[16];
+          tc_ld16_issue(tbase + (uint32_t)q, v);
           tc_ld_wait();
           if (FULL) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) sum[q + j] = (c == 0 ? 0.f : sum[q + j]) + __uint_as_float(v[j]);
+            for (int j = 0; j < 16; ++j) sum[q + j] = (c == 0 ? 0.f : sum[q + j]) + __uint_as_float(v[j]);
           } else if (!direct) {
             float* part = reinterpret_cast<float*>(tiles) + (size_t)(c0 + q) * TR + quad * 32 + lane;
 #pragma unroll
-            for (int j = 0; j < 32; ++j) part[j * TR] = __uint_as_float(v[j]);
+            for (int j = 0; j < 16; ++j) part[j * TR] = __uint_as_float(v[j]);
           } else {
-            float f[32];
+            float f[16];
 #pragma unroll
-            for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]);
+            for (int j = 0; j < 16; ++j) f[j] = __uint_as_float(v[j]);
             finish(f, q);
           }
         }
@@ -480,44 +469,54 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
           for (int j = 0; j < WCOLS; ++j) part[j * TR] = sum[FULL ? j : 0];
         } else {
 #pragma unroll
-          for (int q = 0; q < WCOLS; q += 32) finish(sum + (FULL ? q : 0), q);
+          for (int q = 0; q < WCOLS; q += 16) finish(sum + (FULL ? q : 0), q);
         }
       }
     }
     if (!ok && lane == 0) raise_error(a.err);
   }
   if (!PAIR && csize > 1) {
-    // one tile per cluster: the partial tiles are complete (every stage has been consumed before they were written)
+    // One tile per cluster.  Its eight groups of 16 columns are dealt out to the CTAs, then to the four warps of a
+    // quadrant, so a thread finishes one group at most.
+    const int quad = warp & 3, c = 16 * (rank + ((warp - 2) >> 2) * csize), b = first / per;
+    int mt, nt;
+    tile_of(first - b * per, tiles_n, a.sym, g_tiles, mt, nt);
+    const int m = mt * TILE + quad * 32 + lane, n = nt * TILE + c;
+    const bool mine = warp >= 2 && c < TILE && m < a.M && wanted(a, m, n);
+    RowCtx r{};
+    Src16 src{};
+    if (mine) {
+      r = row_ctx(a, b, m);
+      if (r.src) src = load_src16(a, r, n);
+    }
+    // the partial tiles are complete (every stage had been consumed before they were written)
     __syncwarp();
     cluster_sync();
-    if (warp >= 2) {
-      const int quad = warp & 3, half = (warp - 2) >> 2;
-      const int b = first / per;
-      int mt, nt;
-      tile_of(first - b * per, tiles_n, a.sym, g_tiles, mt, nt);
-      // columns are dealt out 16 at a time: to the CTAs, then to the two warps of a quadrant
-      const int m = mt * TILE + quad * 32 + lane;
-      if (m < a.M) {
-        const RowCtx r = row_ctx(a, b, m);
-        for (int c = 16 * (rank + half * csize); c < TILE; c += 32 * csize) {
-          const int n = nt * TILE + c;
-          if (!wanted(a, m, n)) continue;
-          Src16 s;
-          if (r.src) s = load_src16(a, r, n);
-          float f[16];
+    if (mine) {
+      float f[16];
 #pragma unroll
-          for (int j = 0; j < 16; ++j) f[j] = 0.f;
-          for (int p = 0; p < csize; ++p) {
-            const uint32_t from = cluster_map(smem_u32(tiles), (uint32_t)p) + (uint32_t)((c * TR + quad * 32 + lane) * 4);
-            float x[16];
+      for (int j = 0; j < 16; ++j) f[j] = 0.f;
+      const uint32_t place = smem_u32(tiles) + (uint32_t)((c * TR + quad * 32 + lane) * 4);
+      for (int p0 = 0; p0 < csize; p0 += 2) {  // two partial tiles on their way at a time
+        float x[2][16];
 #pragma unroll
-            for (int j = 0; j < 16; ++j) x[j] = cluster_load(from + (uint32_t)(j * TR * 4));
+        for (int p = 0; p < 2; ++p) {
+          if (p0 + p < csize) {
+            const uint32_t from = cluster_map(place, (uint32_t)(p0 + p));
 #pragma unroll
-            for (int j = 0; j < 16; ++j) f[j] += x[j];
+            for (int j = 0; j < 16; ++j) x[p][j] = cluster_load(from + (uint32_t)(j * TR * 4));
           }
-          finish16(a, r, n, f, s);
+        }
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          if (p0 + p < csize) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) f[j] += x[p][j];
+          }
         }
       }
+      combine16(r, f, src);
+      emit16(a, r, n, f);
     }
   }
   tc_fence_before();

@@ -201,15 +201,15 @@ __global__ void __launch_bounds__(256) mx_dequantize_kernel(const MxView q, T* _
 // ----------------------------------------------------------------- product
 // Warp 0 copies the operands' codes (128-byte rows of 256 elements, 128-byte swizzle) and scales into a ring of
 // stages, warp 1 copies a stage's scales into tensor memory and issues the block-scaled products (64 K values each),
-// eight warps write the result.  As in the fp16 products of muon.cu there are two shapes:
+// sixteen warps write the result.  As in the fp16 products of muon.cu there are two shapes:
 //   PAIR: two CTAs on a 256 x 256 tile (cta_group::2), persistent.  A CTA holds 128 rows of A and of the result, 128 of
 //         the 256 columns of B, and the scales of its rows and of all columns.  The accumulator takes 256 of the 512
 //         columns of tensor memory and the stages' scales most of the rest, so there is only one: the epilogue first
-//         moves it to registers (128 a thread), which frees it for the next tile.
+//         moves it to registers (64 a thread), which frees it for the next tile.
 //   else: a CTA on a 128 x BN tile; with fewer tiles than SMs the CTAs of a cluster share the K range and add up
 //         their partial tiles through distributed shared memory in rank order.
 constexpr int BM = 128, KB = 256;
-constexpr int EPI_WARPS = 8;
+constexpr int EPI_WARPS = 16;
 constexpr int THREADS = 64 + 32 * EPI_WARPS;
 
 template <bool PAIR, int BN>
@@ -319,7 +319,7 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
                                                              const __grid_constant__ CUtensorMap tmSB, const MxGemm p,
                                                              const int split) {
   using T = MxTile<PAIR, BN>;
-  constexpr int STAGES = T::STAGES, WCOLS = T::TN / 2;
+  constexpr int STAGES = T::STAGES, WCOLS = T::TN / 4;  // columns of an epilogue warp
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   __shared__ uint64_t full_bar[STAGES], empty_bar[STAGES], tfull_bar[2], tempty_bar[2];
   __shared__ uint32_t tmem_base_sm;
@@ -425,12 +425,12 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
       if (!ok) raise_error(p.err);
     }
   } else {
-    const int quad = warp & 3, half = (warp - 2) >> 2;
+    const int quad = warp & 3, sub = (warp - 2) >> 2;
     bool ok = true;
     for (int i = 0; i < n_local; ++i) {
       const int slot = i % T::ACC;
       const int u = first + i * stride, mt = u / tiles_n, nt = u - mt * tiles_n;
-      const int m = mt * T::TM + (PAIR ? rank * 128 : 0) + quad * 32 + lane, c0 = half * WCOLS, n0 = nt * T::TN + c0;
+      const int m = mt * T::TM + (PAIR ? rank * 128 : 0) + quad * 32 + lane, c0 = sub * WCOLS, n0 = nt * T::TN + c0;
       if (ok) {
         ok = mbar_wait_bounded(&tfull_bar[slot], (uint32_t)((i / T::ACC) & 1));
         ok = __all_sync(0xffffffffu, ok);
@@ -438,9 +438,9 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
       if (!ok) continue;
       tc_fence_after();
       const uint32_t tbase = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(slot * T::TN + c0);
-      uint32_t v[WCOLS / 32][32];
+      uint32_t v[WCOLS / 16][16];
 #pragma unroll
-      for (int q = 0; q < WCOLS / 32; ++q) tc_ld32_issue(tbase + (uint32_t)(q * 32), v[q]);
+      for (int q = 0; q < WCOLS / 16; ++q) tc_ld16_issue(tbase + (uint32_t)(q * 16), v[q]);
       tc_ld_wait();
       tc_fence_before();
       __syncwarp();
@@ -453,14 +453,14 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
       if (!PAIR && csize > 1) {
         float* part = reinterpret_cast<float*>(tiles) + (size_t)c0 * BM + quad * 32 + lane;
 #pragma unroll
-        for (int j = 0; j < WCOLS; ++j) part[j * BM] = __uint_as_float(v[j >> 5][j & 31]);
+        for (int j = 0; j < WCOLS; ++j) part[j * BM] = __uint_as_float(v[j >> 4][j & 15]);
       } else if (m < M) {
 #pragma unroll
         for (int j = 0; j < WCOLS; j += 16) {
           if (n0 + j < N) {
             float f[16];
 #pragma unroll
-            for (int t = 0; t < 16; ++t) f[t] = __uint_as_float(v[j >> 5][(j & 31) + t]);
+            for (int t = 0; t < 16; ++t) f[t] = __uint_as_float(v[j >> 4][t]);
             mx_finish16(p, m, n0 + j, f);
           }
         }
@@ -472,26 +472,33 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
     // one tile per cluster; every stage had been consumed before the partial tiles were written over them
     __syncwarp();
     cluster_sync();
-    if (warp >= 2) {
-      const int quad = warp & 3, half = (warp - 2) >> 2, mt = first / tiles_n, nt = first - mt * tiles_n;
-      const int m = mt * T::TM + quad * 32 + lane;
-      // columns are dealt out 16 at a time: to the CTAs, then to the two warps of a quadrant
-      for (int c = 16 * (rank + half * csize); c < T::TN && m < M; c += 32 * csize) {
-        const int n = nt * T::TN + c;
-        if (n >= N) break;
-        float f[16];
+    // columns are dealt out 16 at a time, to the CTAs, then to the four warps of a quadrant: one group a thread at most
+    const int quad = warp & 3, c = 16 * (rank + ((warp - 2) >> 2) * csize), mt = first / tiles_n, nt = first - mt * tiles_n;
+    const int m = mt * T::TM + quad * 32 + lane, n = nt * T::TN + c;
+    if (warp >= 2 && c < T::TN && m < M && n < N) {
+      float f[16];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) f[j] = 0.f;
-        for (int r = 0; r < csize; ++r) {
-          const uint32_t from = cluster_map(smem_u32(tiles), (uint32_t)r) + (uint32_t)((c * BM + quad * 32 + lane) * 4);
-          float x[16];
+      for (int j = 0; j < 16; ++j) f[j] = 0.f;
+      const uint32_t place = smem_u32(tiles) + (uint32_t)((c * BM + quad * 32 + lane) * 4);
+      for (int p0 = 0; p0 < csize; p0 += 4) {
+        float x[4][16];
 #pragma unroll
-          for (int j = 0; j < 16; ++j) x[j] = cluster_load(from + (uint32_t)(j * BM * 4));
+        for (int r = 0; r < 4; ++r) {
+          if (p0 + r < csize) {
+            const uint32_t from = cluster_map(place, (uint32_t)(p0 + r));
 #pragma unroll
-          for (int j = 0; j < 16; ++j) f[j] += x[j];
+            for (int j = 0; j < 16; ++j) x[r][j] = cluster_load(from + (uint32_t)(j * BM * 4));
+          }
         }
-        mx_finish16(p, m, n, f);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          if (p0 + r < csize) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) f[j] += x[r][j];
+          }
+        }
       }
+      mx_finish16(p, m, n, f);
     }
   }
   tc_fence_before();
