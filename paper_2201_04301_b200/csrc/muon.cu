@@ -33,10 +33,10 @@ constexpr int TR = 128, BK = 64;                       // rows of an operand blo
 constexpr int BLK_BYTES = 64 * BK * 2;                 // one copy box: 64 x 64 fp16
 constexpr int OP_BYTES = TR * BK * 2;                  // one operand block: 16 KiB
 constexpr int STAGE_BYTES = 2 * OP_BYTES;
-constexpr int STAGES = 6;                              // even: a stage of hi parts is followed by its lo parts
+constexpr int STAGES = 4;                              // even: a stage of hi parts is followed by its lo parts
 constexpr int EPI_WARPS = 16;                          // four to a quadrant of tensor memory's lanes
 constexpr int THREADS = 64 + 32 * EPI_WARPS;
-constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + 1024;
+constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + EPI_WARPS * 4096 + 1024;
 constexpr int CHUNK = 4;                               // FULL: stage pairs summed in tensor memory before the sum
                                                        // moves to registers
 constexpr float SCALE = 1024.f;                        // stored value = SCALE * matrix element
@@ -65,7 +65,7 @@ struct NsGemm {
   float c_src_plain;     // PROD_POLY in the shifted form: c_src where the form does not apply
   const float* rho;      // [batch][MAX_STEPS + 1]; entry step_no is that of the iterate the step starts from
   int step_no;
-  const __half* src;     // [batch][2][.][ld_src] hi / lo planes, or null
+  const __half* src;     // [batch][2][M][ld_src] hi / lo planes, or null
   long long ld_src, src_plane;
   __half* dst;           // OUT_SPLIT: the same layout
   long long ld_dst, dst_plane;
@@ -98,157 +98,174 @@ __host__ __device__ inline int tile_count(int tiles_m, int tiles_n, int sym, int
   return n;
 }
 
-// Eight 32-bit words at once: a thread's 32 bytes are one whole sector of the memory system.
-struct Words8 {
-  uint32_t w[8];
-};
-__device__ __forceinline__ Words8 load32(const void* p) {
-  Words8 r;
-  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-               : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]),
-                 "=r"(r.w[7])
-               : "l"(p));
-  return r;
-}
-__device__ __forceinline__ void store32(void* p, const uint32_t (&w)[8]) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
-               "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-               : "memory");
-}
 __device__ __forceinline__ uint32_t pack_half2(float x, float y) {
   const __half2 h = __floats2half2_rn(x, y);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 __device__ __forceinline__ float2 unpack_half2(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
 
-// What an epilogue thread needs for the tile at hand.
-struct RowCtx {
-  int m;
-  float c_src, c_acc, diag;
-  const __half* src;  // row m
-  __half* dst;        // matrix
-  void* user;         // row m
+// Coefficients of a matrix of the batch.
+struct Coef {
+  float src, acc, diag;
 };
-__device__ __forceinline__ RowCtx row_ctx(const NsGemm& a, int b, int m) {
-  RowCtx r;
-  r.m = m;
+__device__ __forceinline__ Coef coefficients(const NsGemm& a, int b) {
+  Coef r;
   const float* rho = a.rho + (long long)b * (MAX_STEPS + 1) + a.step_no;
   const float r0 = rho[0];
   const bool plain = r0 == 1.f;
-  r.c_src = a.c_src;
-  r.c_acc = a.c_acc;
+  r.src = a.c_src;
+  r.acc = a.c_acc;
   r.diag = plain ? a.diag : 0.f;
   if (a.prod == PROD_POLY) {
     const float k = r0 * r0;
-    if (!plain) r.c_src = a.c_src_plain;
-    r.c_src *= k;
-    r.c_acc *= k * k;
+    if (!plain) r.src = a.c_src_plain;
+    r.src *= k;
+    r.acc *= k * k;
   } else if (a.prod != PROD_GRAM) {
     const float k = a.prod == PROD_APPLY ? r0 / rho[1] : r0;
-    if (plain) r.c_src += a.c_src_shift;
-    r.c_src *= k;
-    r.c_acc *= k;
+    if (plain) r.src += a.c_src_shift;
+    r.src *= k;
+    r.acc *= k;
   }
-  r.src = a.src ? a.src + (long long)b * 2 * a.src_plane + (long long)m * a.ld_src : nullptr;
-  r.dst = a.dst + (long long)b * 2 * a.dst_plane;
-  const long long o = (long long)b * a.user_stride + (long long)m * a.ld_user;
-  r.user = a.out == OUT_F32 || a.out == OUT_UPDATE_F32 ? (void*)(static_cast<float*>(a.user) + o)
-                                                        : (void*)(static_cast<__nv_bfloat16*>(a.user) + o);
   return r;
 }
 
-// Sixteen columns from n of row r.m (in range; n is a multiple of 16, columns from a.N on are padding or absent).
-struct Src16 {
-  Words8 hi, lo;
-};
-__device__ __forceinline__ Src16 load_src16(const NsGemm& a, const RowCtx& r, int n) {
-  Src16 s;
-  s.hi = load32(r.src + n);
-  s.lo = load32(r.src + a.src_plane + n);
-  return s;
+// The epilogue works on pieces of 32 rows (one a lane, as tensor memory gives them) x PW columns, each in a buffer of
+// its warp: the linear term's hi and lo parts arrive there by a tensor copy, the results take their place and leave
+// the same way.  (With a thread reading and writing its own row in global memory every access of a warp touches 32
+// lines, and those 32 cycles each were what a short product spent most of its time on.)
+constexpr int PLANE_BYTES = 2048, PIECE_BYTES = 2 * PLANE_BYTES;
+// Byte of 16-byte chunk `ch` of `row` in a plane as the copies lay it out (64- or 32-byte swizzle) ...
+template <int PW>
+__device__ __forceinline__ int plane_at(int row, int ch) {
+  return PW == 32 ? row * 64 + ((ch ^ ((row >> 1) & 3)) << 4) : row * 32 + ((ch ^ ((row >> 2) & 1)) << 4);
 }
-// Whether a thread has anything to do with the columns from n: below the diagonal blocks nothing is kept.
-__device__ __forceinline__ bool wanted(const NsGemm& a, int m, int n) {
-  return n < a.N && !(a.sym && (m >> a.sym_log) > (n >> a.sym_log));
+// ... and in a piece of floats on its way to the user's matrix.
+template <int PW>
+__device__ __forceinline__ int float_at(int row, int ch) {
+  return PW == 32 ? row * 128 + ((ch ^ (row & 7)) << 4) : row * 64 + ((ch ^ ((row >> 1) & 3)) << 4);
 }
-__device__ __forceinline__ void combine16(const RowCtx& r, float (&f)[16], const Src16& s) {
-  if (r.src) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float2 h = unpack_half2(s.hi.w[j]), l = unpack_half2(s.lo.w[j]);
-      f[2 * j] = r.c_src * (h.x + l.x) + r.c_acc * f[2 * j];
-      f[2 * j + 1] = r.c_src * (h.y + l.y) + r.c_acc * f[2 * j + 1];
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 16; ++j) f[j] = r.c_acc * f[j];
-  }
+
+__device__ __forceinline__ bool kept(const NsGemm& a, int m, int n) {  // whether a piece at (m, n) exists and is stored
+  return m < a.M && n < a.N && !(a.sym && (m >> a.sym_log) > (n >> a.sym_log));
 }
-__device__ __forceinline__ void emit16(const NsGemm& a, const RowCtx& r, int n, float (&f)[16]) {
-  const int m = r.m;
-  if (a.out == OUT_SPLIT) {
-    if (a.sym && m >= n && m < n + 16) {
+
+// One lane: the hi and lo parts of the piece at (m, n) into the buffer, once what left it before has been read.
+template <int PW>
+__device__ __forceinline__ void fetch_piece(const CUtensorMap* tm, unsigned char* buf, uint64_t* bar, int m, int n, int b) {
+  bulk_wait_read();
+  mbar_expect_tx(bar, 2 * 32 * PW * 2);
+  tma_load_3d(buf, tm, n, m, 2 * b, bar);
+  tma_load_3d(buf + PLANE_BYTES, tm, n, m, 2 * b + 1, bar);
+}
+
+// A warp: f holds row m0 + lane, columns n .. n + PW - 1 of the products' sums.
+template <int PW>
+__device__ __forceinline__ void finish_piece(const NsGemm& a, const CUtensorMap* tmD, const Coef& k, unsigned char* buf, int lane,
+                                             int m0, int n, int b, float (&f)[PW]) {
 #pragma unroll
-      for (int j = 0; j < 16; ++j)
-        if (n + j == m) f[j] += r.diag;
-    }
-    uint32_t h[8], l[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      h[j] = pack_half2(f[2 * j], f[2 * j + 1]);
-      const float2 b = unpack_half2(h[j]);
-      l[j] = pack_half2(f[2 * j] - b.x, f[2 * j + 1] - b.y);
-    }
-    __half* o = r.dst + (long long)m * a.ld_dst + n;
-    store32(o, h);
-    if (a.write_lo) store32(o + a.dst_plane, l);
-  } else if (a.out == OUT_F32 || a.out == OUT_UPDATE_F32) {
-    float* o = static_cast<float*>(r.user) + n;
-    const bool upd = a.out == OUT_UPDATE_F32;
-    if (n + 16 <= a.N && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
-      float4 p[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (upd) p[j] = *reinterpret_cast<const float4*>(o + 4 * j);
+  for (int c = 0; c < PW / 8; ++c) {
+    if (a.src) {
+      const uint4 h = *reinterpret_cast<const uint4*>(buf + plane_at<PW>(lane, c));
+      const uint4 l = *reinterpret_cast<const uint4*>(buf + PLANE_BYTES + plane_at<PW>(lane, c));
+      const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, lw[4] = {l.x, l.y, l.z, l.w};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        float4 w = make_float4(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]);
-        if (upd)
-          w = make_float4(a.decay * p[j].x - a.step * w.x, a.decay * p[j].y - a.step * w.y,
-                          a.decay * p[j].z - a.step * w.z, a.decay * p[j].w - a.step * w.w);
-        *reinterpret_cast<float4*>(o + 4 * j) = w;
+        const float2 x = unpack_half2(hw[j]), y = unpack_half2(lw[j]);
+        f[8 * c + 2 * j] = k.src * (x.x + y.x) + k.acc * f[8 * c + 2 * j];
+        f[8 * c + 2 * j + 1] = k.src * (x.y + y.y) + k.acc * f[8 * c + 2 * j + 1];
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < 16; ++j)
-        if (n + j < a.N) o[j] = upd ? a.decay * o[j] - a.step * f[j] : f[j];
-    }
-  } else {
-    __nv_bfloat16* o = static_cast<__nv_bfloat16*>(r.user) + n;
-    const bool upd = a.out == OUT_UPDATE_BF16;
-    if (n + 16 <= a.N && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
-      uint4* o4 = reinterpret_cast<uint4*>(o);
-      if (upd) {
-        const uint4 p = o4[0], q = o4[1];
-        const uint32_t pw[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-          f[j] = a.decay * __uint_as_float(j & 1 ? pw[j >> 1] & 0xffff0000u : pw[j >> 1] << 16) - a.step * f[j];
-      }
-      uint32_t w[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const __nv_bfloat162 t = __floats2bfloat162_rn(f[2 * j], f[2 * j + 1]);
-        w[j] = *reinterpret_cast<const uint32_t*>(&t);
-      }
-      o4[0] = make_uint4(w[0], w[1], w[2], w[3]);
-      o4[1] = make_uint4(w[4], w[5], w[6], w[7]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 16; ++j)
-        if (n + j < a.N) o[j] = __float2bfloat16_rn(upd ? a.decay * __bfloat162float(o[j]) - a.step * f[j] : f[j]);
+      for (int j = 0; j < 8; ++j) f[8 * c + j] *= k.acc;
     }
   }
+  if (a.out == OUT_SPLIT) {
+    const int d = m0 + lane - n;
+    if (a.sym && d >= 0 && d < PW) {
+#pragma unroll
+      for (int j = 0; j < PW; ++j)
+        if (j == d) f[j] += k.diag;
+    }
+    if (!a.src) {  // (with a linear term the piece's fetch has waited for the buffer)
+      if (lane == 0) bulk_wait_read();
+      __syncwarp();
+    }
+#pragma unroll
+    for (int c = 0; c < PW / 8; ++c) {
+      uint32_t h[4], l[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float x = f[8 * c + 2 * j], y = f[8 * c + 2 * j + 1];
+        h[j] = pack_half2(x, y);
+        const float2 r = unpack_half2(h[j]);
+        l[j] = pack_half2(x - r.x, y - r.y);
+      }
+      *reinterpret_cast<uint4*>(buf + plane_at<PW>(lane, c)) = make_uint4(h[0], h[1], h[2], h[3]);
+      if (a.write_lo) *reinterpret_cast<uint4*>(buf + PLANE_BYTES + plane_at<PW>(lane, c)) = make_uint4(l[0], l[1], l[2], l[3]);
+    }
+    fence_async_shared();
+    __syncwarp();
+    if (lane == 0) {
+      tma_store_3d(tmD, buf, n, m0, 2 * b);
+      if (a.write_lo) tma_store_3d(tmD, buf + PLANE_BYTES, n, m0, 2 * b + 1);
+      bulk_commit();
+    }
+    return;
+  }
+  // the user's matrix: through the buffer as floats, then neighbouring lanes along a row
+  __syncwarp();
+#pragma unroll
+  for (int c = 0; c < PW / 4; ++c)
+    *reinterpret_cast<float4*>(buf + float_at<PW>(lane, c)) = make_float4(f[4 * c], f[4 * c + 1], f[4 * c + 2], f[4 * c + 3]);
+  __syncwarp();
+  constexpr int CH = PW / 4, RPP = 32 / CH;  // chunks of a row, rows of a pass
+  const bool f32 = a.out == OUT_F32 || a.out == OUT_UPDATE_F32, upd = a.out == OUT_UPDATE_F32 || a.out == OUT_UPDATE_BF16;
+  const int ch = lane % CH, col = n + 4 * ch;
+#pragma unroll 1
+  for (int r0 = 0; r0 < 32; r0 += RPP) {
+    const int row = r0 + lane / CH, m = m0 + row;
+    if (m >= a.M || col >= a.N) continue;
+    const float4 v4 = *reinterpret_cast<const float4*>(buf + float_at<PW>(row, ch));
+    float v[4] = {v4.x, v4.y, v4.z, v4.w};
+    const long long at = (long long)b * a.user_stride + (long long)m * a.ld_user + col;
+    if (f32) {
+      float* o = static_cast<float*>(a.user) + at;
+      if (col + 4 <= a.N && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+        if (upd) {
+          const float4 w = *reinterpret_cast<const float4*>(o);
+          v[0] = a.decay * w.x - a.step * v[0];
+          v[1] = a.decay * w.y - a.step * v[1];
+          v[2] = a.decay * w.z - a.step * v[2];
+          v[3] = a.decay * w.w - a.step * v[3];
+        }
+        *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (col + j < a.N) o[j] = upd ? a.decay * o[j] - a.step * v[j] : v[j];
+      }
+    } else {
+      __nv_bfloat16* o = static_cast<__nv_bfloat16*>(a.user) + at;
+      if (col + 4 <= a.N && (reinterpret_cast<uintptr_t>(o) & 7) == 0) {
+        if (upd) {
+          const uint2 w = *reinterpret_cast<const uint2*>(o);
+          v[0] = a.decay * __uint_as_float(w.x << 16) - a.step * v[0];
+          v[1] = a.decay * __uint_as_float(w.x & 0xffff0000u) - a.step * v[1];
+          v[2] = a.decay * __uint_as_float(w.y << 16) - a.step * v[2];
+          v[3] = a.decay * __uint_as_float(w.y & 0xffff0000u) - a.step * v[3];
+        }
+        const __nv_bfloat162 x = __floats2bfloat162_rn(v[0], v[1]), y = __floats2bfloat162_rn(v[2], v[3]);
+        *reinterpret_cast<uint2*>(o) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (col + j < a.N) o[j] = __float2bfloat16_rn(upd ? a.decay * __bfloat162float(o[j]) - a.step * v[j] : v[j]);
+      }
+    }
+  }
+  fence_async_shared();  // the buffer's next content may come by a tensor copy
+  __syncwarp();
 }
 
 // One product.  Warp 0 copies operand blocks (128 rows or columns x 64 K values) into a ring of stages, warp 1
@@ -263,9 +280,11 @@ __device__ __forceinline__ void emit16(const NsGemm& a, const RowCtx& r, int n, 
 // registers, because the tensor cores cut (not round) each partial sum.
 template <bool PAIR, bool FULL>
 __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_constant__ CUtensorMap tmA,
-                                                             const __grid_constant__ CUtensorMap tmB, const NsGemm a) {
+                                                             const __grid_constant__ CUtensorMap tmB,
+                                                             const __grid_constant__ CUtensorMap tmS,
+                                                             const __grid_constant__ CUtensorMap tmD, const NsGemm a) {
   extern __shared__ __align__(1024) unsigned char smem_raw[];
-  __shared__ uint64_t full_bar[STAGES], empty_bar[STAGES], tfull_bar[2], tempty_bar[2];
+  __shared__ uint64_t full_bar[STAGES], empty_bar[STAGES], tfull_bar[2], tempty_bar[2], src_bar[EPI_WARPS];
   __shared__ uint32_t tmem_base_sm;
   constexpr int TILE = PAIR ? 256 : 128;
   constexpr int WCOLS = TILE / 4;                // columns of an epilogue warp
@@ -295,9 +314,16 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
       mbar_init(&tfull_bar[s], 1);
       mbar_init(&tempty_bar[s], PAIR ? 2 * EPI_WARPS : EPI_WARPS);
     }
+    for (int s = 0; s < EPI_WARPS; ++s) mbar_init(&src_bar[s], 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) tmem_alloc<PAIR>(&tmem_base_sm, TMEM_COLS);
+  if (threadIdx.x == 64) {
+    prefetch_map(&tmA);
+    prefetch_map(&tmB);
+    prefetch_map(&tmS);
+    prefetch_map(&tmD);
+  }
   tc_fence_before();
   __syncthreads();
   if (PAIR) cluster_sync();  // the peer's barriers exist
@@ -398,32 +424,20 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
   } else {
     // epilogue: warp w may touch TMEM lanes 32*(w%4) .. +31; the four warps of a quadrant split the columns
     const int quad = warp & 3, sub = (warp - 2) >> 2;
+    unsigned char* buf = tiles + (size_t)STAGES * STAGE_BYTES + (size_t)(warp - 2) * PIECE_BYTES;
+    uint64_t* bar = &src_bar[warp - 2];
+    const bool direct = PAIR || csize == 1;
+    uint32_t fetched = 0;  // pieces fetched so far: the parity of the buffer's barrier
     bool ok = true;
     int acc_no = 0;
     for (int i = 0; i < n_local; ++i) {
       const int u = first + i * stride, b = u / per;
       int mt, nt;
       tile_of(u - b * per, tiles_n, a.sym, g_tiles, mt, nt);
-      const int m = mt * TILE + (PAIR ? rank * 128 : 0) + quad * 32 + lane;
-      const int c0 = sub * WCOLS, n0 = nt * TILE + c0;
-      const bool row_ok = m < a.M;
-      RowCtx r{};
-      if (row_ok) r = row_ctx(a, b, m);
-      const bool direct = PAIR || csize == 1;
-      // the linear term's values do not depend on the products: each group of 16 is fetched one group ahead
-      Src16 src;
-      auto fetch = [&](int q) {
-        if (direct && row_ok && r.src && wanted(a, m, n0 + q)) src = load_src16(a, r, n0 + q);
-      };
-      auto finish = [&](const float* v, int q) {
-        float f[16];
-#pragma unroll
-        for (int j = 0; j < 16; ++j) f[j] = v[j];
-        combine16(r, f, src);
-        if (q + 16 < WCOLS) fetch(q + 16);
-        if (row_ok && wanted(a, m, n0 + q)) emit16(a, r, n0 + q, f);
-      };
-      fetch(0);
+      const int m0 = mt * TILE + (PAIR ? rank * 128 : 0) + quad * 32, c0 = sub * WCOLS, n0 = nt * TILE + c0;
+      // the linear term does not depend on the products: the first piece's is on its way while those are formed
+      if (direct && a.src && lane == 0 && kept(a, m0, n0)) fetch_piece<32>(&tmS, buf, bar, m0, n0, b);
+      const Coef k = coefficients(a, b);
       float sum[FULL ? WCOLS : 1];
       for (int c = 0; c < chunks; ++c, ++acc_no) {
         const int slot = acc_no & 1;
@@ -434,23 +448,41 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
         if (!ok) continue;
         tc_fence_after();
         const uint32_t tbase = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(slot * TILE + c0);
+        if (FULL && chunks > 1) {
+          // the chunks are added up in registers; the last one's accumulator takes the total
 #pragma unroll
-        for (int q = 0; q < WCOLS; q += 16) {
-          uint32_t v[16];
-          tc_ld16_issue(tbase + (uint32_t)q, v);
-          tc_ld_wait();
-          if (FULL) {
+          for (int q = 0; q < WCOLS; q += 16) {
+            uint32_t v[16];
+            tc_ld16_issue(tbase + (uint32_t)q, v);
+            tc_ld_wait();
 #pragma unroll
-            for (int j = 0; j < 16; ++j) sum[q + j] = (c == 0 ? 0.f : sum[q + j]) + __uint_as_float(v[j]);
-          } else if (!direct) {
-            float* part = reinterpret_cast<float*>(tiles) + (size_t)(c0 + q) * TR + quad * 32 + lane;
+            for (int j = 0; j < 16; ++j) sum[FULL ? q + j : 0] = (c == 0 ? 0.f : sum[FULL ? q + j : 0]) + __uint_as_float(v[j]);
+            if (c == chunks - 1) tc_st16(tbase + (uint32_t)q, sum + (FULL ? q : 0));
+          }
+          if (c == chunks - 1) tc_st_wait();
+        }
+        if (c == chunks - 1) {
+#pragma unroll 1
+          for (int q = 0; q < WCOLS; q += 32) {
+            uint32_t v[32];
+            tc_ld32_issue(tbase + (uint32_t)q, v);
+            tc_ld_wait();
+            if (!direct) {
+              float* part = reinterpret_cast<float*>(tiles) + (size_t)(c0 + q) * TR + quad * 32 + lane;
 #pragma unroll
-            for (int j = 0; j < 16; ++j) part[j * TR] = __uint_as_float(v[j]);
-          } else {
-            float f[16];
+              for (int j = 0; j < 32; ++j) part[j * TR] = __uint_as_float(v[j]);
+              continue;
+            }
+            if (!kept(a, m0, n0 + q)) continue;
+            if (a.src) {
+              if (q && lane == 0) fetch_piece<32>(&tmS, buf, bar, m0, n0 + q, b);
+              ok = __all_sync(0xffffffffu, mbar_wait_bounded(bar, fetched++ & 1u));
+              if (!ok) break;
+            }
+            float f[32];
 #pragma unroll
-            for (int j = 0; j < 16; ++j) f[j] = __uint_as_float(v[j]);
-            finish(f, q);
+            for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]);
+            finish_piece<32>(a, &tmD, k, buf, lane, m0, n0 + q, b, f);
           }
         }
         tc_fence_before();
@@ -462,33 +494,19 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
             mbar_arrive(&tempty_bar[slot]);
         }
       }
-      if (FULL && ok) {
-        if (!direct) {
-          float* part = reinterpret_cast<float*>(tiles) + (size_t)c0 * TR + quad * 32 + lane;
-#pragma unroll
-          for (int j = 0; j < WCOLS; ++j) part[j * TR] = sum[FULL ? j : 0];
-        } else {
-#pragma unroll
-          for (int q = 0; q < WCOLS; q += 16) finish(sum + (FULL ? q : 0), q);
-        }
-      }
     }
     if (!ok && lane == 0) raise_error(a.err);
   }
   if (!PAIR && csize > 1) {
     // One tile per cluster.  Its eight groups of 16 columns are dealt out to the CTAs, then to the four warps of a
-    // quadrant, so a thread finishes one group at most.
+    // quadrant, so a warp finishes one piece of 16 columns at most.
     const int quad = warp & 3, c = 16 * (rank + ((warp - 2) >> 2) * csize), b = first / per;
     int mt, nt;
     tile_of(first - b * per, tiles_n, a.sym, g_tiles, mt, nt);
-    const int m = mt * TILE + quad * 32 + lane, n = nt * TILE + c;
-    const bool mine = warp >= 2 && c < TILE && m < a.M && wanted(a, m, n);
-    RowCtx r{};
-    Src16 src{};
-    if (mine) {
-      r = row_ctx(a, b, m);
-      if (r.src) src = load_src16(a, r, n);
-    }
+    const int m0 = mt * TILE + quad * 32, n = nt * TILE + c;
+    const bool mine = warp >= 2 && c < TILE && kept(a, m0, n);
+    unsigned char* buf = tiles + (size_t)STAGES * STAGE_BYTES + (size_t)(warp - 2) * PIECE_BYTES;
+    if (mine && a.src && lane == 0) fetch_piece<16>(&tmS, buf, &src_bar[warp - 2], m0, n, b);
     // the partial tiles are complete (every stage had been consumed before they were written)
     __syncwarp();
     cluster_sync();
@@ -497,6 +515,7 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
 #pragma unroll
       for (int j = 0; j < 16; ++j) f[j] = 0.f;
       const uint32_t place = smem_u32(tiles) + (uint32_t)((c * TR + quad * 32 + lane) * 4);
+#pragma unroll 1
       for (int p0 = 0; p0 < csize; p0 += 2) {  // two partial tiles on their way at a time
         float x[2][16];
 #pragma unroll
@@ -515,10 +534,15 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
           }
         }
       }
-      combine16(r, f, src);
-      emit16(a, r, n, f);
+      bool ok = true;
+      if (a.src) ok = __all_sync(0xffffffffu, mbar_wait_bounded(&src_bar[warp - 2], 0));
+      if (ok)
+        finish_piece<16>(a, &tmD, coefficients(a, b), buf, lane, m0, n, b, f);
+      else if (lane == 0)
+        raise_error(a.err);
     }
   }
+  if (warp >= 2 && lane == 0) bulk_wait();  // the results have left
   tc_fence_before();
   __syncthreads();
   if (csize > 1) cluster_sync();  // nobody reads this CTA's shared or tensor memory any more
@@ -663,17 +687,20 @@ __global__ void __launch_bounds__(256) ns_copy_kernel(const NsGemm a) {
 }
 
 // ----------------------------------------------------------------- host
-// fp16 array [planes][rows][cols], row stride ld elements; boxes of 64 x 64, 128-byte swizzle, zero fill outside.
+// fp16 array [planes][rows][cols], row stride ld elements, zero fill outside; boxes of 64 columns x 64 rows with the
+// 128-byte swizzle (operands), or 32 or 16 columns x 32 rows with the 64- or 32-byte one (epilogue pieces).
 bool make_map_f16(CUtensorMap* tm, const void* base, long long cols, long long rows, long long planes, long long ld,
-                  long long plane) {
+                  long long plane, int width = 64) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
   cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
   cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)plane * 2};
-  cuuint32_t box[3] = {64, 64, 1};
+  cuuint32_t box[3] = {(cuuint32_t)width, width == 64 ? 64u : 32u, 1};
   cuuint32_t es[3] = {1, 1, 1};
   return fn(tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(base), dims, strides, box, es,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+            CU_TENSOR_MAP_INTERLEAVE_NONE,
+            width == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : width == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -720,6 +747,11 @@ cudaError_t set_attributes() {
 
 template <bool PAIR, bool FULL>
 cudaError_t launch_shape(const CUtensorMap& ta, const CUtensorMap& tb, const NsGemm& a, int ctas, cudaStream_t st) {
+  CUtensorMap ts = ta, td = ta;  // the epilogue's pieces; not used where there is no linear term or a user's matrix
+  const int width = PAIR || a.split == 1 ? 32 : 16;
+  if ((a.src && !make_map_f16(&ts, a.src, a.N, a.M, 2LL * a.batch, a.ld_src, a.src_plane, width)) ||
+      (a.out == OUT_SPLIT && !make_map_f16(&td, a.dst, a.N, a.M, 2LL * a.batch, a.ld_dst, a.dst_plane, width)))
+    return cudaErrorInvalidValue;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)ctas);
   cfg.blockDim = dim3(THREADS);
@@ -733,7 +765,7 @@ cudaError_t launch_shape(const CUtensorMap& ta, const CUtensorMap& tb, const NsG
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = PAIR || a.split > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, ns_gemm_kernel<PAIR, FULL>, ta, tb, a);
+  return cudaLaunchKernelEx(&cfg, ns_gemm_kernel<PAIR, FULL>, ta, tb, ts, td, a);
 }
 
 // A K block costs a CTA the same 32 KiB from L2 in either shape (about 512 cycles), so the shape is the one with

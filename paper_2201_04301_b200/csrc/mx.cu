@@ -347,6 +347,12 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) tmem_alloc<PAIR>(&tmem_base_sm, (uint32_t)T::TMEM_COLS);
+  if (threadIdx.x == 64) {
+    prefetch_map(&tmA);
+    prefetch_map(&tmB);
+    prefetch_map(&tmSA);
+    prefetch_map(&tmSB);
+  }
   tc_fence_before();
   __syncthreads();
   if (PAIR) cluster_sync();  // the peer's barriers exist
