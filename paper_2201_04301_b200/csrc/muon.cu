@@ -779,11 +779,11 @@ Shape choose_shape(int M, int N, int K, int sym, int g, int batch, int full, int
   auto tiles = [&](int t, int gt) { return (long long)tile_count((M + t - 1) / t, (N + t - 1) / t, sym, gt) * batch; };
   const long long pairs = tiles(256, 0), singles = tiles(128, g);
   // FULL: 64 KiB and three products a block; a pair's products (1536 cycles) then outlast its copies (1024)
-  const int kb_pair = full ? 3 : 1, kb_single = full ? 2 : 1, ramp_pair = 10, ramp_single = 6;
+  const int kb_pair = full ? 3 : 1, kb_single = full ? 2 : 1, ramp_pair = 14, ramp_single = 6;
   Shape s{false, 1};
   long long cost = (singles + sms - 1) / sms * kb * kb_single + ramp_single;
   for (int k = 2; k <= 8 && singles <= max_clusters(k, sms) && kb >= 2 * k; ++k) {
-    const long long c = (kb + k - 1) / k * kb_single + ramp_single + 2;
+    const long long c = (kb + k - 1) / k * kb_single + ramp_single + 10;
     if (c < cost) {
       cost = c;
       s.split = k;

@@ -61,75 +61,109 @@ __device__ __forceinline__ void load8(const T* p, long long n, float (&f)[8]) {
   }
 }
 
-// One warp: a row's 256 columns, eight per lane; four lanes share a block.  Rows run to the end of the last row
-// tile (their scales are zeroed).
+__device__ __forceinline__ long long scale_word(const MxView& q, int r, int ct, int half) {  // byte of a row's four scales
+  return ((long long)(r >> 7) * q.col_tiles + ct) * 1024 + half * 512 + (r & 31) * 16 + ((r & 127) >> 5) * 4;
+}
+
+// A warp takes one column tile (256 columns, eight a lane, four lanes to a block of 32) of every `pass`-th row; warps
+// next to each other take neighbouring tiles of a row.  ROWS_AT_ONCE rows' loads are on their way together.
+constexpr int ROWS_AT_ONCE = 4;
+struct WarpPlace {
+  int ct, row;
+};
+__device__ __forceinline__ WarpPlace warp_place(const MxView& q, int pass) {
+  const unsigned int g = blockIdx.x * 8u + (threadIdx.x >> 5), tiles = (unsigned int)q.col_tiles, row = g / tiles;
+  return WarpPlace{(int)(g - row * tiles), (int)row < pass ? (int)row : 1 << 30};
+}
+
+// Rows run to the end of the last row tile (their scales are zeroed).
 template <typename T>
-__global__ void __launch_bounds__(256) mx_quantize_kernel(const T* __restrict__ x, long long ld, const MxView q) {
-  const int lane = threadIdx.x & 31;
-  const long long row_end = (q.rows + 127) / 128 * 128, units = row_end * q.col_tiles;
-  for (long long u = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); u < units; u += (long long)gridDim.x * 8) {
-    const long long r = u / q.col_tiles, ct = u - r * q.col_tiles, c = ct * 256 + lane * 8;
-    float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (r < q.rows && c < q.cols) load8(x + r * ld + c, q.cols - c, f);
-    uint32_t top = 0;
+__global__ void __launch_bounds__(256) mx_quantize_kernel(const T* __restrict__ x, long long ld, const MxView q, int pass) {
+  const int lane = threadIdx.x & 31, rows = (int)q.rows, row_end = (rows + 127) / 128 * 128;
+  const WarpPlace at = warp_place(q, pass);
+  const int ct = at.ct;
+  const long long c = (long long)ct * 256 + lane * 8;
+  for (int r0 = at.row; r0 < row_end; r0 += ROWS_AT_ONCE * pass) {
+    float f[ROWS_AT_ONCE][8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) top = max(top, abs_bits(f[j]));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    const uint32_t sc = scale_code(__uint_as_float(top));
-    const float inv = inverse_scale(sc);
+    for (int u = 0; u < ROWS_AT_ONCE; ++u) {
+      const int r = r0 + u * pass;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] *= inv;
-    if (r < q.rows && c < q.pitch * 2) *reinterpret_cast<uint32_t*>(q.codes + r * q.pitch + c / 2) = codes8(f);
-    // four blocks' scales are one word of a tile
-    uint32_t word = sc << (8 * ((lane >> 2) & 3));
-    word |= __shfl_xor_sync(0xffffffffu, word, 4);
-    word |= __shfl_xor_sync(0xffffffffu, word, 8);
-    if ((lane & 15) == 0) {
-      const int rr = (int)(r & 127);
-      *reinterpret_cast<uint32_t*>(q.scales + ((r >> 7) * q.col_tiles + ct) * 1024 + (lane >> 4) * 512 + (rr & 31) * 16 +
-                                   (rr >> 5) * 4) = word;
+      for (int j = 0; j < 8; ++j) f[u][j] = 0.f;
+      if (r < rows && c < q.cols) load8(x + r * ld + c, q.cols - c, f[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < ROWS_AT_ONCE; ++u) {
+      const int r = r0 + u * pass;
+      uint32_t top = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = max(top, abs_bits(f[u][j]));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const uint32_t sc = scale_code(__uint_as_float(top));
+      const float inv = inverse_scale(sc);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[u][j] *= inv;
+      if (r < rows && c < q.pitch * 2) *reinterpret_cast<uint32_t*>(q.codes + r * q.pitch + c / 2) = codes8(f[u]);
+      // four blocks' scales are one word of a tile
+      uint32_t word = sc << (8 * ((lane >> 2) & 3));
+      word |= __shfl_xor_sync(0xffffffffu, word, 4);
+      word |= __shfl_xor_sync(0xffffffffu, word, 8);
+      if ((lane & 15) == 0 && r < row_end) *reinterpret_cast<uint32_t*>(q.scales + scale_word(q, r, ct, lane >> 4)) = word;
     }
   }
 }
 
+// Two neighbouring elements, as loaded.
+template <typename T>
+struct Pair2;
+template <>
+struct Pair2<float> {
+  using raw = float2;
+  static __device__ __forceinline__ float lo(float2 v) { return v.x; }
+  static __device__ __forceinline__ float hi(float2 v) { return v.y; }
+  static __device__ __forceinline__ float2 make(float a, float b) { return make_float2(a, b); }
+};
+template <>
+struct Pair2<__nv_bfloat16> {
+  using raw = uint32_t;
+  static __device__ __forceinline__ float lo(uint32_t v) { return __uint_as_float(v << 16); }
+  static __device__ __forceinline__ float hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
+  static __device__ __forceinline__ uint32_t make(__nv_bfloat16 a, __nv_bfloat16 b) {
+    return (uint32_t)__bfloat16_as_ushort(a) | ((uint32_t)__bfloat16_as_ushort(b) << 16);
+  }
+};
+
 // Transposed source: x is [q.cols][q.rows], blocks run down its columns.  A CTA takes 64 columns (rows of the
-// result) x 256 rows; warp w the block of 32 rows w, two columns per lane; codes and scales leave through shared
-// memory so that a result row's 128 bytes are written together.
+// result) x 256 rows; warp w the block of 32 rows w, two columns per lane, all 32 loads on their way together
+// (guarded one by one they were not: 321 us for 32768 x 4096 bf16); codes and scales leave through shared memory so
+// that a result row's 128 bytes are written together.  CTAs that run together take neighbouring columns.
 template <typename T>
 __global__ void __launch_bounds__(256) mx_quantize_t_kernel(const T* __restrict__ x, long long ld, const MxView q) {
+  using P = Pair2<T>;
   __shared__ __align__(16) uint4 codes_sm[64][9];  // [row][block], padded
   __shared__ uint32_t scale_sm[64][2];
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  const long long strips = (q.rows + 127) / 128 * 2, ct = blockIdx.x / strips, r0 = (blockIdx.x - ct * strips) * 64, k0 = ct * 256 + w * 32, r = r0 + 2 * lane;
-  float v[2][32];
-  const bool pair = (reinterpret_cast<uintptr_t>(x) & (2 * sizeof(T) - 1)) == 0 && (ld & 1) == 0 && r + 1 < q.rows;
+  const long long strips = (q.rows + 127) / 128 * 2, ct = blockIdx.x / strips, r0 = (blockIdx.x - ct * strips) * 64;
+  const long long k0 = ct * 256 + w * 32, r = r0 + 2 * lane;
+  typename P::raw v[32];
+  const T* p = x + k0 * ld + r;
+  const bool aligned = (reinterpret_cast<uintptr_t>(x) & (2 * sizeof(T) - 1)) == 0 && (ld & 1) == 0;
+  if (aligned && r0 + 64 <= q.rows && k0 + 32 <= q.cols) {  // the same for the whole warp
 #pragma unroll
-  for (int j = 0; j < 32; ++j) {
-    v[0][j] = v[1][j] = 0.f;
-    if (k0 + j < q.cols) {
-      const T* p = x + (k0 + j) * ld + r;
-      if (pair) {
-        if (sizeof(T) == 4) {
-          const float2 t = *reinterpret_cast<const float2*>(p);
-          v[0][j] = t.x;
-          v[1][j] = t.y;
-        } else {
-          const uint32_t t = *reinterpret_cast<const uint32_t*>(p);
-          v[0][j] = __uint_as_float(t << 16);
-          v[1][j] = __uint_as_float(t & 0xffff0000u);
-        }
-      } else {
-        if (r < q.rows) v[0][j] = (float)p[0];
-        if (r + 1 < q.rows) v[1][j] = (float)p[1];
-      }
+    for (int j = 0; j < 32; ++j) v[j] = *reinterpret_cast<const typename P::raw*>(p + j * ld);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+      const bool in = k0 + j < q.cols;
+      v[j] = P::make(in && r < q.rows ? p[j * ld] : (T)0.f, in && r + 1 < q.rows ? p[j * ld + 1] : (T)0.f);
     }
   }
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     uint32_t top = 0;
 #pragma unroll
-    for (int j = 0; j < 32; ++j) top = max(top, abs_bits(v[h][j]));
+    for (int j = 0; j < 32; ++j) top = max(top, abs_bits(h ? P::hi(v[j]) : P::lo(v[j])));
     const uint32_t sc = scale_code(__uint_as_float(top));
     const float inv = inverse_scale(sc);
     uint32_t c[4];
@@ -137,7 +171,7 @@ __global__ void __launch_bounds__(256) mx_quantize_t_kernel(const T* __restrict_
     for (int g = 0; g < 4; ++g) {
       float f[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = v[h][8 * g + j] * inv;
+      for (int j = 0; j < 8; ++j) f[j] = (h ? P::hi(v[8 * g + j]) : P::lo(v[8 * g + j])) * inv;
       c[g] = codes8(f);
     }
     codes_sm[2 * lane + h][w] = make_uint4(c[0], c[1], c[2], c[3]);
@@ -151,49 +185,77 @@ __global__ void __launch_bounds__(256) mx_quantize_t_kernel(const T* __restrict_
   }
   if (threadIdx.x < 128) {  // rows behind the end have zero elements, hence zero scales
     const int rr = threadIdx.x >> 1, half = threadIdx.x & 1;
-    const long long row = r0 + rr;
-    const int in = (int)(row & 127);
-    *reinterpret_cast<uint32_t*>(q.scales + ((row >> 7) * q.col_tiles + ct) * 1024 + half * 512 + (in & 31) * 16 +
-                                 (in >> 5) * 4) = scale_sm[rr][half];
+    *reinterpret_cast<uint32_t*>(q.scales + scale_word(q, (int)r0 + rr, (int)ct, half)) = scale_sm[rr][half];
+  }
+}
+
+// Eight codes as four pairs of bfloat16 numbers: the magnitudes' two bytes looked up four codes at a time, the signs
+// put in their place, one product with the scale (exact: a power of two).
+__device__ __forceinline__ void values8(uint32_t w, uint32_t sc, uint32_t (&o)[4]) {
+  const uint32_t s16 = sc == 255u ? 0x7fffu : (sc ? sc << 7 : 0x40u), scale = s16 | (s16 << 16);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t v = w >> (16 * h), sel = v & 0x7777u;
+    const uint32_t top = __byte_perm(0x3f3f3f00u, 0x40404040u, sel), low = __byte_perm(0xc0800000u, 0xc0804000u, sel);
+    uint32_t a = __byte_perm(low, top, 0x5140), b = __byte_perm(low, top, 0x7362);
+    a |= ((v << 12) & 0x8000u) | ((v << 24) & 0x80000000u);
+    b |= ((v << 4) & 0x8000u) | ((v << 16) & 0x80000000u);
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(o[2 * h]) : "r"(a), "r"(scale));
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(o[2 * h + 1]) : "r"(b), "r"(scale));
   }
 }
 
 template <typename T>
-__global__ void __launch_bounds__(256) mx_dequantize_kernel(const MxView q, T* __restrict__ out, long long ld) {
-  const int lane = threadIdx.x & 31;
-  const long long units = q.rows * q.col_tiles;
-  for (long long u = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); u < units; u += (long long)gridDim.x * 8) {
-    const long long r = u / q.col_tiles, ct = u - r * q.col_tiles, c = ct * 256 + lane * 8;
-    if (c >= q.cols) continue;
-    const uint32_t w = *reinterpret_cast<const uint32_t*>(q.codes + r * q.pitch + c / 2);
-    const int rr = (int)(r & 127);
-    const float s = scale_value(q.scales[((r >> 7) * q.col_tiles + ct) * 1024 + (lane >> 4) * 512 + (rr & 31) * 16 +
-                                         (rr >> 5) * 4 + ((lane >> 2) & 3)]);
-    float f[8];
+__global__ void __launch_bounds__(256) mx_dequantize_kernel(const MxView q, T* __restrict__ out, long long ld, int pass) {
+  const int lane = threadIdx.x & 31, rows = (int)q.rows;
+  const WarpPlace at = warp_place(q, pass);
+  const int ct = at.ct;
+  const long long c = (long long)ct * 256 + lane * 8;
+  if (c < q.cols) {
+    const bool full = c + 8 <= q.cols;
+    for (int r0 = at.row; r0 < rows; r0 += ROWS_AT_ONCE * pass) {
+      uint32_t w[ROWS_AT_ONCE], sc[ROWS_AT_ONCE];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float2 t = values2((w >> (8 * j)) & 255u);
-      f[2 * j] = t.x * s;
-      f[2 * j + 1] = t.y * s;
-    }
-    T* o = out + r * ld + c;
-    if (c + 8 <= q.cols && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
-      if (sizeof(T) == 4) {
-        *reinterpret_cast<float4*>(o) = make_float4(f[0], f[1], f[2], f[3]);
-        *(reinterpret_cast<float4*>(o) + 1) = make_float4(f[4], f[5], f[6], f[7]);
-      } else {
-        uint32_t p[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const __nv_bfloat162 t = __floats2bfloat162_rn(f[2 * j], f[2 * j + 1]);
-          p[j] = *reinterpret_cast<const uint32_t*>(&t);
-        }
-        *reinterpret_cast<uint4*>(o) = make_uint4(p[0], p[1], p[2], p[3]);
+      for (int u = 0; u < ROWS_AT_ONCE; ++u) {
+        const int r = r0 + u * pass < rows ? r0 + u * pass : r0;
+        w[u] = *reinterpret_cast<const uint32_t*>(q.codes + r * q.pitch + c / 2);
+        sc[u] = q.scales[scale_word(q, r, ct, lane >> 4) + ((lane >> 2) & 3)];
       }
-    } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (c + j < q.cols) o[j] = (T)f[j];
+      for (int u = 0; u < ROWS_AT_ONCE; ++u) {
+        const int r = r0 + u * pass;
+        if (r >= rows) break;
+        T* o = out + r * ld + c;
+        const bool fast = full && (reinterpret_cast<uintptr_t>(o) & 15) == 0;
+        if (sizeof(T) == 2) {
+          uint32_t v[4];
+          values8(w[u], sc[u], v);
+          if (fast) {
+            *reinterpret_cast<uint4*>(o) = make_uint4(v[0], v[1], v[2], v[3]);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (c + j < q.cols) reinterpret_cast<unsigned short*>(o)[j] = (unsigned short)(v[j >> 1] >> (16 * (j & 1)));
+          }
+        } else {
+          const float s = scale_value(sc[u]);
+          float f[8];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float2 t = values2((w[u] >> (8 * j)) & 255u);
+            f[2 * j] = t.x * s;
+            f[2 * j + 1] = t.y * s;
+          }
+          if (fast) {
+            reinterpret_cast<float4*>(o)[0] = make_float4(f[0], f[1], f[2], f[3]);
+            reinterpret_cast<float4*>(o)[1] = make_float4(f[4], f[5], f[6], f[7]);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (c + j < q.cols) o[j] = (T)f[j];
+          }
+        }
+      }
     }
   }
 }
@@ -576,6 +638,12 @@ cudaError_t launch_shape(const MxGemm& p, int split, long long ctas, cudaStream_
 
 }  // namespace
 
+// Rows that the row-wise kernels take in one pass: as many as fill the machine with warps.
+static int rows_per_pass(long long rows, long long col_tiles) {
+  const long long fill = 148 * 8 * 8 / col_tiles;
+  return (int)(fill < 1 ? 1 : fill < rows ? fill : rows);
+}
+
 cudaError_t mx_quantize(const void* x, int bf16, long long ld, int transpose, const MxView& q, cudaStream_t st) {
   if (transpose) {
     const dim3 grid((unsigned)((q.rows + 127) / 128 * 2 * q.col_tiles));
@@ -584,23 +652,23 @@ cudaError_t mx_quantize(const void* x, int bf16, long long ld, int transpose, co
     else
       mx_quantize_t_kernel<<<grid, 256, 0, st>>>(static_cast<const float*>(x), ld, q);
   } else {
-    const long long want = ((q.rows + 127) / 128 * 128 * q.col_tiles + 7) / 8;
-    const int blocks = (int)(want < 148 * 16 ? want : 148 * 16);
+    const int pass = rows_per_pass((q.rows + 127) / 128 * 128, q.col_tiles);
+    const unsigned blocks = (unsigned)((pass * q.col_tiles + 7) / 8);
     if (bf16)
-      mx_quantize_kernel<<<blocks, 256, 0, st>>>(static_cast<const __nv_bfloat16*>(x), ld, q);
+      mx_quantize_kernel<<<blocks, 256, 0, st>>>(static_cast<const __nv_bfloat16*>(x), ld, q, pass);
     else
-      mx_quantize_kernel<<<blocks, 256, 0, st>>>(static_cast<const float*>(x), ld, q);
+      mx_quantize_kernel<<<blocks, 256, 0, st>>>(static_cast<const float*>(x), ld, q, pass);
   }
   return cudaGetLastError();
 }
 
 cudaError_t mx_dequantize(const MxView& q, void* out, int bf16, long long ld, cudaStream_t st) {
-  const long long want = (q.rows * q.col_tiles + 7) / 8;
-  const int blocks = (int)(want < 148 * 16 ? want : 148 * 16);
+  const int pass = rows_per_pass(q.rows, q.col_tiles);
+  const unsigned blocks = (unsigned)((pass * q.col_tiles + 7) / 8);
   if (bf16)
-    mx_dequantize_kernel<<<blocks, 256, 0, st>>>(q, static_cast<__nv_bfloat16*>(out), ld);
+    mx_dequantize_kernel<<<blocks, 256, 0, st>>>(q, static_cast<__nv_bfloat16*>(out), ld, pass);
   else
-    mx_dequantize_kernel<<<blocks, 256, 0, st>>>(q, static_cast<float*>(out), ld);
+    mx_dequantize_kernel<<<blocks, 256, 0, st>>>(q, static_cast<float*>(out), ld, pass);
   return cudaGetLastError();
 }
 
