@@ -5,6 +5,7 @@ library's CUDA kernels.  `load()` fails loudly when the shared library is
 missing or cannot be loaded: there is no fallback implementation.
 """
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -335,6 +336,8 @@ def innovation_norms_noalloc(fresh, stale, lhs_out, stream=None):
 # ---------------------------------------------------------------------------
 PRECISIONS = {"full": 0, "half": 1}
 MUON_COEF = (3.4445, -4.7750, 2.0315)
+_NO_WORK = 256       # a work area of this size is asked for, but not used (narrow matrices stay on chip)
+_unused_work = {}    # device index -> one such area, shared by every call
 _status_words = {}   # device index -> an int32 tensor that a kernel whose bounded wait gave up makes non-zero
 
 
@@ -443,9 +446,10 @@ def _steps(steps, coef, eps, precision, narrow):
     return PRECISIONS[precision], int(steps), array, float(eps)
 
 
-def _work_bytes(lib, batch, rows, cols):
+@functools.lru_cache(maxsize=256)
+def _work_bytes(batch, rows, cols):
     n = C.c_size_t()
-    st = lib.gcada_orthogonalize_work(batch, rows, cols, C.byref(n))
+    st = load().gcada_orthogonalize_work(batch, rows, cols, C.byref(n))
     if st != OK:
         raise GCadaError(st, "matrix sizes out of range")
     return n.value
@@ -453,7 +457,13 @@ def _work_bytes(lib, batch, rows, cols):
 
 def _ns_work(run, batch, rows, cols, work):
     if work is None:
-        work = run.fresh(max(1, _work_bytes(run.lib, batch, rows, cols)), dtype=run.torch.uint8)
+        need = _work_bytes(batch, rows, cols)
+        if need > _NO_WORK:
+            work = run.fresh(need, dtype=run.torch.uint8)
+        else:
+            work = _unused_work.get(run.index)
+            if work is None:
+                work = _unused_work[run.index] = run.fresh(_NO_WORK, dtype=run.torch.uint8)
     elif not work.is_contiguous():
         raise ValueError("work must be contiguous")
     return work, work.data_ptr(), work.numel() * work.element_size()
@@ -468,7 +478,7 @@ def orthogonalize(g, out=None, steps=5, coef=MUON_COEF, eps=1e-7, precision=None
     run = _Launch(g, (out, work), stream)
     shape = g.shape
     if out is None:
-        out = run.fresh(*shape, dtype=g.dtype)
+        out = run.torch.empty_like(g) if run.other is None and g.is_contiguous() else run.fresh(*shape, dtype=g.dtype)
     elif out.shape != shape or out.dtype != g.dtype:
         raise ValueError("out must have g's shape and type")
     ld_o = _matrix(out, "out", (2, 3))
@@ -485,7 +495,7 @@ def orthogonalize(g, out=None, steps=5, coef=MUON_COEF, eps=1e-7, precision=None
 def orthogonalize_work(g):
     """Bytes of the work area that orthogonalize(g) or muon_update(w=g) needs."""
     rows, cols = g.shape[-2:]
-    return _work_bytes(load(), g.shape[0] if g.dim() == 3 else 1, rows, cols)
+    return _work_bytes(g.shape[0] if g.dim() == 3 else 1, rows, cols)
 
 
 def muon_update(w, m, g, lr, beta=0.95, nesterov=True, weight_decay=0.0, scale=None, steps=5, coef=MUON_COEF,
@@ -511,9 +521,10 @@ def muon_update(w, m, g, lr, beta=0.95, nesterov=True, weight_decay=0.0, scale=N
               size, run.status()), (w, m, g, work))
 
 
+@functools.lru_cache(maxsize=256)
 def _mx_bytes(rows, cols):
     n, s = C.c_size_t(), C.c_size_t()
-    st = (_lib or load()).gcada_mx_size(rows, cols, C.byref(n), C.byref(s))
+    st = load().gcada_mx_size(rows, cols, C.byref(n), C.byref(s))
     if st != OK:
         raise GCadaError(st, "matrix sizes out of range")
     return n.value, s.value
@@ -524,25 +535,46 @@ class MxMatrix:
     CUDA tensors of the sizes that gcada_mx_size gives, any shape, contiguous."""
 
     def __init__(self, rows, cols, codes, scales):
-        self.rows, self.cols, self.codes, self.scales = int(rows), int(cols), codes, scales
+        self.rows, self.cols = int(rows), int(cols)
         for t, want, name in zip((codes, scales), _mx_bytes(self.rows, self.cols), ("codes", "scales")):
             if not t.is_cuda or str(t.dtype) != "torch.uint8" or not t.is_contiguous() or t.numel() != want:
                 raise ValueError("%s of a %d x %d matrix must be a contiguous CUDA tensor of %d bytes"
                                  % (name, self.rows, self.cols, want))
         if codes.device != scales.device:
             raise ValueError("codes and scales on different devices")
+        self._parts = codes, scales
+        self._where = codes.data_ptr(), scales.data_ptr()
+
+    @classmethod
+    def _fresh(cls, run, rows, cols):
+        """One allocation for both arrays (a row of codes is a multiple of 16 bytes, so the scales are aligned)."""
+        self = cls.__new__(cls)
+        self.rows, self.cols = rows, cols
+        n, s = _mx_bytes(rows, cols)
+        both = run.fresh(n + s, dtype=run.torch.uint8)
+        self._parts, at = (both,), both.data_ptr()
+        self._where = at, at + n
+        return self
+
+    def _part(self, i):
+        if len(self._parts) == 1:
+            self._parts = self._parts[0].split(_mx_bytes(self.rows, self.cols))
+        return self._parts[i]
+
+    codes = property(lambda self: self._part(0), doc="the elements, two to a byte")
+    scales = property(lambda self: self._part(1), doc="the blocks' scales")
 
     def dequantize(self, dtype=None, out=None, stream=None):
         """The values as a float32 (default) or bfloat16 tensor.  See gcada_mx_dequantize."""
-        run = _Launch(self.codes, (out,), stream)
+        run = _Launch(self._parts[0], (out,), stream)
         if out is None:
             out = run.fresh(self.rows, self.cols, dtype=dtype or run.torch.float32)
         elif tuple(out.shape) != (self.rows, self.cols) or (dtype is not None and out.dtype != dtype):
             raise ValueError("out must be a %d x %d matrix of the type asked for" % (self.rows, self.cols))
         ld = _matrix(out, "out")
         run.call(run.lib.gcada_mx_dequantize,
-                 (self.codes.data_ptr(), self.scales.data_ptr(), self.rows, self.cols, out.data_ptr(),
-                  _compute_type(out, "out"), ld), (self.codes, self.scales, out))
+                 (*self._where, self.rows, self.cols, out.data_ptr(), _compute_type(out, "out"), ld),
+                 (*self._parts, out))
         return out
 
 
@@ -552,17 +584,13 @@ def mx_quantize(x, transpose=False, out=None, stream=None):
     kind, ld = _compute_type(x, "x"), _matrix(x, "x")
     rows, cols = x.shape
     shape = (cols, rows) if transpose else (rows, cols)
-    run = _Launch(x, () if out is None else (out.codes,), stream)
+    run = _Launch(x, () if out is None else out._parts, stream)
     if out is None:
-        n, s = _mx_bytes(*shape)
-        out = MxMatrix.__new__(MxMatrix)
-        out.rows, out.cols = shape
-        out.codes, out.scales = run.fresh(n, dtype=run.torch.uint8), run.fresh(s, dtype=run.torch.uint8)
+        out = MxMatrix._fresh(run, *shape)
     elif (out.rows, out.cols) != shape:
         raise ValueError("out must be %d x %d" % shape)
     run.call(run.lib.gcada_mx_quantize,
-             (x.data_ptr(), kind, rows, cols, ld, 1 if transpose else 0, out.codes.data_ptr(), out.scales.data_ptr()),
-             (x, out.codes, out.scales))
+             (x.data_ptr(), kind, rows, cols, ld, 1 if transpose else 0, *out._where), (x, *out._parts))
     return out
 
 
@@ -571,7 +599,7 @@ def mx_gemm(a, b, out=None, dtype=None, alpha=1.0, beta=0.0, bias=None, stream=N
     tensor.  See gcada_mx_gemm.  `bias`: float32, n values."""
     if a.cols != b.cols:
         raise ValueError("a has %d columns and b %d" % (a.cols, b.cols))
-    run = _Launch(a.codes, (b.codes, out, bias), stream)
+    run = _Launch(a._parts[0], (b._parts[0], out, bias), stream)
     if out is None:
         if beta != 0:
             raise ValueError("beta needs out")
@@ -582,10 +610,9 @@ def mx_gemm(a, b, out=None, dtype=None, alpha=1.0, beta=0.0, bias=None, stream=N
         raise ValueError("bias must hold %d contiguous float32 values" % b.rows)
     ld = _matrix(out, "out")
     run.call(run.lib.gcada_mx_gemm,
-             (a.codes.data_ptr(), a.scales.data_ptr(), a.rows, b.codes.data_ptr(), b.scales.data_ptr(), b.rows, a.cols,
-              out.data_ptr(), _compute_type(out, "out"), ld, float(alpha), float(beta),
-              None if bias is None else bias.data_ptr(), run.status()),
-             (a.codes, a.scales, b.codes, b.scales, out, bias))
+             (*a._where, a.rows, *b._where, b.rows, a.cols, out.data_ptr(), _compute_type(out, "out"), ld, float(alpha),
+              float(beta), None if bias is None else bias.data_ptr(), run.status()),
+             (*a._parts, *b._parts, out, bias))
     return out
 
 
