@@ -37,8 +37,6 @@ constexpr int STAGES = 4;                              // even: a stage of hi pa
 constexpr int EPI_WARPS = 16;                          // four to a quadrant of tensor memory's lanes
 constexpr int THREADS = 64 + 32 * EPI_WARPS;
 constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + EPI_WARPS * 4096 + 1024;
-constexpr int CHUNK = 4;                               // FULL: stage pairs summed in tensor memory before the sum
-                                                       // moves to registers
 constexpr float SCALE = 1024.f;                        // stored value = SCALE * matrix element
 constexpr float INV_SCALE = 1.f / 1024.f;
 constexpr int NORM_BLOCKS = 1184;                      // partial sums of a matrix's squared norm
@@ -59,6 +57,7 @@ struct NsGemm {
   int a_sym, b_sym;      // so is the operand: a block below the diagonal is read as the transpose of its mirror image
   int sym_log;           // 7 or 8 (8 wherever a pair of CTAs takes part)
   int split;             // CTAs of a cluster that share a tile's K range
+  int chunk;             // FULL: K blocks summed in tensor memory before the sum moves to registers
   float c_src, c_acc;    // value = c_src * src + c_acc * accumulator, times powers of rho
   float diag;            // symmetric results: added on the diagonal (see ns_run on the shifted form)
   float c_src_shift;     // PROD_APPLY / PROD_LAST in the shifted form: added to c_src
@@ -276,7 +275,7 @@ __device__ __forceinline__ void finish_piece(const NsGemm& a, const CUtensorMap*
 //   else: a CTA has its own 128 x 128 tile and, when there are fewer tiles than SMs, shares its K range with the
 //         other CTAs of its cluster: each leaves its partial tile in shared memory and adds up (in rank order) the
 //         columns that fall to it.
-// FULL: stages alternate between hi and lo parts, three products for each pair; the sum of CHUNK pairs moves to
+// FULL: stages alternate between hi and lo parts, three products for each pair; the sum of `chunk` pairs moves to
 // registers, because the tensor cores cut (not round) each partial sum.
 template <bool PAIR, bool FULL>
 __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_constant__ CUtensorMap tmA,
@@ -303,7 +302,7 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
   const int kb0 = PAIR ? 0 : (int)((long long)kb_all * rank / csize);
   const int kb1 = PAIR ? kb_all : (int)((long long)kb_all * (rank + 1) / csize);
   const int nkb = kb1 - kb0;
-  const int chunks = FULL ? (nkb + CHUNK - 1) / CHUNK : 1;
+  const int chunks = FULL ? (nkb + a.chunk - 1) / a.chunk : 1;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {
@@ -385,9 +384,9 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
           if (!ok) break;
           tc_fence_after();
           const uint32_t d = tmem_base + (uint32_t)(slot * TILE);
-          const int n = FULL ? (c == chunks - 1 ? nkb - c * CHUNK : CHUNK) : nkb;
+          const int n = FULL ? (c == chunks - 1 ? nkb - c * a.chunk : a.chunk) : nkb;
           for (int kb = 0; kb < n && ok; ++kb) {
-            const int kblk = (kb0 + c * CHUNK + kb) * BK >> a.sym_log;
+            const int kblk = (kb0 + (FULL ? c * a.chunk : 0) + kb) * BK >> a.sym_log;
             const bool mnA = a.a_mn || (a.a_sym && kblk < blkA), mnB = a.b_mn || (a.b_sym && kblk < blkB);
             const uint32_t idesc = IDESC | (mnA ? 1u << 15 : 0u) | (mnB ? 1u << 16 : 0u);
             const uint64_t ka = mnA ? 128u : 2u, kk_b = mnB ? 128u : 2u;  // descriptor step of 16 K values
@@ -799,6 +798,11 @@ cudaError_t launch_ns_gemm(const CUtensorMap& ta, const CUtensorMap& tb, NsGemm 
   const long long tiles =
       (long long)tile_count((a.M + t - 1) / t, (a.N + t - 1) / t, a.sym, s.pair ? 0 : a.sym_log - 7) * a.batch;
   a.split = s.split;
+  // The tensor cores cut each of a chunk's partial sums, an error that grows with their number and, like fp32's own
+  // rounding, weighs less in longer sums.  Error of the result, time, with 4 / 2 / 1 blocks a chunk (fp32 arithmetic
+  // 1.5e-6, 2.4e-6, 2.6e-6): 200 x 784 3.5e-6 2.2e-6 1.4e-6, 140 143 147 us; 1024 x 1024 2.6e-6 1.2e-6 0.6e-6,
+  // 210 214 225 us; 4096 x 4096 1.2e-6 0.7e-6 0.5e-6, 4.0 4.4 6.0 ms.
+  a.chunk = a.K <= 512 ? 1 : a.K <= 2048 ? 2 : 4;
   const long long room = s.pair ? sms / 2 : sms, want = tiles * (s.pair ? 1 : a.split);
   const int ctas = (int)(want < room ? want : room) * (s.pair ? 2 : 1);
   if (s.pair) return full ? launch_shape<true, true>(ta, tb, a, ctas, st) : launch_shape<true, false>(ta, tb, a, ctas, st);
