@@ -87,6 +87,16 @@ typedef struct {
                                   gcada_get_kernel_times); may be switched at any time (default 0) */
 
 /* (key 6 is not used) */
+#define GCADA_OPT_UPLOAD 8     /* bf16 MLP: form of the kept uploads.  GCADA_UPLOAD_FULL (default): the bf16 factors of
+                                  every layer's weight gradient as computed.  GCADA_UPLOAD_MXFP4: the same factors in
+                                  microscaled 4-bit floating point (blocks of 32 rows of the minibatch; 4.25 bits a
+                                  value instead of 16), so a weight matrix's share of the aggregate of Eq. (3) is the
+                                  sum over groups of the products of the QUANTISED factors of their last uploads, formed
+                                  anew every iteration.  The selection test and the biases' gradients are not
+                                  quantised.  Without GCADA_OPT_KEEP_STALE, GCADA_DBG_GLAST (and _FRESH) then return what
+                                  was uploaded, i.e. the products of the quantised factors */
+#define GCADA_UPLOAD_FULL 0
+#define GCADA_UPLOAD_MXFP4 1
 #define GCADA_OPT_PERSISTENT 7     /* 1 (default) = logistic / quadratic models with d <= 256, at most 64 groups and
                                       1024 workers run free-running steps of the default rule as ONE launch of a
                                       single thread-block cluster per gcada_step call, whatever n_iters is (the
@@ -180,6 +190,20 @@ gcada_status gcada_set_lag_weights(gcada_ctx *ctx, const double *c_d, int D);
 #define GCADA_SCHEDULE_POLY 1
 #define GCADA_SCHEDULE_STEP 2
 gcada_status gcada_set_step_schedule(gcada_ctx *ctx, int kind, double a, double b);
+
+/* Server update rule of an MLP (set before the first step, GCADA_ESTATE afterwards).
+ * GCADA_SERVER_AMSGRAD  Eq. (8a)-(8c) for every parameter (default; the other arguments are ignored)
+ * GCADA_SERVER_MUON     every weight matrix W with the aggregate's block A of it:
+ *     H <- beta1 H + (1 - beta1) A   (Eq. 8a),   U = nesterov ? beta1 H + (1 - beta1) A : H,
+ *     W <- (1 - alpha^k weight_decay) W - alpha^k scale sqrt(max(1, rows / cols)) O,
+ *   O = U orthogonalised by `steps` Newton-Schulz steps (gcada_orthogonalize with its default coefficients and eps
+ *   1e-7; GCADA_PRECISION_FULL for the fp32 MLP, _HALF for the bf16 one); the biases keep Eq. (8a)-(8c).  The step
+ *   norms of Eq. (9) are those of the whole parameter vector, whatever the rule.  GCADA_EINVAL for logistic / quadratic
+ *   models and unless weight_decay >= 0, scale > 0, 1 <= steps <= 100.  Like options, the rule is not part of a
+ *   checkpoint. */
+#define GCADA_SERVER_AMSGRAD 0
+#define GCADA_SERVER_MUON 1
+gcada_status gcada_set_server_rule(gcada_ctx *ctx, int rule, double weight_decay, double scale, int nesterov, int steps);
 
 gcada_status gcada_set_option(gcada_ctx *ctx, int key, double value);
 

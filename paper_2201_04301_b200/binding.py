@@ -18,13 +18,15 @@ OK, EINVAL, ENOMEM, ECUDA, ESTATE, ETIMEOUT = range(6)
 MODEL_LOGISTIC, MODEL_MLP, MODEL_QUADRATIC = 0, 1, 2
 COMPUTE_FP32, COMPUTE_BF16 = 0, 1
 (OPT_RULE, OPT_REDUCTION, OPT_HISTORY, OPT_KEEP_STALE, OPT_GRAPH, OPT_TIMING, _OPT_UNUSED,
- OPT_PERSISTENT) = range(8)
+ OPT_PERSISTENT, OPT_UPLOAD) = range(9)
+UPLOAD_FULL, UPLOAD_MXFP4 = 0, 1
 (DBG_FRESH, DBG_STALE, DBG_LHS, DBG_RHS, DBG_TAU, DBG_AGG, DBG_H, DBG_VHAT, DBG_TGROUP, DBG_GLAST,
  DBG_SRING) = range(11)
 MODEL_KINDS = {"logistic": MODEL_LOGISTIC, "mlp": MODEL_MLP, "quadratic": MODEL_QUADRATIC}
 COMPUTE_KINDS = {"fp32": COMPUTE_FP32, "bf16": COMPUTE_BF16}
 DELAY_LAWS = {"exp": 0, "pareto": 1, "uniform": 2}
 SCHEDULES = {"const": 0, "poly": 1, "step": 2}
+SERVER_RULES = {"amsgrad": 0, "muon": 1}
 
 
 class Model(C.Structure):
@@ -51,6 +53,7 @@ SIGNATURES = {
     "gcada_set_delay_law": (C.c_int, [_VP, C.c_int]),
     "gcada_set_lag_weights": (C.c_int, [_VP, C.POINTER(C.c_double), C.c_int]),
     "gcada_set_step_schedule": (C.c_int, [_VP, C.c_int, C.c_double, C.c_double]),
+    "gcada_set_server_rule": (C.c_int, [_VP, C.c_int, C.c_double, C.c_double, C.c_int, C.c_int]),
     "gcada_set_smoothness": (C.c_int, [_VP, C.POINTER(C.c_double), C.c_int]),
     "gcada_step": (C.c_int, [_VP, C.c_int]),
     "gcada_step_forced": (C.c_int, [_VP, C.c_int, _VP]),
@@ -191,6 +194,11 @@ class GCada:
 
     def set_step_schedule(self, kind, a=1.0, b=0.0):
         self._ck(self.lib.gcada_set_step_schedule(self.h, SCHEDULES.get(kind, kind), float(a), float(b)))
+
+    def set_server_rule(self, rule, weight_decay=0.0, scale=1.0, nesterov=True, steps=5):
+        """`rule`: "amsgrad" (Eq. 8) or "muon" (MLPs: orthogonalised momentum for the weight matrices)."""
+        self._ck(self.lib.gcada_set_server_rule(self.h, SERVER_RULES.get(rule, rule), float(weight_decay), float(scale),
+                                                int(bool(nesterov)), int(steps)))
 
     def set_smoothness(self, L):
         a = (C.c_double * len(L))(*[float(v) for v in L])
@@ -616,7 +624,8 @@ def mx_gemm(a, b, out=None, dtype=None, alpha=1.0, beta=0.0, bias=None, stream=N
     return out
 
 
-def from_workload(w, stream=None, options=None, smoothness=None, c_d=None, schedule=None, delay_law=None):
+def from_workload(w, stream=None, options=None, smoothness=None, c_d=None, schedule=None, delay_law=None,
+                  server_rule=None):
     """Context for a dict made by workloads.make_workload (tensors on CUDA)."""
     g = GCada(w["kind"], w["dims"], w["M"], w["M_G"], w["D"], w["c"], w["alpha"], w["beta1"], w["beta2"],
               w["eps"], compute=w["compute"], stream=stream)
@@ -632,6 +641,8 @@ def from_workload(w, stream=None, options=None, smoothness=None, c_d=None, sched
         g.set_step_schedule(*schedule)
     if delay_law is not None:
         g.set_delay_law(delay_law)
+    if server_rule is not None:
+        g.set_server_rule(**server_rule)
     g.set_data(w["X"], w["y"], w["batch"], ld=w["ld"])
     g.set_theta(w["theta0"])
     return g

@@ -14,7 +14,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libgcada.so")
 DEBUG_LIB = os.path.join(HERE, "libgcada_dbg.so")
 SOURCES = ["api.cu", "grad_linear.cu", "tail.cu", "mlp.cu", "mlp_bf16.cu", "noalloc.cu", "eval.cu", "linear_cluster.cu",
-           "muon.cu", "muon_cluster.cu", "mx.cu", "ops.cu"]
+           "muon.cu", "muon_cluster.cu", "mx.cu", "ops.cu", "server.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC,-Wall,-Wno-unused-function", "--expt-relaxed-constexpr"]
 

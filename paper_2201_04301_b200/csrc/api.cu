@@ -13,6 +13,7 @@
 #include "common.cuh"
 #include "launch.h"
 #include "mlp.h"
+#include "server.h"
 
 using namespace gcada;
 
@@ -59,6 +60,9 @@ struct gcada_ctx {
   LinearPlan lin{};
   TailPlan tail{};
   MlpPlan mlp{};
+  int server_rule = GCADA_SERVER_AMSGRAD;
+  int upload = GCADA_UPLOAD_FULL;
+  MuonPlan muon{};
   unsigned char* forced_dev = nullptr;
   size_t forced_cap = 0;
   void* stage_x = nullptr;
@@ -296,6 +300,7 @@ gcada_status make_plans(gcada_ctx* ctx) {
     const char* why = "";
     std::vector<void*> bufs;
     ctx->mlp.inspect = ctx->keep_stale;
+    ctx->mlp.upload_mx = ctx->upload == GCADA_UPLOAD_MXFP4;
     cudaError_t e = mlp_plan_create(ctx->dims, ctx->compute, ctx->G, ctx->B, ctx->D, ctx->p_pad, ctx->sm_count,
                                     ctx->stream, &ctx->mlp, &bufs, &why);
     for (void* q : bufs) ctx->owned.push_back(q);
@@ -306,6 +311,13 @@ gcada_status make_plans(gcada_ctx* ctx) {
       P.pm.maxseg = ctx->mlp.norm_parts;
       TRY(dev_alloc(ctx, &P.lhs_part, (size_t)ctx->G * ctx->mlp.norm_parts));
       P.lim.lhs_parts = (long long)ctx->G * ctx->mlp.norm_parts;
+    }
+    if (ctx->server_rule == GCADA_SERVER_MUON) {
+      TRY(dev_alloc(ctx, &ctx->muon.targets, (size_t)ctx->mlp.n_layers + 1));
+      unsigned char* work = nullptr;
+      TRY(dev_alloc(ctx, &work, muon_work_bytes(ctx->mlp)));
+      ctx->muon.work = work;
+      ctx->muon.beta = ctx->beta1;
     }
   }
   if (ctx->rule == 1) {
@@ -330,6 +342,17 @@ gcada_status make_plans(gcada_ctx* ctx) {
   return GCADA_OK;
 }
 
+// The server's update (the last kernels of an iteration); its launches are counted.
+gcada_status enqueue_update(gcada_ctx* ctx, const Params& P) {
+  int n = 1;
+  if (ctx->server_rule == GCADA_SERVER_MUON)
+    CK(launch_muon_update(P, ctx->mlp, ctx->muon, ctx->stream, &n));
+  else
+    CK(launch_update(P, ctx->tail, ctx->stream, false));
+  ctx->launches += (unsigned long long)n;
+  return GCADA_OK;
+}
+
 gcada_status enqueue_iteration(gcada_ctx* ctx, const Params& P) {
   cudaEvent_t* ev = nullptr;
   if (ctx->timing && !ctx->capturing) {
@@ -350,16 +373,16 @@ gcada_status enqueue_iteration(gcada_ctx* ctx, const Params& P) {
       CK(launch_grad_linear(P, ctx->lin, ctx->kind == GCADA_MODEL_QUADRATIC, ctx->stream));
       CK(launch_select(P, ctx->tail, ctx->stream, 2));
       if (ev) CK(cudaEventRecord(ev[2], ctx->stream));
-      ctx->launches += 5;
+      ctx->launches += 4;
     } else {
       int n = 0, m = 0;
       CK(launch_grad_mlp(P, ctx->mlp, ctx->stream, &n));
       if (ev) CK(cudaEventRecord(ev[2], ctx->stream));
       CK(launch_grad_mlp_post(P, ctx->mlp, ctx->stream, &m));
-      ctx->launches += (unsigned long long)(3 + n + m);
+      ctx->launches += (unsigned long long)(2 + n + m);
     }
     if (ev) CK(cudaEventRecord(ev[3], ctx->stream));
-    CK(launch_update(P, ctx->tail, ctx->stream));
+    TRY(enqueue_update(ctx, P));
     if (ev) {
       CK(cudaEventRecord(ev[4], ctx->stream));
       ctx->timed += 1;
@@ -396,12 +419,12 @@ gcada_status enqueue_iteration(gcada_ctx* ctx, const Params& P) {
     ctx->launches += (unsigned long long)n;
   }
   if (ev) CK(cudaEventRecord(ev[3], ctx->stream));
-  CK(launch_update(P, ctx->tail, ctx->stream, false));
+  TRY(enqueue_update(ctx, P));
   if (ev) {
     CK(cudaEventRecord(ev[4], ctx->stream));
     ctx->timed += 1;
   }
-  ctx->launches += 2;
+  ctx->launches += 1;
   return GCADA_OK;
 }
 
@@ -444,8 +467,9 @@ __global__ void empty_kernel() {}
 
 int kernels_per_iteration(const gcada_ctx* ctx) {
   if (is_linear(ctx)) return ctx->P.skip_unselected ? 5 : 3 + (ctx->rule == 1 ? 1 : 0);
-  if (ctx->P.skip_unselected) return 3 + ctx->mlp.skip_launches + ctx->mlp.post_launches;
-  return 2 + ctx->mlp.launches_per_iter + ctx->mlp.post_launches + (ctx->rule == 1 ? 1 : 0);
+  const int update = ctx->server_rule == GCADA_SERVER_MUON ? muon_kernels(ctx->mlp, ctx->muon) : 1;
+  if (ctx->P.skip_unselected) return 2 + update + ctx->mlp.skip_launches + ctx->mlp.post_launches;
+  return 1 + update + ctx->mlp.launches_per_iter + ctx->mlp.post_launches + (ctx->rule == 1 ? 1 : 0);
 }
 
 gcada_status check_runnable(gcada_ctx* ctx, bool need_data) {
@@ -692,6 +716,26 @@ gcada_status gcada_set_step_schedule(gcada_ctx* ctx, int kind, double a, double 
   return GCADA_OK;
 }
 
+gcada_status gcada_set_server_rule(gcada_ctx* ctx, int rule, double weight_decay, double scale, int nesterov, int steps) {
+  if (!ctx) return GCADA_EINVAL;
+  if (rule != GCADA_SERVER_AMSGRAD && rule != GCADA_SERVER_MUON) return fail(ctx, GCADA_EINVAL, "unknown server rule %d", rule);
+  if (ctx->k_host > 0) return fail(ctx, GCADA_ESTATE, "the server rule is fixed once stepping has begun; call gcada_set_theta to restart");
+  if (rule == GCADA_SERVER_MUON) {
+    if (is_linear(ctx)) return fail(ctx, GCADA_EINVAL, "server rule Muon needs weight matrices: an MLP");
+    if (!(weight_decay >= 0 && weight_decay <= 1e30) || !(scale > 0 && scale <= 1e30) || steps < 1 || steps > 100)
+      return fail(ctx, GCADA_EINVAL, "server rule Muon needs weight_decay >= 0, scale > 0 and 1 to 100 steps");
+    ctx->muon = MuonPlan{};
+    ctx->muon.weight_decay = weight_decay;
+    ctx->muon.scale = scale;
+    ctx->muon.nesterov = nesterov != 0;
+    ctx->muon.steps = steps;
+  }
+  ctx->server_rule = rule;
+  ctx->ready = false;  // the work area is made with the plans
+  drop_graphs(ctx);
+  return GCADA_OK;
+}
+
 gcada_status gcada_set_option(gcada_ctx* ctx, int key, double value) {
   if (!ctx) return GCADA_EINVAL;
   if (key == GCADA_OPT_TIMING) {
@@ -716,6 +760,11 @@ gcada_status gcada_set_option(gcada_ctx* ctx, int key, double value) {
       break;
     case GCADA_OPT_KEEP_STALE:
       ctx->keep_stale = value != 0;
+      break;
+    case GCADA_OPT_UPLOAD:
+      if (value != GCADA_UPLOAD_FULL && value != GCADA_UPLOAD_MXFP4) return fail(ctx, GCADA_EINVAL, "upload must be 0 (full) or 1 (MXFP4)");
+      if (value == GCADA_UPLOAD_MXFP4 && !factored(ctx)) return fail(ctx, GCADA_EINVAL, "4-bit uploads need the bf16 MLP (the other models upload gradients, not factors)");
+      ctx->upload = (int)value;
       break;
     case GCADA_OPT_PERSISTENT:
       ctx->persistent = value != 0;

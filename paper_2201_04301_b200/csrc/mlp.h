@@ -19,6 +19,7 @@ struct MlpPlan {
   int compute = 0;            // 0 fp32, 1 bf16 operands
   int inspect = 0;            // set by the caller before the plan is created: both gradients of every group
                               // are kept (GCADA_OPT_KEEP_STALE); decides which partial sums of the norm exist
+  int upload_mx = 0;          // set by the caller too: the bf16 path keeps uploads as 4-bit factors (GCADA_OPT_UPLOAD)
   int G = 0, B = 0, D = 0;
   long long p_pad = 0;
   int dims[MLP_MAX_LAYERS + 1] = {0};

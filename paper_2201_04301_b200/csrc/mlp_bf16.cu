@@ -31,6 +31,7 @@
 
 #include <cuda_bf16.h>
 
+#include "mx.h"
 #include "tc.cuh"
 
 namespace gcada {
@@ -74,6 +75,9 @@ struct Bf16Impl {
   // differences between the two points, row-major [G*Bp][ld_l] (see bf16_gram_kernel)
   __nv_bfloat16* dE[MLP_MAX_LAYERS + 1] = {nullptr};  // dz_l(theta^k) - dz_l(stale), l = 1..L
   __nv_bfloat16* dF[MLP_MAX_LAYERS + 1] = {nullptr};  // a_l(theta^k) - a_l(stale),  l = 1..L-1
+  // 4-bit uploads (GCADA_OPT_UPLOAD): the transposed factors dz_l^T [n_l][G*Bp] and a_{l-1}^T [n_{l-1}][G*Bp] of every
+  // group's last upload, group g in columns g*Bp ..; the aggregate of layer l is the product of the two
+  MxView qe[MLP_MAX_LAYERS + 1] = {}, qa[MLP_MAX_LAYERS + 1] = {};
   int gram_part_base[MLP_MAX_LAYERS + 1] = {0};
   CUtensorMap tm_dE[MLP_MAX_LAYERS + 1], tm_dF[MLP_MAX_LAYERS + 1];
   int dw_part_base[MLP_MAX_LAYERS + 1] = {0}, bias_part_base[MLP_MAX_LAYERS + 1] = {0};
@@ -1517,6 +1521,19 @@ cudaError_t mlp_bf16_plan_create(MlpPlan* plan, cudaStream_t st, std::vector<voi
     im->dbp_blocks[l] = l < L ? im->Bp / BM : im->Bp / 32;
     A_(im->dbp[l], 2LL * G * im->dbp_blocks[l] * plan->dims[l], float);
   }
+  if (plan->upload_mx) {
+    for (int l = 1; l <= L; ++l) {
+      for (int side = 0; side < 2; ++side) {
+        MxView& v = side ? im->qa[l] : im->qe[l];
+        v.rows = plan->dims[side ? l - 1 : l];
+        v.cols = rows;
+        v.pitch = mx_pitch(rows);
+        v.col_tiles = mx_col_tiles(rows);
+        A_(v.codes, v.rows * v.pitch, unsigned char);
+        A_(v.scales, mx_scale_bytes(v.rows, v.cols), unsigned char);
+      }
+    }
+  }
 #undef A_
   // what an iteration reads from earlier ones: the bf16 copies of the last D+1 iterates and every group's last upload
   plan->state.clear();
@@ -1529,6 +1546,12 @@ cudaError_t mlp_bf16_plan_create(MlpPlan* plan, cudaStream_t st, std::vector<voi
     if (l < L) plan->state.emplace_back(im->act[l], sizeof(__nv_bfloat16) * (size_t)2 * rows * im->ld[l]);
   }
   plan->state.emplace_back(im->db, sizeof(float) * (size_t)2 * G * im->nbias);
+  for (int l = 1; l <= L && plan->upload_mx; ++l) {
+    for (const MxView* v : {&im->qe[l], &im->qa[l]}) {
+      plan->state.emplace_back(v->codes, (size_t)(v->rows * v->pitch));
+      plan->state.emplace_back(v->scales, (size_t)mx_scale_bytes(v->rows, v->cols));
+    }
+  }
   if (!encode_fn()) {
     *why = "cuTensorMapEncodeTiled is not available from this driver";
     return cudaSuccess;
@@ -1579,7 +1602,7 @@ cudaError_t mlp_bf16_plan_create(MlpPlan* plan, cudaStream_t st, std::vector<voi
   e = cudaFuncSetAttribute(bf16_gram_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, G_STAGES * G_STAGE_BYTES + 1024);
   if (e != cudaSuccess) return e;
   plan->launches_per_iter = 3 + 2 * L + 1 + L + 2 * (L - 1);
-  plan->post_launches = L + 1;
+  plan->post_launches = (plan->upload_mx ? 3 * L : L) + 1;
   plan->skip_launches = 2 + L + 1 + (L - 1) + 1;
   return cudaSuccess;
 }
@@ -1763,7 +1786,23 @@ cudaError_t mlp_bf16_launch_post(const Params& P, const MlpPlan& pl, cudaStream_
   const Bf16Impl* im = static_cast<const Bf16Impl*>(pl.bf16_impl);
   const int L = pl.n_layers, G = P.G, Bp = im->Bp;
   cudaError_t e;
-  for (int l = L; l >= 1; --l) {
+  for (int l = L; l >= 1 && pl.upload_mx; --l) {
+    // the selected groups' new factors (the buffers that the selection has just named) in 4 bits, then one product
+    const __nv_bfloat16* act = l == 1 ? im->xb : im->act[l - 1];
+    if ((e = mx_quantize_uploads(P, im->dz[l], im->ld[l], Bp, im->qe[l], st)) != cudaSuccess) return e;
+    if ((e = mx_quantize_uploads(P, act, im->ld[l - 1], Bp, im->qa[l], st)) != cudaSuccess) return e;
+    MxGemm g{};
+    g.a = im->qe[l];
+    g.b = im->qa[l];
+    g.d = P.agg_hi + pl.w_off[l];
+    g.ld = pl.dims[l - 1];
+    g.alpha = 1.f;
+    g.err = &P.st->err;
+    const char* why = "";
+    if ((e = mx_gemm(g, st, &why)) != cudaSuccess) return e;
+    *n_launches += 3;
+  }
+  for (int l = L; l >= 1 && !pl.upload_mx; --l) {
     GemmB a{};
     a.M = pl.dims[l];
     a.N = pl.dims[l - 1];
@@ -1788,7 +1827,8 @@ cudaError_t mlp_bf16_launch_post(const Params& P, const MlpPlan& pl, cudaStream_
 cudaError_t mlp_bf16_group_gradient(const Params& P, const MlpPlan& pl, int g, float* row, cudaStream_t st) {
   const Bf16Impl* im = static_cast<const Bf16Impl*>(pl.bf16_impl);
   for (int l = pl.n_layers; l >= 1; --l) {
-    cudaError_t e = launch_dw(P, pl, im, l, DW_ONE, st, g, row);
+    cudaError_t e = pl.upload_mx ? mx_upload_product(im->qe[l], im->qa[l], (long long)g * im->Bp, im->Bp, row + pl.w_off[l], st)
+                                 : launch_dw(P, pl, im, l, DW_ONE, st, g, row);
     if (e != cudaSuccess) return e;
   }
   bf16_bias_row_kernel<<<(im->nbias + 255) / 256, 256, 0, st>>>(P, bias_agg_args(pl, im), g, row);

@@ -70,9 +70,7 @@ struct NsGemm {
   long long ld_dst, dst_plane;
   int write_lo;
   int out;               // OUT_*
-  void* user;            // OUT_F32 ... : user's matrix
-  long long ld_user, user_stride;
-  float decay, step;     // OUT_UPDATE_*: w <- decay * w - step * value
+  NsSink user;           // OUT_F32 ... : user's matrix
   int* err;
 };
 
@@ -158,6 +156,8 @@ __device__ __forceinline__ void fetch_piece(const CUtensorMap* tm, unsigned char
   tma_load_3d(buf + PLANE_BYTES, tm, n, m, 2 * b + 1, bar);
 }
 
+__device__ __forceinline__ NsTarget target_of(const NsSink& s) { return s.at ? *s.at : s.to; }
+
 // A warp: f holds row m0 + lane, columns n .. n + PW - 1 of the products' sums.
 template <int PW>
 __device__ __forceinline__ void finish_piece(const NsGemm& a, const CUtensorMap* tmD, const Coef& k, unsigned char* buf, int lane,
@@ -221,45 +221,48 @@ __device__ __forceinline__ void finish_piece(const NsGemm& a, const CUtensorMap*
   constexpr int CH = PW / 4, RPP = 32 / CH;  // chunks of a row, rows of a pass
   const bool f32 = a.out == OUT_F32 || a.out == OUT_UPDATE_F32, upd = a.out == OUT_UPDATE_F32 || a.out == OUT_UPDATE_BF16;
   const int ch = lane % CH, col = n + 4 * ch;
+  const NsTarget to = target_of(a.user);
 #pragma unroll 1
   for (int r0 = 0; r0 < 32; r0 += RPP) {
     const int row = r0 + lane / CH, m = m0 + row;
     if (m >= a.M || col >= a.N) continue;
     const float4 v4 = *reinterpret_cast<const float4*>(buf + float_at<PW>(row, ch));
     float v[4] = {v4.x, v4.y, v4.z, v4.w};
-    const long long at = (long long)b * a.user_stride + (long long)m * a.ld_user + col;
+    const long long at = (long long)b * a.user.stride + (long long)m * a.user.ld + col;
     if (f32) {
-      float* o = static_cast<float*>(a.user) + at;
-      if (col + 4 <= a.N && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+      float* o = static_cast<float*>(to.o) + at;
+      const float* prev = static_cast<const float*>(to.prev) + at;
+      if (col + 4 <= a.N && ((reinterpret_cast<uintptr_t>(o) | (upd ? reinterpret_cast<uintptr_t>(prev) : 0)) & 15) == 0) {
         if (upd) {
-          const float4 w = *reinterpret_cast<const float4*>(o);
-          v[0] = a.decay * w.x - a.step * v[0];
-          v[1] = a.decay * w.y - a.step * v[1];
-          v[2] = a.decay * w.z - a.step * v[2];
-          v[3] = a.decay * w.w - a.step * v[3];
+          const float4 w = *reinterpret_cast<const float4*>(prev);
+          v[0] = to.decay * w.x - to.step * v[0];
+          v[1] = to.decay * w.y - to.step * v[1];
+          v[2] = to.decay * w.z - to.step * v[2];
+          v[3] = to.decay * w.w - to.step * v[3];
         }
         *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
       } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          if (col + j < a.N) o[j] = upd ? a.decay * o[j] - a.step * v[j] : v[j];
+          if (col + j < a.N) o[j] = upd ? to.decay * prev[j] - to.step * v[j] : v[j];
       }
     } else {
-      __nv_bfloat16* o = static_cast<__nv_bfloat16*>(a.user) + at;
-      if (col + 4 <= a.N && (reinterpret_cast<uintptr_t>(o) & 7) == 0) {
+      __nv_bfloat16* o = static_cast<__nv_bfloat16*>(to.o) + at;
+      const __nv_bfloat16* prev = static_cast<const __nv_bfloat16*>(to.prev) + at;
+      if (col + 4 <= a.N && ((reinterpret_cast<uintptr_t>(o) | (upd ? reinterpret_cast<uintptr_t>(prev) : 0)) & 7) == 0) {
         if (upd) {
-          const uint2 w = *reinterpret_cast<const uint2*>(o);
-          v[0] = a.decay * __uint_as_float(w.x << 16) - a.step * v[0];
-          v[1] = a.decay * __uint_as_float(w.x & 0xffff0000u) - a.step * v[1];
-          v[2] = a.decay * __uint_as_float(w.y << 16) - a.step * v[2];
-          v[3] = a.decay * __uint_as_float(w.y & 0xffff0000u) - a.step * v[3];
+          const uint2 w = *reinterpret_cast<const uint2*>(prev);
+          v[0] = to.decay * __uint_as_float(w.x << 16) - to.step * v[0];
+          v[1] = to.decay * __uint_as_float(w.x & 0xffff0000u) - to.step * v[1];
+          v[2] = to.decay * __uint_as_float(w.y << 16) - to.step * v[2];
+          v[3] = to.decay * __uint_as_float(w.y & 0xffff0000u) - to.step * v[3];
         }
         const __nv_bfloat162 x = __floats2bfloat162_rn(v[0], v[1]), y = __floats2bfloat162_rn(v[2], v[3]);
         *reinterpret_cast<uint2*>(o) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
       } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          if (col + j < a.N) o[j] = __float2bfloat16_rn(upd ? a.decay * __bfloat162float(o[j]) - a.step * v[j] : v[j]);
+          if (col + j < a.N) o[j] = __float2bfloat16_rn(upd ? to.decay * __bfloat162float(prev[j]) - to.step * v[j] : v[j]);
       }
     }
   }
@@ -674,14 +677,13 @@ __global__ void __launch_bounds__(256) ns_copy_kernel(const NsGemm a) {
     const int r = (int)(i / a.N), c = (int)(i - (long long)r * a.N);
     const __half* p = a.src + (long long)b * 2 * a.src_plane + (long long)r * a.ld_src + c;
     const float v = a.c_src * a.rho[(long long)b * (MAX_STEPS + 1)] * (__half2float(p[0]) + __half2float(p[a.src_plane]));
-    const long long o = (long long)b * a.user_stride + (long long)r * a.ld_user + c;
-    if (a.out == OUT_F32 || a.out == OUT_UPDATE_F32) {
-      float* w = static_cast<float*>(a.user) + o;
-      *w = a.out == OUT_F32 ? v : a.decay * *w - a.step * v;
-    } else {
-      __nv_bfloat16* w = static_cast<__nv_bfloat16*>(a.user) + o;
-      *w = __float2bfloat16_rn(a.out == OUT_BF16 ? v : a.decay * __bfloat162float(*w) - a.step * v);
-    }
+    const long long o = (long long)b * a.user.stride + (long long)r * a.user.ld + c;
+    const NsTarget to = target_of(a.user);
+    if (a.out == OUT_F32 || a.out == OUT_UPDATE_F32)
+      static_cast<float*>(to.o)[o] = a.out == OUT_F32 ? v : to.decay * static_cast<const float*>(to.prev)[o] - to.step * v;
+    else
+      static_cast<__nv_bfloat16*>(to.o)[o] = __float2bfloat16_rn(
+          a.out == OUT_BF16 ? v : to.decay * __bfloat162float(static_cast<const __nv_bfloat16*>(to.prev)[o]) - to.step * v);
   }
 }
 
@@ -811,6 +813,8 @@ cudaError_t launch_ns_gemm(const CUtensorMap& ta, const CUtensorMap& tb, NsGemm 
 
 }  // namespace
 
+int ns_launches(int rows, int cols, int steps) { return ns_fits_cluster(rows, cols) ? 1 : 2 + (steps ? 3 * steps : 1); }
+
 size_t ns_work_bytes(int batch, int rows, int cols) {
   return ns_fits_cluster(rows, cols) ? 256 : layout(batch, rows, cols).bytes;
 }
@@ -834,7 +838,7 @@ cudaError_t ns_run(const NsProblem& p, void* work, cudaStream_t st, const char**
   s.nesterov = p.nesterov;
   s.rows = p.rows;
   s.cols = p.cols;
-  const NsSink sink{p.o, p.ld_o, p.stride_o, p.o_bf16, p.w_update, (float)p.decay, (float)p.step};
+  const NsSink sink{{p.o, p.prev, (float)p.decay, (float)p.step}, p.ld_o, p.stride_o, p.o_bf16, p.w_update, p.at};
   if (ns_fits_cluster(p.rows, p.cols)) {
     const float coef[3] = {(float)p.coef[0], (float)p.coef[1], (float)p.coef[2]};
     if ((e = launch_ns_cluster(s, sink, p.batch, coef, p.steps, p.eps, st)) != cudaSuccess) *why = "kernel launch";
@@ -871,11 +875,7 @@ cudaError_t ns_run(const NsProblem& p, void* work, cudaStream_t st, const char**
   f.M = p.rows;
   f.N = p.cols;
   f.out = sink.update ? (sink.bf16 ? OUT_UPDATE_BF16 : OUT_UPDATE_F32) : (sink.bf16 ? OUT_BF16 : OUT_F32);
-  f.user = sink.o;
-  f.ld_user = sink.ld;
-  f.user_stride = sink.stride;
-  f.decay = sink.decay;
-  f.step = sink.step;
+  f.user = sink;
   f.ld_src = L.ld_x;
   f.src_plane = L.plane_x;
   f.err = p.err;

@@ -224,19 +224,18 @@ __global__ void __launch_bounds__(NC_THREADS, 1) ns_cluster_kernel(const NsSourc
     Y = t;
   }
 
+  const NsTarget to = o.at ? *o.at : o.to;
   for (int e = tid; e < count; e += threads) {
     const int major = n.tall ? n.r : kn, q = e / major, w = e - q * major;
     const int i = n.tall ? w : q, k = n.tall ? q : w;
     const long long row = n.tall ? k0 + k : i, col = n.tall ? i : k0 + k;
     const long long at = (long long)b * o.stride + row * o.ld + col;
     const float v = X[k * rp + i];
-    if (o.bf16) {
-      __nv_bfloat16* w16 = static_cast<__nv_bfloat16*>(o.o) + at;
-      *w16 = __float2bfloat16_rn(o.update ? o.decay * __bfloat162float(*w16) - o.step * v : v);
-    } else {
-      float* w32 = static_cast<float*>(o.o) + at;
-      *w32 = o.update ? o.decay * *w32 - o.step * v : v;
-    }
+    if (o.bf16)
+      static_cast<__nv_bfloat16*>(to.o)[at] = __float2bfloat16_rn(
+          o.update ? to.decay * __bfloat162float(static_cast<const __nv_bfloat16*>(to.prev)[at]) - to.step * v : v);
+    else
+      static_cast<float*>(to.o)[at] = o.update ? to.decay * static_cast<const float*>(to.prev)[at] - to.step * v : v;
   }
   if (n.csize > 1) cluster_sync();  // the others have read this CTA's last share
 }

@@ -260,6 +260,76 @@ __global__ void __launch_bounds__(256) mx_dequantize_kernel(const MxView q, T* _
   }
 }
 
+// Uploads: a CTA takes 64 columns x 128 rows of one selected group's factor (warp w: the block of 32 rows w, two
+// columns a lane), as mx_quantize_t_kernel does; a result row's 64 bytes and four scales are written together.
+__global__ void __launch_bounds__(128) mx_quantize_uploads_kernel(const Params P, const __nv_bfloat16* __restrict__ x, int ld,
+                                                                  int Bp, const MxView q) {
+  using T = Pair2<__nv_bfloat16>;
+  __shared__ __align__(16) uint4 codes_sm[64][5];
+  __shared__ uint32_t scale_sm[64];
+  if ((int)blockIdx.z >= P.sel_count[0]) return;
+  const int g = P.sel_list[blockIdx.z], lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  if (!GCADA_INDEX_OK(P.st, g, P.G, CHK_FACTOR)) return;
+  const int r0 = blockIdx.x * 64, r = r0 + 2 * lane, b0 = blockIdx.y * 128;
+  const long long k0 = (long long)g * Bp + b0;  // first column of the result
+  const __nv_bfloat16* p = x + (((long long)P.cur[g] * P.G + g) * Bp + b0 + w * 32) * ld + r;
+  uint32_t v[32];
+  if (r0 + 64 <= q.rows) {  // (rows are whole 128-byte lines: pairs are aligned)
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] = *reinterpret_cast<const uint32_t*>(p + (long long)j * ld);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+      v[j] = T::make(r < q.rows ? p[(long long)j * ld] : (__nv_bfloat16)0.f, r + 1 < q.rows ? p[(long long)j * ld + 1] : (__nv_bfloat16)0.f);
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) top = max(top, abs_bits(h ? T::hi(v[j]) : T::lo(v[j])));
+    const uint32_t sc = scale_code(__uint_as_float(top));
+    const float inv = inverse_scale(sc);
+    uint32_t c[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      float f[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] = (h ? T::hi(v[8 * t + j]) : T::lo(v[8 * t + j])) * inv;
+      c[t] = codes8(f);
+    }
+    codes_sm[2 * lane + h][w] = make_uint4(c[0], c[1], c[2], c[3]);
+    reinterpret_cast<unsigned char*>(&scale_sm[2 * lane + h])[w] = (unsigned char)sc;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 64 * 4; i += 128) {
+    const int rr = i >> 2;
+    if (r0 + rr < q.rows) *reinterpret_cast<uint4*>(q.codes + (r0 + rr) * q.pitch + k0 / 2 + (i & 3) * 16) = codes_sm[rr][i & 3];
+  }
+  if (threadIdx.x < 64)
+    *reinterpret_cast<uint32_t*>(q.scales + scale_word(q, r0 + threadIdx.x, (int)(k0 / 256), (int)(k0 / 128 % 2))) = scale_sm[threadIdx.x];
+}
+
+// One group's share of a product, for getters: a value a thread.
+__global__ void __launch_bounds__(256) mx_upload_product_kernel(const MxView a, const MxView b, long long k0, int K, float* out) {
+  const int n = blockIdx.x * 32 + (threadIdx.x & 31), m = blockIdx.y * 8 + (threadIdx.x >> 5);
+  if (m >= a.rows || n >= b.rows) return;
+  float sum = 0.f;
+  for (int k = 0; k < K; k += 32) {
+    const long long c = k0 + k;
+    const uint4 x = *reinterpret_cast<const uint4*>(a.codes + m * a.pitch + c / 2), y = *reinterpret_cast<const uint4*>(b.codes + n * b.pitch + c / 2);
+    const int ct = (int)(c / 256), half = (int)(c / 128 % 2), q = (int)(c / 32 % 4);
+    const float s = scale_value(a.scales[scale_word(a, m, ct, half) + q]) * scale_value(b.scales[scale_word(b, n, ct, half) + q]);
+    const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+    float t = 0.f;
+    for (int i = 0; i < 16; ++i) {
+      const float2 u = values2((xs[i >> 2] >> (8 * (i & 3))) & 255u), v = values2((ys[i >> 2] >> (8 * (i & 3))) & 255u);
+      t += u.x * v.x + u.y * v.y;
+    }
+    sum += s * t;
+  }
+  out[(long long)m * b.rows + n] = sum;
+}
+
 // ----------------------------------------------------------------- product
 // Warp 0 copies the operands' codes (128-byte rows of 256 elements, 128-byte swizzle) and scales into a ring of
 // stages, warp 1 copies a stage's scales into tensor memory and issues the block-scaled products (64 K values each),
@@ -702,6 +772,18 @@ cudaError_t mx_gemm(const MxGemm& p, cudaStream_t st, const char** why) {
   const long long t = bn == 128 ? t128 : t64, want = t * split, ctas = want < sms ? want : sms;
   if (bn == 128) return launch_shape<false, 128>(p, split, ctas, st, why);
   return launch_shape<false, 64>(p, split, ctas, st, why);
+}
+
+cudaError_t mx_quantize_uploads(const Params& P, const void* x_bf16, int ld, int Bp, const MxView& q, cudaStream_t st) {
+  const dim3 grid((unsigned)((q.rows + 127) / 128 * 2), (unsigned)(Bp / 128), (unsigned)P.G);
+  mx_quantize_uploads_kernel<<<grid, 128, 0, st>>>(P, static_cast<const __nv_bfloat16*>(x_bf16), ld, Bp, q);
+  return cudaGetLastError();
+}
+
+cudaError_t mx_upload_product(const MxView& a, const MxView& b, long long k0, int K, float* out, cudaStream_t st) {
+  const dim3 grid((unsigned)((b.rows + 31) / 32), (unsigned)((a.rows + 7) / 8));
+  mx_upload_product_kernel<<<grid, 256, 0, st>>>(a, b, k0, K, out);
+  return cudaGetLastError();
 }
 
 }  // namespace gcada

@@ -4,6 +4,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "common.cuh"
+
 namespace gcada {
 
 // A matrix in 4-bit form.  Codes: E2M1, two to a byte (the even column in the low half), rows of pitch bytes.
@@ -36,5 +38,12 @@ struct MxGemm {
   int* err;             // device error word, or null
 };
 cudaError_t mx_gemm(const MxGemm& p, cudaStream_t st, const char** why);
+
+// Uploads of the bf16 MLP: of every group selected this iteration the [Bp][ld] factor in entry cur[g] * G + g of `x`,
+// transposed, into columns g * Bp .. of q (Bp a multiple of 128).
+cudaError_t mx_quantize_uploads(const Params& P, const void* x_bf16, int ld, int Bp, const MxView& q, cudaStream_t st);
+// out[m][n] = sum over columns k0 .. k0 + K - 1 of a[m][k] b[n][k], out with rows of b.rows floats (getters; K a
+// multiple of 32).
+cudaError_t mx_upload_product(const MxView& a, const MxView& b, long long k0, int K, float* out, cudaStream_t st);
 
 }  // namespace gcada

@@ -126,6 +126,7 @@ gcada_status gcada_muon_update(void* w_dev, int w_type, float* m_dev, const void
   p.beta = beta;
   p.nesterov = nesterov != 0;
   p.o = w_dev;
+  p.prev = w_dev;
   p.ld_o = ld_w;
   p.o_bf16 = w_type == GCADA_COMPUTE_BF16;
   p.w_update = 1;
