@@ -74,24 +74,25 @@ struct NsGemm {
   int* err;
 };
 
-// Square tiles; of a symmetric result only those in the upper blocks of 2^g tiles (g = 0 or 1).
-__device__ __forceinline__ void tile_of(int u, int tiles_n, int sym, int g, int& mt, int& nt) {
+// Tiles of a result; of a symmetric one only those from the row's own block of 2^g row tiles on, a row tile being `r`
+// column tiles wide.
+__device__ __forceinline__ void tile_of(int u, int tiles_n, int sym, int g, int r, int& mt, int& nt) {
   if (!sym) {
     mt = u / tiles_n;
     nt = u - mt * tiles_n;
     return;
   }
   for (mt = 0;; ++mt) {
-    const int w = tiles_n - (mt >> g << g);
+    const int w = tiles_n - (mt >> g << g) * r;
     if (u < w) break;
     u -= w;
   }
-  nt = (mt >> g << g) + u;
+  nt = (mt >> g << g) * r + u;
 }
-__host__ __device__ inline int tile_count(int tiles_m, int tiles_n, int sym, int g) {
+__host__ __device__ inline int tile_count(int tiles_m, int tiles_n, int sym, int g, int r) {
   if (!sym) return tiles_m * tiles_n;
   int n = 0;
-  for (int mt = 0; mt < tiles_m; ++mt) n += tiles_n - (mt >> g << g);
+  for (int mt = 0; mt < tiles_m; ++mt) n += tiles_n - (mt >> g << g) * r;
   return n;
 }
 
@@ -272,15 +273,17 @@ __device__ __forceinline__ void finish_piece(const NsGemm& a, const CUtensorMap*
 
 // One product.  Warp 0 copies operand blocks (128 rows or columns x 64 K values) into a ring of stages, warp 1
 // issues the tcgen05 products into one of two accumulators, eight warps finish the other one.
-//   PAIR: the two CTAs of a cluster work on one 256 x 256 tile (cta_group::2): each holds 128 rows of A, 128 of the
+//   PAIR (TN = 256): the two CTAs of a cluster work on one 256 x 256 tile (cta_group::2): each holds 128 rows of A, 128 of the
 //         256 columns of B and 128 rows of the result, so a stage of 32 KiB feeds 512 cycles of the tensor core: 64
 //         bytes a cycle, what an SM can take from L2.  (A single CTA's 128 x 256 tile needs 94.)
-//   else: a CTA has its own 128 x 128 tile and, when there are fewer tiles than SMs, shares its K range with the
+//   else: a CTA has its own 128 x TN tile and, when there are fewer tiles than SMs, shares its K range with the
 //         other CTAs of its cluster: each leaves its partial tile in shared memory and adds up (in rank order) the
 //         columns that fall to it.
 // FULL: stages alternate between hi and lo parts, three products for each pair; the sum of `chunk` pairs moves to
 // registers, because the tensor cores cut (not round) each partial sum.
-template <bool PAIR, bool FULL>
+//         Tiles of 64 columns leave an epilogue warp 16 of them instead of 32, and a K block costs 24 KiB: for results of
+//         so few tiles that it is their number that counts.
+template <int TN, bool FULL>
 __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_constant__ CUtensorMap tmA,
                                                              const __grid_constant__ CUtensorMap tmB,
                                                              const __grid_constant__ CUtensorMap tmS,
@@ -288,17 +291,21 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   __shared__ uint64_t full_bar[STAGES], empty_bar[STAGES], tfull_bar[2], tempty_bar[2], src_bar[EPI_WARPS];
   __shared__ uint32_t tmem_base_sm;
-  constexpr int TILE = PAIR ? 256 : 128;
-  constexpr int WCOLS = TILE / 4;                // columns of an epilogue warp
-  constexpr uint32_t TMEM_COLS = 2 * TILE;
+  constexpr bool PAIR = TN == 256;
+  constexpr int TM = PAIR ? 256 : 128, RATIO = TM / TN;
+  constexpr int B_ROWS = PAIR ? 128 : TN;        // columns of B that this CTA copies
+  constexpr int STAGE_USED = OP_BYTES + B_ROWS * BK * 2;
+  constexpr int WCOLS = TN / 4;                  // columns of an epilogue warp ...
+  constexpr int PW = WCOLS < 32 ? WCOLS : 32;    // ... and of a piece
+  constexpr uint32_t TMEM_COLS = 2 * TN;
   unsigned char* tiles = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int csize = PAIR ? 2 : a.split;
   const int rank = csize > 1 ? (int)cluster_rank() : 0;
   const int first = (int)blockIdx.x / csize, stride = (int)gridDim.x / csize;
-  const int tiles_m = (a.M + TILE - 1) / TILE, tiles_n = (a.N + TILE - 1) / TILE;
-  const int g_tiles = PAIR ? 0 : a.sym_log - 7;  // log2 of the tiles in a symmetric block
-  const int per = tile_count(tiles_m, tiles_n, a.sym, g_tiles), total = per * a.batch;
+  const int tiles_m = (a.M + TM - 1) / TM, tiles_n = (a.N + TN - 1) / TN;
+  const int g_tiles = PAIR ? 0 : a.sym_log - 7;  // log2 of the row tiles in a symmetric block
+  const int per = tile_count(tiles_m, tiles_n, a.sym, g_tiles, RATIO), total = per * a.batch;
   const int n_local = first < total ? (total - first + stride - 1) / stride : 0;
   const int kb_all = (a.K + BK - 1) / BK;
   // this CTA's K blocks
@@ -341,8 +348,8 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
       for (int i = 0; i < n_local && ok; ++i) {
         const int u = first + i * stride, b = u / per;
         int mt, nt;
-        tile_of(u - b * per, tiles_n, a.sym, g_tiles, mt, nt);
-        const int rA = PAIR ? mt * 256 + rank * 128 : mt * 128, rB = PAIR ? nt * 256 + rank * 128 : nt * 128;
+        tile_of(u - b * per, tiles_n, a.sym, g_tiles, RATIO, mt, nt);
+        const int rA = PAIR ? mt * 256 + rank * 128 : mt * 128, rB = PAIR ? nt * 256 + rank * 128 : nt * TN;
         for (int kb = kb0; kb < kb1 && ok; ++kb) {
           const int kblk = kb * BK >> a.sym_log;
           const bool mnA = a.a_mn || (a.a_sym && kblk < rA >> a.sym_log), mnB = a.b_mn || (a.b_sym && kblk < rB >> a.sym_log);
@@ -352,7 +359,7 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
             ok = mbar_spin_bounded(&empty_bar[s], (uint32_t)(((it / STAGES) & 1) ^ 1));
             if (!ok) break;
             unsigned char* sa = tiles + (size_t)s * STAGE_BYTES;
-            if (!PAIR || rank == 0) mbar_expect_tx(&full_bar[s], PAIR ? 2 * STAGE_BYTES : STAGE_BYTES);
+            if (!PAIR || rank == 0) mbar_expect_tx(&full_bar[s], PAIR ? 2 * STAGE_USED : STAGE_USED);
             // a pair's copies are all counted by its first CTA, whose thread issues the products
             const uint32_t bar = PAIR ? cluster_map(smem_u32(&full_bar[s]), 0) : smem_u32(&full_bar[s]);
 #pragma unroll
@@ -361,7 +368,7 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
               tma_load_3d_to<PAIR>(sa + j * BLK_BYTES, &tmA, mnA ? r : kc, mnA ? kc : r, z, bar);
             }
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
+            for (int j = 0; j < B_ROWS / 64; ++j) {
               const int r = rB + j * 64;
               tma_load_3d_to<PAIR>(sa + OP_BYTES + j * BLK_BYTES, &tmB, mnB ? r : kc, mnB ? kc : r, z, bar);
             }
@@ -373,20 +380,20 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
   } else if (warp == 1) {
     if (lane == 0 && (!PAIR || rank == 0)) {
       // fp16 operands, fp32 sum
-      constexpr uint32_t IDESC = (1u << 4) | ((uint32_t)(TILE >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24);
+      constexpr uint32_t IDESC = (1u << 4) | ((uint32_t)(TN >> 3) << 17) | ((uint32_t)(TM >> 4) << 24);
       bool ok = true;
       int it = 0, acc_no = 0;
       for (int i = 0; i < n_local && ok; ++i) {
         const int u = first + i * stride, b = u / per;
         int mt, nt;
-        tile_of(u - b * per, tiles_n, a.sym, g_tiles, mt, nt);
-        const int blkA = mt * TILE >> a.sym_log, blkB = nt * TILE >> a.sym_log;
+        tile_of(u - b * per, tiles_n, a.sym, g_tiles, RATIO, mt, nt);
+        const int blkA = mt * TM >> a.sym_log, blkB = nt * TN >> a.sym_log;
         for (int c = 0; c < chunks && ok; ++c, ++acc_no) {
           const int slot = acc_no & 1;
           ok = mbar_spin_bounded(&tempty_bar[slot], (uint32_t)(((acc_no >> 1) & 1) ^ 1));
           if (!ok) break;
           tc_fence_after();
-          const uint32_t d = tmem_base + (uint32_t)(slot * TILE);
+          const uint32_t d = tmem_base + (uint32_t)(slot * TN);
           const int n = FULL ? (c == chunks - 1 ? nkb - c * a.chunk : a.chunk) : nkb;
           for (int kb = 0; kb < n && ok; ++kb) {
             const int kblk = (kb0 + (FULL ? c * a.chunk : 0) + kb) * BK >> a.sym_log;
@@ -435,10 +442,10 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
     for (int i = 0; i < n_local; ++i) {
       const int u = first + i * stride, b = u / per;
       int mt, nt;
-      tile_of(u - b * per, tiles_n, a.sym, g_tiles, mt, nt);
-      const int m0 = mt * TILE + (PAIR ? rank * 128 : 0) + quad * 32, c0 = sub * WCOLS, n0 = nt * TILE + c0;
+      tile_of(u - b * per, tiles_n, a.sym, g_tiles, RATIO, mt, nt);
+      const int m0 = mt * TM + (PAIR ? rank * 128 : 0) + quad * 32, c0 = sub * WCOLS, n0 = nt * TN + c0;
       // the linear term does not depend on the products: the first piece's is on its way while those are formed
-      if (direct && a.src && lane == 0 && kept(a, m0, n0)) fetch_piece<32>(&tmS, buf, bar, m0, n0, b);
+      if (direct && a.src && lane == 0 && kept(a, m0, n0)) fetch_piece<PW>(&tmS, buf, bar, m0, n0, b);
       const Coef k = coefficients(a, b);
       float sum[FULL ? WCOLS : 1];
       for (int c = 0; c < chunks; ++c, ++acc_no) {
@@ -449,7 +456,7 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
         }
         if (!ok) continue;
         tc_fence_after();
-        const uint32_t tbase = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(slot * TILE + c0);
+        const uint32_t tbase = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(slot * TN + c0);
         if (FULL && chunks > 1) {
           // the chunks are added up in registers; the last one's accumulator takes the total
 #pragma unroll
@@ -465,26 +472,29 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
         }
         if (c == chunks - 1) {
 #pragma unroll 1
-          for (int q = 0; q < WCOLS; q += 32) {
-            uint32_t v[32];
-            tc_ld32_issue(tbase + (uint32_t)q, v);
+          for (int q = 0; q < WCOLS; q += PW) {
+            uint32_t v[PW];
+            if constexpr (PW == 32)
+              tc_ld32_issue(tbase + (uint32_t)q, v);
+            else
+              tc_ld16_issue(tbase + (uint32_t)q, v);
             tc_ld_wait();
             if (!direct) {
               float* part = reinterpret_cast<float*>(tiles) + (size_t)(c0 + q) * TR + quad * 32 + lane;
 #pragma unroll
-              for (int j = 0; j < 32; ++j) part[j * TR] = __uint_as_float(v[j]);
+              for (int j = 0; j < PW; ++j) part[j * TR] = __uint_as_float(v[j]);
               continue;
             }
             if (!kept(a, m0, n0 + q)) continue;
             if (a.src) {
-              if (q && lane == 0) fetch_piece<32>(&tmS, buf, bar, m0, n0 + q, b);
+              if (q && lane == 0) fetch_piece<PW>(&tmS, buf, bar, m0, n0 + q, b);
               ok = __all_sync(0xffffffffu, mbar_wait_bounded(bar, fetched++ & 1u));
               if (!ok) break;
             }
-            float f[32];
+            float f[PW];
 #pragma unroll
-            for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]);
-            finish_piece<32>(a, &tmD, k, buf, lane, m0, n0 + q, b, f);
+            for (int j = 0; j < PW; ++j) f[j] = __uint_as_float(v[j]);
+            finish_piece<PW>(a, &tmD, k, buf, lane, m0, n0 + q, b, f);
           }
         }
         tc_fence_before();
@@ -500,13 +510,13 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
     if (!ok && lane == 0) raise_error(a.err);
   }
   if (!PAIR && csize > 1) {
-    // One tile per cluster.  Its eight groups of 16 columns are dealt out to the CTAs, then to the four warps of a
-    // quadrant, so a warp finishes one piece of 16 columns at most.
+    // One tile per cluster.  Its groups of 16 columns are dealt out to the CTAs, then to the four warps of a quadrant,
+    // so a warp finishes one piece of 16 columns at most.
     const int quad = warp & 3, c = 16 * (rank + ((warp - 2) >> 2) * csize), b = first / per;
     int mt, nt;
-    tile_of(first - b * per, tiles_n, a.sym, g_tiles, mt, nt);
-    const int m0 = mt * TILE + quad * 32, n = nt * TILE + c;
-    const bool mine = warp >= 2 && c < TILE && kept(a, m0, n);
+    tile_of(first - b * per, tiles_n, a.sym, g_tiles, RATIO, mt, nt);
+    const int m0 = mt * TM + quad * 32, n = nt * TN + c;
+    const bool mine = warp >= 2 && c < TN && kept(a, m0, n);
     unsigned char* buf = tiles + (size_t)STAGES * STAGE_BYTES + (size_t)(warp - 2) * PIECE_BYTES;
     if (mine && a.src && lane == 0) fetch_piece<16>(&tmS, buf, &src_bar[warp - 2], m0, n, b);
     // the partial tiles are complete (every stage had been consumed before they were written)
@@ -738,18 +748,21 @@ NsLayout layout(int batch, int rows, int cols) {
 
 cudaError_t set_attributes() {
   const cudaFuncAttribute at = cudaFuncAttributeMaxDynamicSharedMemorySize;
-  cudaError_t e = cudaFuncSetAttribute(ns_gemm_kernel<true, true>, at, SMEM_BYTES);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<true, false>, at, SMEM_BYTES);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<false, true>, at, SMEM_BYTES);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<false, false>, at, SMEM_BYTES);
+  cudaError_t e = cudaFuncSetAttribute(ns_gemm_kernel<256, true>, at, SMEM_BYTES);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<256, false>, at, SMEM_BYTES);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<128, true>, at, SMEM_BYTES);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<128, false>, at, SMEM_BYTES);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<64, true>, at, SMEM_BYTES);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<64, false>, at, SMEM_BYTES);
   if (e == cudaSuccess) e = ns_cluster_set_attributes();
   return e;
 }
 
-template <bool PAIR, bool FULL>
+template <int TN, bool FULL>
 cudaError_t launch_shape(const CUtensorMap& ta, const CUtensorMap& tb, const NsGemm& a, int ctas, cudaStream_t st) {
   CUtensorMap ts = ta, td = ta;  // the epilogue's pieces; not used where there is no linear term or a user's matrix
-  const int width = PAIR || a.split == 1 ? 32 : 16;
+  constexpr bool PAIR = TN == 256;
+  const int width = TN >= 128 && a.split == 1 ? 32 : 16;
   if ((a.src && !make_map_f16(&ts, a.src, a.N, a.M, 2LL * a.batch, a.ld_src, a.src_plane, width)) ||
       (a.out == OUT_SPLIT && !make_map_f16(&td, a.dst, a.N, a.M, 2LL * a.batch, a.ld_dst, a.dst_plane, width)))
     return cudaErrorInvalidValue;
@@ -766,49 +779,53 @@ cudaError_t launch_shape(const CUtensorMap& ta, const CUtensorMap& tb, const NsG
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = PAIR || a.split > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, ns_gemm_kernel<PAIR, FULL>, ta, tb, ts, td, a);
+  return cudaLaunchKernelEx(&cfg, ns_gemm_kernel<TN, FULL>, ta, tb, ts, td, a);
 }
 
-// A K block costs a CTA the same 32 KiB from L2 in either shape (about 512 cycles), so the shape is the one with
-// fewer K blocks in sequence; `ramp` is what filling and draining a tile costs, in K blocks.
+// The shape with the least work in sequence, in units of 512 cycles, what 32 KiB from L2 take an SM: a K block of a
+// pair's tile or of 128 x 128 is one, of 128 x 64 three quarters (FULL twice that, and a pair's products, 1536 cycles a
+// block, then outlast its copies); filling and draining a tile, and adding up a split one, are counted as measured.
 struct Shape {
-  bool pair;
-  int split;
+  int tn, split;
 };
+long long shape_tiles(int M, int N, int sym, int g, int batch, int tn) {
+  const int tm = tn == 256 ? 256 : 128;
+  return (long long)tile_count((M + tm - 1) / tm, (N + tn - 1) / tn, sym, tn == 256 ? 0 : g, tm / tn) * batch;
+}
 Shape choose_shape(int M, int N, int K, int sym, int g, int batch, int full, int sms) {
   const int kb = (K + BK - 1) / BK;
-  auto tiles = [&](int t, int gt) { return (long long)tile_count((M + t - 1) / t, (N + t - 1) / t, sym, gt) * batch; };
-  const long long pairs = tiles(256, 0), singles = tiles(128, g);
-  // FULL: 64 KiB and three products a block; a pair's products (1536 cycles) then outlast its copies (1024)
-  const int kb_pair = full ? 3 : 1, kb_single = full ? 2 : 1, ramp_pair = 14, ramp_single = 6;
-  Shape s{false, 1};
-  long long cost = (singles + sms - 1) / sms * kb * kb_single + ramp_single;
-  for (int k = 2; k <= 8 && singles <= max_clusters(k, sms) && kb >= 2 * k; ++k) {
-    const long long c = (kb + k - 1) / k * kb_single + ramp_single + 10;
-    if (c < cost) {
-      cost = c;
-      s.split = k;
+  const long long pairs = shape_tiles(M, N, sym, g, batch, 256);
+  Shape s{256, 1};
+  double cost = (double)((pairs + sms / 2 - 1) / (sms / 2)) * kb * (full ? 3 : 1) + 14;
+  for (int tn = 128; tn >= 64; tn -= 64) {
+    const long long t = shape_tiles(M, N, sym, g, batch, tn);
+    const double block = (tn == 128 ? 1.0 : 0.75) * (full ? 2 : 1), ramp = tn == 128 ? 6 : 4;
+    for (int k = 1; k <= 8; ++k) {
+      if (k > 1 && (t > max_clusters(k, sms) || kb < 2 * k)) break;
+      const double c = (k == 1 ? (double)((t + sms - 1) / sms) : 1.0) * ((kb + k - 1) / k) * block + ramp + (k > 1 ? 10 : 0);
+      if (c < cost) {
+        cost = c;
+        s = Shape{tn, k};
+      }
     }
   }
-  if ((pairs + sms / 2 - 1) / (sms / 2) * kb * kb_pair + ramp_pair < cost) s = Shape{true, 1};
   return s;
 }
 
 cudaError_t launch_ns_gemm(const CUtensorMap& ta, const CUtensorMap& tb, NsGemm a, const Shape& s, int full, int sms,
                            cudaStream_t st) {
-  const int t = s.pair ? 256 : 128;
-  const long long tiles =
-      (long long)tile_count((a.M + t - 1) / t, (a.N + t - 1) / t, a.sym, s.pair ? 0 : a.sym_log - 7) * a.batch;
+  const long long tiles = shape_tiles(a.M, a.N, a.sym, a.sym_log - 7, a.batch, s.tn);
   a.split = s.split;
   // The tensor cores cut each of a chunk's partial sums, an error that grows with their number and, like fp32's own
   // rounding, weighs less in longer sums.  Error of the result, time, with 4 / 2 / 1 blocks a chunk (fp32 arithmetic
   // 1.5e-6, 2.4e-6, 2.6e-6): 200 x 784 3.5e-6 2.2e-6 1.4e-6, 140 143 147 us; 1024 x 1024 2.6e-6 1.2e-6 0.6e-6,
   // 210 214 225 us; 4096 x 4096 1.2e-6 0.7e-6 0.5e-6, 4.0 4.4 6.0 ms.
   a.chunk = a.K <= 512 ? 1 : a.K <= 2048 ? 2 : 4;
-  const long long room = s.pair ? sms / 2 : sms, want = tiles * (s.pair ? 1 : a.split);
-  const int ctas = (int)(want < room ? want : room) * (s.pair ? 2 : 1);
-  if (s.pair) return full ? launch_shape<true, true>(ta, tb, a, ctas, st) : launch_shape<true, false>(ta, tb, a, ctas, st);
-  return full ? launch_shape<false, true>(ta, tb, a, ctas, st) : launch_shape<false, false>(ta, tb, a, ctas, st);
+  const long long room = s.tn == 256 ? sms / 2 : sms, want = tiles * a.split;
+  const int ctas = (int)(want < room ? want : room) * (s.tn == 256 ? 2 : 1);
+  if (s.tn == 256) return full ? launch_shape<256, true>(ta, tb, a, ctas, st) : launch_shape<256, false>(ta, tb, a, ctas, st);
+  if (s.tn == 128) return full ? launch_shape<128, true>(ta, tb, a, ctas, st) : launch_shape<128, false>(ta, tb, a, ctas, st);
+  return full ? launch_shape<64, true>(ta, tb, a, ctas, st) : launch_shape<64, false>(ta, tb, a, ctas, st);
 }
 
 }  // namespace
@@ -887,7 +904,7 @@ cudaError_t ns_run(const NsProblem& p, void* work, cudaStream_t st, const char**
     gram = choose_shape(L.r, L.r, L.c, 1, g, p.batch, p.full, sms);
     poly = choose_shape(L.r, L.r, L.r, 1, g, p.batch, p.full, sms);
     apply = choose_shape(p.rows, p.cols, L.r, 0, g, p.batch, p.full, sms);
-    if (sym_log == 8 || !(gram.pair || poly.pair || apply.pair)) break;
+    if (sym_log == 8 || (gram.tn != 256 && poly.tn != 256 && apply.tn != 256)) break;
     sym_log = 8;
   }
   const float ca = (float)p.coef[0], cb = (float)p.coef[1], cc = (float)p.coef[2];
