@@ -348,7 +348,8 @@ gcada_status gcada_innovation_norms_noalloc(const float *fresh_dev, const float 
  *     X_0 = g / (||g||_F + eps),  X_{j+1} = a X_j + (b A_j + c A_j^2) X_j,  A_j = X_j X_j^T
  * which drive the singular values towards one.  coef = {a, b, c} (host; NULL: 3.4445, -4.7750, 2.0315, for which
  * five steps take singular values above 0.01 of the norm to between 0.68 and 1.21).  The iterates' singular values
- * have to stay below 7.  A matrix of zeros gives zeros; one that holds an infinity or NaN gives NaN.  o may be g.
+ * have to stay below 7.  A matrix of zeros gives zeros; one that holds an infinity or NaN gives NaN
+ * everywhere (after one step at least).  o may be g, in the same layout.
  * GCADA_EINVAL unless 0 <= steps <= 100, |a|, |b|, |c| <= 16, 1e-30 <= eps <= 1e30, rows, cols <= 2^20, batch <=
  * 65535, the results do not overlap, and work_dev is 256-byte aligned with at least the bytes that
  * gcada_orthogonalize_work gives (256 means that the area is not used: matrices with a short side of up to 64 stay
@@ -366,7 +367,7 @@ gcada_status gcada_orthogonalize(const void *g_dev, void *o_dev, int type, int b
  *     m <- beta m + (1 - beta) g           (the weighting of Eq. 8a)
  *     u  = nesterov ? beta m + (1 - beta) g : m
  *     w <- (1 - lr weight_decay) w - lr scale o,   o = u orthogonalised as above
- * m is float; w and g have their own types.  The work area is that of gcada_orthogonalize with batch 1.
+ * m is float; w and g have their own types; the three do not overlap.  The work area is that of gcada_orthogonalize with batch 1.
  * GCADA_EINVAL as there, and unless 0 <= beta < 1 and lr, weight_decay, scale are finite (at most 1e30).
  */
 gcada_status gcada_muon_update(void *w_dev, int w_type, float *m_dev, const void *g_dev, int g_type, int rows,

@@ -112,6 +112,7 @@ gcada_status gcada_muon_update(void* w_dev, int w_type, float* m_dev, const void
   REFUSE(!aligned_to(w_dev, type_bytes(w_type)) || !aligned_to(m_dev, 4) || !aligned_to(g_dev, type_bytes(g_type)),
          "a matrix pointer is not aligned to its type");
   REFUSE(ld_w < cols || ld_m < cols || ld_g < cols, "a row stride is smaller than cols");
+  REFUSE(w_dev == m_dev || w_dev == g_dev || m_dev == g_dev, "w, m and g must be different matrices");
   const size_t need = gcada::ns_work_bytes(1, rows, cols);
   REFUSE(!work_dev || !aligned_to(work_dev, 256) || work_bytes < need, "need a 256-byte aligned work area of %zu bytes", need);
   gcada::NsProblem p{};

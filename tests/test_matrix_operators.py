@@ -84,7 +84,7 @@ def c_muon(lib, **kw):
 @pytest.mark.parametrize("bad", [
     dict(wt=3), dict(gt=-1), dict(rows=-1), dict(lr=float("nan")), dict(lr=float("inf")), dict(beta=1.0), dict(beta=-0.1),
     dict(wd=float("inf")), dict(scale=float("nan")), dict(w=0), dict(m=0), dict(g=0), dict(m=8194), dict(ld=(3, 4, 4)),
-    dict(ld=(4, 3, 4)), dict(ld=(4, 4, 3)), dict(work=0), dict(bytes=100)])
+    dict(ld=(4, 3, 4)), dict(ld=(4, 4, 3)), dict(work=0), dict(bytes=100), dict(m=4096), dict(g=4096), dict(g=8192)])
 def test_muon_refuses(lib, bad):
     st, text = c_muon(lib, **bad)
     assert st == binding.EINVAL and text
@@ -117,6 +117,20 @@ def test_mx_refuses(lib):
     n, s = C.c_size_t(), C.c_size_t()
     assert lib.gcada_mx_size(-1, 4, C.byref(n), C.byref(s)) == binding.EINVAL
     assert lib.gcada_mx_size(130, 257, C.byref(n), C.byref(s)) == binding.OK and (n.value, s.value) == (130 * 144, 4 * 1024)
+
+
+def test_without_a_device_the_operators_fail(lib):
+    if torch.cuda.is_available():
+        pytest.skip("a GPU is present")
+    st, text = c_orth(lib)
+    assert st == binding.ECUDA and text
+    st, text = c_muon(lib)
+    assert st == binding.ECUDA and text
+    buf = binding.C.create_string_buffer(256)
+    VP = binding._VP
+    assert lib.gcada_mx_quantize(VP(4096), 0, 4, 4, 4, 0, VP(4096), VP(8192), None, buf, 256) == binding.ECUDA and buf.value
+    assert lib.gcada_mx_gemm(VP(4096), VP(4096), 4, VP(4096), VP(4096), 4, 32, VP(4096), 0, 4, 1.0, 0.0, None, None, None, buf, 256) == binding.ECUDA
+    assert lib.gcada_mx_gemm(VP(4096), VP(4096), 4, VP(4096), VP(4096), 4, 32, VP(4096), 0, 4, 1.0, 0.0, None, None, None, None, 0) == binding.ECUDA
 
 
 def test_python_refusals():
@@ -195,6 +209,82 @@ def test_orthogonalize_steps_coefficients_and_scale():
         h = g.clone()
         h[3, 4] = bad
         assert binding.orthogonalize(h).isnan().all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+def test_orthogonalize_extremes(t):
+    """What test_orthogonalize_steps_coefficients_and_scale checks for matrices that stay on chip, for larger ones."""
+    tol = (FULL_TOL if t == "f32" else HALF_TOL) + OUT[t]
+    for shape in ((100, 150), (150, 100), (700, 300)):
+        g = torch.from_numpy(spectrum(*shape, "gauss")).to(TYPES[t]).cuda()
+        for factor in (1e-30, 1e-9, 1e-6, 1e25):
+            h = g * factor
+            assert rel(num(binding.orthogonalize(h)), om.newton_schulz(num(h))) <= tol, (shape, factor)
+        for steps in (0, 1, 2, 9):
+            assert rel(num(binding.orthogonalize(g, steps=steps)), om.newton_schulz(num(g), steps)) <= tol
+        assert (binding.orthogonalize(torch.zeros_like(g)) == 0).all()
+        for bad in (float("nan"), float("inf"), -float("inf")):
+            h = g.clone()
+            h[3, 4] = bad
+            assert binding.orthogonalize(h).isnan().all()
+    assert binding.orthogonalize(g[:0]).shape == (0, 300) and binding.orthogonalize(g[:, :0]).shape == (700, 0)
+    assert binding.orthogonalize(g[None][:0]).shape == (0, 700, 300)
+    assert binding.mx_quantize(g[:0]).dequantize().shape == (0, 300)
+    q = binding.mx_quantize(g)
+    assert binding.mx_gemm(binding.mx_quantize(g[:0]), q).shape == (0, 700)
+    with pytest.raises(binding.GCadaError):
+        binding.mx_gemm(binding.mx_quantize(g[:, :0]), binding.mx_quantize(g[:, :0]))
+    for bad in (g.T, g[:, ::2], g.double()):
+        with pytest.raises(ValueError):
+            binding.orthogonalize(bad)
+
+
+def exact_orthogonalize(g, steps=5):
+    """The 64-bit form on the device, for sweeps."""
+    x = g.double()
+    x = x / (torch.linalg.matrix_norm(x)[..., None, None] + 1e-7)
+    a, b, c = om.COEF
+    for _ in range(steps):
+        s = x @ x.mT if x.shape[-2] <= x.shape[-1] else x.mT @ x
+        p = b * s + c * (s @ s)
+        x = a * x + (p @ x if x.shape[-2] <= x.shape[-1] else x @ p)
+    return x
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("seed", range(6))
+def test_orthogonalize_sweep(seed):
+    rng = np.random.default_rng(seed)
+    for _ in range(25):
+        rows, cols = (int(round(np.exp(rng.uniform(0, np.log(1500))))) for _ in range(2))
+        batch = int(rng.integers(1, 4))
+        t = ("f32", "bf16")[int(rng.integers(2))]
+        gen = torch.Generator(device="cuda").manual_seed(int(rng.integers(1 << 30)))
+        g = torch.randn(batch, rows, cols, generator=gen, device="cuda")
+        g *= torch.exp(torch.randn(batch, rows, 1, generator=gen, device="cuda"))
+        g = g.to(TYPES[t])
+        want = exact_orthogonalize(g)
+        for precision, tol in (("full", FULL_TOL), ("half", HALF_TOL)):
+            o = binding.orthogonalize(g, precision=precision)
+            err = torch.linalg.matrix_norm(o.double() - want) / torch.linalg.matrix_norm(want)
+            assert (err <= tol + OUT[t]).all(), (batch, rows, cols, t, precision, err)
+    binding.check_operators()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("seed", range(4))
+def test_product_sweep(seed):
+    rng = np.random.default_rng(seed)
+    for _ in range(25):
+        m, n, k = (int(round(np.exp(rng.uniform(0, np.log(top))))) for top in (1500, 1500, 6000))
+        gen = torch.Generator(device="cuda").manual_seed(int(rng.integers(1 << 30)))
+        x, y = (torch.randn(s, k, generator=gen, device="cuda") * torch.exp(2 * torch.randn(s, 1, generator=gen, device="cuda")) for s in (m, n))
+        a, b = binding.mx_quantize(x), binding.mx_quantize(y.T.contiguous(), transpose=True)
+        av, bv = a.dequantize().double(), b.dequantize().double()
+        d = binding.mx_gemm(a, b).double()
+        assert ((d - av @ bv.T).abs() <= (k / 32 + 3) * 2.0 ** -23 * (av.abs() @ bv.abs().T)).all(), (m, n, k)
+    binding.check_operators()
 
 
 @pytest.mark.gpu
