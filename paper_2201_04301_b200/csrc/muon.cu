@@ -633,6 +633,8 @@ __device__ __forceinline__ void split8(const float (&f)[8], uint4& h, uint4& l) 
 // Squared Frobenius norm in doubles, NORM_BLOCKS partial sums per matrix (fixed order: bitwise reproducible).
 __global__ void __launch_bounds__(256) ns_norm_kernel(const NsSource s, double* part) {
   __shared__ double scratch[40];
+  pdl_launch_dependents();
+  pdl_wait();
   const int b = blockIdx.y, cpr = (s.cols + 7) / 8;
   const long long total = (long long)cpr * s.rows;
   double acc = 0.0;
@@ -652,6 +654,8 @@ __global__ void __launch_bounds__(256) ns_scale_kernel(const NsSource s, const d
                                                        float growth, int steps, float* rho, __half* x, long long ld,
                                                        long long plane) {
   __shared__ double scratch[40];
+  pdl_launch_dependents();
+  pdl_wait();
   const int b = blockIdx.y, cpr = (s.cols + 7) / 8;
   const long long total = (long long)cpr * s.rows;
   double ss = 0.0;
@@ -880,10 +884,11 @@ cudaError_t ns_run(const NsProblem& p, void* work, cudaStream_t st, const char**
   const int nb = (int)(want < NORM_BLOCKS ? want : NORM_BLOCKS);
   float growth = 1.f;  // power of two >= max(1, |a|)
   while (growth < fabs(p.coef[0])) growth *= 2.f;
-  ns_norm_kernel<<<dim3(nb, p.batch), 256, 0, st>>>(s, part);
-  ns_scale_kernel<<<dim3(nb, p.batch), 256, 0, st>>>(s, part, nb, p.eps, growth, p.steps, rho, X[0], L.ld_x,
-                                                         L.plane_x);
-  if ((e = cudaGetLastError()) != cudaSuccess) return *why = "kernel launch", e;
+  const dim3 grid((unsigned)nb, (unsigned)p.batch);
+  if ((e = launch_k(ns_norm_kernel, grid, dim3(256), 0, st, true, s, part)) != cudaSuccess ||
+      (e = launch_k(ns_scale_kernel, grid, dim3(256), 0, st, true, s, part, nb, p.eps, growth, p.steps, rho, X[0], L.ld_x,
+                    L.plane_x)) != cudaSuccess)
+    return *why = "kernel launch", e;
   int n = 2;
 
   const bool tall = p.rows > p.cols;

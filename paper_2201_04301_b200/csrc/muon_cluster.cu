@@ -108,6 +108,8 @@ __global__ void __launch_bounds__(NC_THREADS, 1) ns_cluster_kernel(const NsSourc
 
   // the slice, momentum moved on the way; squares in doubles
   for (int e = tid; e < n.csp * rp; e += threads) X[e] = 0.f;
+  pdl_launch_dependents();
+  pdl_wait();
   __syncthreads();
   const int count = kn * n.r;
   double ss = 0.0;
@@ -293,12 +295,14 @@ cudaError_t launch_ns_cluster(const NsSource& s, const NsSink& o, int batch, con
   cfg.blockDim = dim3((unsigned)(want <= 64 ? 128 : want <= 192 ? 256 : NC_THREADS));
   cfg.dynamicSmemBytes = bytes;
   cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = (unsigned)n.csize;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)n.csize;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = n.csize > 1 ? 1 : 0;
+  cfg.numAttrs = n.csize > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, ns_cluster_kernel, s, o, n);
 }
 

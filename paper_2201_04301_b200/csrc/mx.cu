@@ -81,6 +81,8 @@ template <typename T>
 __global__ void __launch_bounds__(256) mx_quantize_kernel(const T* __restrict__ x, long long ld, const MxView q, int pass) {
   const int lane = threadIdx.x & 31, rows = (int)q.rows, row_end = (rows + 127) / 128 * 128;
   const WarpPlace at = warp_place(q, pass);
+  pdl_launch_dependents();
+  pdl_wait();
   const int ct = at.ct;
   const long long c = (long long)ct * 256 + lane * 8;
   for (int r0 = at.row; r0 < row_end; r0 += ROWS_AT_ONCE * pass) {
@@ -149,6 +151,8 @@ __global__ void __launch_bounds__(256) mx_quantize_t_kernel(const T* __restrict_
   typename P::raw v[32];
   const T* p = x + k0 * ld + r;
   const bool aligned = (reinterpret_cast<uintptr_t>(x) & (2 * sizeof(T) - 1)) == 0 && (ld & 1) == 0;
+  pdl_launch_dependents();
+  pdl_wait();
   if (aligned && r0 + 64 <= q.rows && k0 + 32 <= q.cols) {  // the same for the whole warp
 #pragma unroll
     for (int j = 0; j < 32; ++j) v[j] = *reinterpret_cast<const typename P::raw*>(p + j * ld);
@@ -209,6 +213,8 @@ template <typename T>
 __global__ void __launch_bounds__(256) mx_dequantize_kernel(const MxView q, T* __restrict__ out, long long ld, int pass) {
   const int lane = threadIdx.x & 31, rows = (int)q.rows;
   const WarpPlace at = warp_place(q, pass);
+  pdl_launch_dependents();
+  pdl_wait();
   const int ct = at.ct;
   const long long c = (long long)ct * 256 + lane * 8;
   if (c < q.cols) {
@@ -715,31 +721,24 @@ static int rows_per_pass(long long rows, long long col_tiles) {
 }
 
 cudaError_t mx_quantize(const void* x, int bf16, long long ld, int transpose, const MxView& q, cudaStream_t st) {
+  const float* f = static_cast<const float*>(x);
+  const __nv_bfloat16* h = static_cast<const __nv_bfloat16*>(x);
   if (transpose) {
     const dim3 grid((unsigned)((q.rows + 127) / 128 * 2 * q.col_tiles));
-    if (bf16)
-      mx_quantize_t_kernel<<<grid, 256, 0, st>>>(static_cast<const __nv_bfloat16*>(x), ld, q);
-    else
-      mx_quantize_t_kernel<<<grid, 256, 0, st>>>(static_cast<const float*>(x), ld, q);
-  } else {
-    const int pass = rows_per_pass((q.rows + 127) / 128 * 128, q.col_tiles);
-    const unsigned blocks = (unsigned)((pass * q.col_tiles + 7) / 8);
-    if (bf16)
-      mx_quantize_kernel<<<blocks, 256, 0, st>>>(static_cast<const __nv_bfloat16*>(x), ld, q, pass);
-    else
-      mx_quantize_kernel<<<blocks, 256, 0, st>>>(static_cast<const float*>(x), ld, q, pass);
+    return bf16 ? launch_k(mx_quantize_t_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, true, h, ld, q)
+                : launch_k(mx_quantize_t_kernel<float>, grid, dim3(256), 0, st, true, f, ld, q);
   }
-  return cudaGetLastError();
+  const int pass = rows_per_pass((q.rows + 127) / 128 * 128, q.col_tiles);
+  const dim3 grid((unsigned)((pass * q.col_tiles + 7) / 8));
+  return bf16 ? launch_k(mx_quantize_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, true, h, ld, q, pass)
+              : launch_k(mx_quantize_kernel<float>, grid, dim3(256), 0, st, true, f, ld, q, pass);
 }
 
 cudaError_t mx_dequantize(const MxView& q, void* out, int bf16, long long ld, cudaStream_t st) {
   const int pass = rows_per_pass(q.rows, q.col_tiles);
-  const unsigned blocks = (unsigned)((pass * q.col_tiles + 7) / 8);
-  if (bf16)
-    mx_dequantize_kernel<<<blocks, 256, 0, st>>>(q, static_cast<__nv_bfloat16*>(out), ld, pass);
-  else
-    mx_dequantize_kernel<<<blocks, 256, 0, st>>>(q, static_cast<float*>(out), ld, pass);
-  return cudaGetLastError();
+  const dim3 grid((unsigned)((pass * q.col_tiles + 7) / 8));
+  return bf16 ? launch_k(mx_dequantize_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, true, q, static_cast<__nv_bfloat16*>(out), ld, pass)
+              : launch_k(mx_dequantize_kernel<float>, grid, dim3(256), 0, st, true, q, static_cast<float*>(out), ld, pass);
 }
 
 cudaError_t mx_gemm(const MxGemm& p, cudaStream_t st, const char** why) {
