@@ -1,11 +1,11 @@
 // Newton-Schulz steps of a narrow matrix (short side up to 64) in one launch: the long side is dealt out to the CTAs
 // of a thread-block cluster, which keep their slices of X in shared memory for all steps, in fp32 throughout.
 //
-// A step: every CTA forms its slice's share of A = X X^T; cluster barrier; every CTA adds up its part of A from all
-// shares (through distributed shared memory, in rank order: bitwise reproducible) and hands it to all; cluster
-// barrier; every CTA forms b A + c A^2 for itself and applies it to its slice.  Bound: latency - each phase is some
-// hundred to some thousand cycles of FMAs between barriers.  As separate tensor-core launches the same steps cost
-// 4 to 5 us per product however small it is.
+// A step: every CTA forms its slice's share of A = X X^T; cluster barrier; A is added up from all shares through
+// distributed shared memory, in rank order (bitwise reproducible); every CTA forms b A + c A^2 for itself and applies
+// it to its slice.  Bound: latency - each phase is about a thousand cycles of dependent loads, FMAs and a barrier for
+// narrow matrices, some thousands for 64 rows.  As separate tensor-core launches the same steps cost 4 to 5 us per
+// product however small it is.
 #include <cuda_bf16.h>
 
 #include "common.cuh"
@@ -19,11 +19,15 @@ constexpr int NC_THREADS = 512;
 constexpr int NC_MAX_R = 64;
 static_assert(NC_MAX_R <= 64, "the tiles of A fit the smallest block that they are given");
 constexpr int NC_MAX_SMEM = 220 * 1024;
+// Multiply-adds of a product beyond which the tensor cores win in spite of their launches (here / there, us, fp32 and
+// bf16: 32 x 2048 59 / 85 71, 48 x 1500 79 / 86 73, 64 x 1024 94 / 82 72, 64 x 2048 151 / 90 75).
+constexpr long long NC_MAX_WORK = 3300000;
 
 struct NcArgs {
   int r, c, cs;   // short and long side; columns of the long side per CTA
   int rp, csp;    // padded row length (4 x odd: rows start in different banks) and slice length (multiple of 4)
   int tall, csize, steps;
+  int direct;     // every CTA reads all shares of A
   float a, b, cc;
   double eps;
 };
@@ -94,14 +98,13 @@ __device__ __forceinline__ void symmetric_product(const SymPlace& p, const float
 
 __global__ void __launch_bounds__(NC_THREADS, 1) ns_cluster_kernel(const NsSource s, const NsSink o, const NcArgs n) {
   extern __shared__ __align__(16) float sm[];
-  __shared__ double scratch[40];
-  __shared__ double share[1];
+  __shared__ double share[NC_THREADS / 32];
   const int rp = n.rp, sq = rp * rp;
   float* X = sm;                       // [csp][rp]: X transposed, element (i, k) at k * rp + i
   float* Y = X + (size_t)n.csp * rp;   // the next iterate
   float* A = Y + (size_t)n.csp * rp;
   float* Q = A + sq;
-  float* part = Q + sq;                // clusters: this CTA's share of A
+  float* part = Q + sq;                // clusters: this CTA's share of A (two of them if read directly)
   const int b = blockIdx.x / n.csize, rank = n.csize > 1 ? (int)cluster_rank() : 0;
   const int k0 = rank * n.cs, kn = max(0, min(n.cs, n.c - k0));
   const int tid = threadIdx.x, threads = blockDim.x;
@@ -128,50 +131,57 @@ __global__ void __launch_bounds__(NC_THREADS, 1) ns_cluster_kernel(const NsSourc
     X[k * rp + i] = v;
     ss += (double)v * (double)v;
   }
-  ss = block_sum(ss, scratch);
-  if (n.csize > 1) {
-    if (tid == 0) share[0] = ss;
+  // every warp adds up all warps' sums of all CTAs itself, in one order
+  ss = warp_sum(ss);
+  const int warps = threads >> 5, lane = tid & 31;
+  if (lane == 0) share[tid >> 5] = ss;
+  if (n.csize > 1)
     cluster_sync();
-    if (tid == 0) {
-      ss = 0.0;
-      for (int p = 0; p < n.csize; ++p) {
-        double v;
-        asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(cluster_map(smem_u32(share), (uint32_t)p)) : "memory");
-        ss += v;
-      }
-      scratch[0] = ss;
-    }
+  else
     __syncthreads();
-    ss = scratch[0];
+  ss = 0.0;
+  for (int i = lane; i < warps * n.csize; i += 32) {
+    const int p = i / warps, w = i - p * warps;
+    ss += n.csize > 1 ? cluster_load_f64(cluster_map(smem_u32(share + w), (uint32_t)p)) : share[w];
   }
-  const double norm = sqrt(ss) + n.eps;
-  for (int e = tid; e < n.csp * rp; e += threads) X[e] = (float)((double)X[e] / norm);
+  ss = warp_sum(ss);
+  const double inv = 1.0 / (sqrt(ss) + n.eps);
+  for (int e = tid; e < kn * rp; e += threads) X[e] = (float)((double)X[e] * inv);
   __syncthreads();
 
   const int nt = rp >> 2, kgroups = (kn + 3) >> 2, items = kgroups * nt;
   int lk = 0;  // 2^lk lanes share an item's sum over j
   while (lk < 4 && (items << (lk + 1)) <= threads && (2 << lk) <= nt) ++lk;
   const SymPlace gram = sym_place(nt, kn), poly = sym_place(nt, n.r);
-  const int e0 = (sq >> 2) * rank / n.csize, e1 = (sq >> 2) * (rank + 1) / n.csize;
+  const int e0 = n.direct ? 0 : (sq >> 2) * rank / n.csize, e1 = n.direct ? sq >> 2 : (sq >> 2) * (rank + 1) / n.csize;
   for (int step = 0; step < n.steps; ++step) {
-    symmetric_product(gram, X, kn, rp, n.csize > 1 ? part : A, nullptr, 0.f, 1.f);
+    float* mine = n.csize > 1 ? part + (n.direct && (step & 1) ? sq : 0) : A;
+    symmetric_product(gram, X, kn, rp, mine, nullptr, 0.f, 1.f);
     if (n.csize > 1) {
-      // each CTA adds up its part of the matrix and hands it to all
+      // A is the sum of all shares: of a small matrix every CTA reads them all (from alternating buffers, so that the
+      // next step's may be written meanwhile), of a larger one each adds up a part and hands it to all
       cluster_sync();
       for (int e = e0 + tid; e < e1; e += threads) {
         float4 v[8];
 #pragma unroll
         for (int p = 0; p < 8; ++p)
-          if (p < n.csize) v[p] = cluster_load4(cluster_map(smem_u32(part + 4 * e), (uint32_t)p));
+          if (p < n.csize) v[p] = cluster_load4(cluster_map(smem_u32(mine + 4 * e), (uint32_t)p));
         float4 t = v[0];
 #pragma unroll
         for (int p = 1; p < 8; ++p)
           if (p < n.csize) t = make_float4(t.x + v[p].x, t.y + v[p].y, t.z + v[p].z, t.w + v[p].w);
+        if (n.direct) {
+          *reinterpret_cast<float4*>(A + 4 * e) = t;
+        } else {
 #pragma unroll
-        for (int p = 0; p < 8; ++p)
-          if (p < n.csize) cluster_store4(cluster_map(smem_u32(A + 4 * e), (uint32_t)p), t);
+          for (int p = 0; p < 8; ++p)
+            if (p < n.csize) cluster_store4(cluster_map(smem_u32(A + 4 * e), (uint32_t)p), t);
+        }
       }
-      cluster_sync();
+      if (n.direct)
+        __syncthreads();
+      else
+        cluster_sync();
     } else {
       __syncthreads();
     }
@@ -239,26 +249,29 @@ __global__ void __launch_bounds__(NC_THREADS, 1) ns_cluster_kernel(const NsSourc
     else
       static_cast<float*>(to.o)[at] = o.update ? to.decay * static_cast<const float*>(to.prev)[at] - to.step * v : v;
   }
-  if (n.csize > 1) cluster_sync();  // the others have read this CTA's last share
+  // nobody reads this CTA's shared memory any more: with steps in between, since the last barrier or, read directly, once
+  // all have passed this one
+  if (n.csize > 1 && (n.direct || n.steps == 0)) cluster_sync();
 }
 
-// CTAs for a matrix.  One is fastest only while a barrier costs more than the work (16 x 16: 13 us with one, 15 with
-// eight; 16 x 64: equal); from there on eight (10 x 200: 20 and 18 us, 64 x 200: 116 and 43), but no more than let
+// CTAs for a matrix.  One is fastest only while a barrier costs more than the work (16 x 16: 12 us with one, 15 with
+// eight; 16 x 64: 15 and 16); from there on eight (10 x 200: 17 and 15 us, 64 x 200: 111 and 40), but no more than let
 // all matrices of a batch run at once, and enough for the slices to fit.
 NcArgs plan(int batch, int rows, int cols, size_t* bytes) {
   NcArgs n{};
   n.tall = rows > cols;
   n.r = n.tall ? cols : rows;
   n.c = n.tall ? rows : cols;
-  if (n.r > NC_MAX_R) return n;
+  if (n.r > NC_MAX_R || (long long)n.r * n.r * n.c > NC_MAX_WORK) return n;
   const int q = (n.r + 3) / 4;
   n.rp = 4 * (q | 1);
-  int want = (long long)n.rp * n.c <= 1200 ? 1 : 8;
+  n.direct = n.rp <= 20;  // at most 100 pieces of 16 bytes from each of eight CTAs
+  int want = (long long)n.rp * n.c <= 1300 ? 1 : 8;
   while (want > 1 && batch * want > 128) want /= 2;
   for (int cs = want; cs <= 8; cs *= 2) {
     n.cs = (n.c + cs - 1) / cs;
     n.csp = (n.cs + 3) / 4 * 4;
-    const double size = sizeof(float) * ((double)2 * n.csp * n.rp + (double)(cs > 1 ? 3 : 2) * n.rp * n.rp);
+    const double size = sizeof(float) * ((double)2 * n.csp * n.rp + (double)(cs > 1 ? (n.direct ? 4 : 3) : 2) * n.rp * n.rp);
     if (size > NC_MAX_SMEM) continue;
     *bytes = (size_t)size;
     n.csize = cs;
