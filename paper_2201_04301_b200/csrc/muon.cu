@@ -56,8 +56,9 @@ struct NsGemm {
   int sym;               // the result is symmetric (M == N): only its upper blocks of 2^sym_log rows are written
   int a_sym, b_sym;      // so is the operand: a block below the diagonal is read as the transpose of its mirror image
   int sym_log;           // 7 or 8 (8 wherever a pair of CTAs takes part)
+  int tiles_n, per, total;  // tiles in a row, of a matrix, of all matrices
   int split;             // CTAs of a cluster that share a tile's K range
-  int chunk;             // FULL: K blocks summed in tensor memory before the sum moves to registers
+  int chunk, chunk_log;  // FULL: K blocks summed in tensor memory before the sum moves to registers
   float c_src, c_acc;    // value = c_src * src + c_acc * accumulator, times powers of rho
   float diag;            // symmetric results: added on the diagonal (see ns_run on the shifted form)
   float c_src_shift;     // PROD_APPLY / PROD_LAST in the shifted form: added to c_src
@@ -78,7 +79,7 @@ struct NsGemm {
 // column tiles wide.
 __device__ __forceinline__ void tile_of(int u, int tiles_n, int sym, int g, int r, int& mt, int& nt) {
   if (!sym) {
-    mt = u / tiles_n;
+    mt = (int)((unsigned)u / (unsigned)tiles_n);
     nt = u - mt * tiles_n;
     return;
   }
@@ -162,7 +163,7 @@ __device__ __forceinline__ NsTarget target_of(const NsSink& s) { return s.at ? *
 // A warp: f holds row m0 + lane, columns n .. n + PW - 1 of the products' sums.
 template <int PW>
 __device__ __forceinline__ void finish_piece(const NsGemm& a, const CUtensorMap* tmD, const Coef& k, unsigned char* buf, int lane,
-                                             int m0, int n, int b, float (&f)[PW]) {
+                                             bool leader, int m0, int n, int b, float (&f)[PW]) {
 #pragma unroll
   for (int c = 0; c < PW / 8; ++c) {
     if (a.src) {
@@ -182,13 +183,13 @@ __device__ __forceinline__ void finish_piece(const NsGemm& a, const CUtensorMap*
   }
   if (a.out == OUT_SPLIT) {
     const int d = m0 + lane - n;
-    if (a.sym && d >= 0 && d < PW) {
+    if (a.sym && m0 < n + PW && n < m0 + 32 && d >= 0 && d < PW) {
 #pragma unroll
       for (int j = 0; j < PW; ++j)
         if (j == d) f[j] += k.diag;
     }
     if (!a.src) {  // (with a linear term the piece's fetch has waited for the buffer)
-      if (lane == 0) bulk_wait_read();
+      if (leader) bulk_wait_read();
       __syncwarp();
     }
 #pragma unroll
@@ -206,7 +207,7 @@ __device__ __forceinline__ void finish_piece(const NsGemm& a, const CUtensorMap*
     }
     fence_async_shared();
     __syncwarp();
-    if (lane == 0) {
+    if (leader) {
       tma_store_3d(tmD, buf, n, m0, 2 * b);
       if (a.write_lo) tma_store_3d(tmD, buf + PLANE_BYTES, n, m0, 2 * b + 1);
       bulk_commit();
@@ -302,17 +303,18 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int csize = PAIR ? 2 : a.split;
   const int rank = csize > 1 ? (int)cluster_rank() : 0;
-  const int first = (int)blockIdx.x / csize, stride = (int)gridDim.x / csize;
-  const int tiles_m = (a.M + TM - 1) / TM, tiles_n = (a.N + TN - 1) / TN;
+  const int first = (int)(blockIdx.x / (unsigned)csize), stride = (int)(gridDim.x / (unsigned)csize);
+  const int tiles_n = a.tiles_n, per = a.per, total = a.total;
   const int g_tiles = PAIR ? 0 : a.sym_log - 7;  // log2 of the row tiles in a symmetric block
-  const int per = tile_count(tiles_m, tiles_n, a.sym, g_tiles, RATIO), total = per * a.batch;
-  const int n_local = first < total ? (total - first + stride - 1) / stride : 0;
   const int kb_all = (a.K + BK - 1) / BK;
   // this CTA's K blocks
-  const int kb0 = PAIR ? 0 : (int)((long long)kb_all * rank / csize);
-  const int kb1 = PAIR ? kb_all : (int)((long long)kb_all * (rank + 1) / csize);
+  int kb0 = 0, kb1 = kb_all;
+  if (!PAIR && csize > 1) {
+    kb0 = (int)((unsigned)(kb_all * rank) / (unsigned)csize);
+    kb1 = (int)((unsigned)(kb_all * (rank + 1)) / (unsigned)csize);
+  }
   const int nkb = kb1 - kb0;
-  const int chunks = FULL ? (nkb + a.chunk - 1) / a.chunk : 1;
+  const int chunks = FULL ? (nkb + a.chunk - 1) >> a.chunk_log : 1;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {
@@ -340,19 +342,22 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
   const uint32_t tmem_base = tmem_base_sm;
   pdl_launch_dependents();
   pdl_wait();
+  const bool leader = elect_one();
 
   if (warp == 0) {
-    if (lane == 0) {
+    if (leader) {
       bool ok = true;
       int it = 0;
-      for (int i = 0; i < n_local && ok; ++i) {
-        const int u = first + i * stride, b = u / per;
+      const int sym_log = a.sym_log;
+      const bool a_mn = a.a_mn, a_sym = a.a_sym, b_mn = a.b_mn, b_sym = a.b_sym;
+      for (int u = first; u < total && ok; u += stride) {
+        const int b = u < per ? 0 : (int)((unsigned)u / (unsigned)per);
         int mt, nt;
         tile_of(u - b * per, tiles_n, a.sym, g_tiles, RATIO, mt, nt);
         const int rA = PAIR ? mt * 256 + rank * 128 : mt * 128, rB = PAIR ? nt * 256 + rank * 128 : nt * TN;
         for (int kb = kb0; kb < kb1 && ok; ++kb) {
-          const int kblk = kb * BK >> a.sym_log;
-          const bool mnA = a.a_mn || (a.a_sym && kblk < rA >> a.sym_log), mnB = a.b_mn || (a.b_sym && kblk < rB >> a.sym_log);
+          const int kblk = kb * BK >> sym_log;
+          const bool mnA = a_mn || (a_sym && kblk < rA >> sym_log), mnB = b_mn || (b_sym && kblk < rB >> sym_log);
 #pragma unroll
           for (int t = 0; t < (FULL ? 2 : 1); ++t, ++it) {  // plane 0 = hi, 1 = lo
             const int s = it % STAGES, kc = kb * BK, z = 2 * b + t;
@@ -378,16 +383,18 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
       if (!ok) raise_error(a.err);
     }
   } else if (warp == 1) {
-    if (lane == 0 && (!PAIR || rank == 0)) {
+    if (leader && (!PAIR || rank == 0)) {
       // fp16 operands, fp32 sum
       constexpr uint32_t IDESC = (1u << 4) | ((uint32_t)(TN >> 3) << 17) | ((uint32_t)(TM >> 4) << 24);
       bool ok = true;
       int it = 0, acc_no = 0;
-      for (int i = 0; i < n_local && ok; ++i) {
-        const int u = first + i * stride, b = u / per;
+      const int sym_log = a.sym_log;
+      const bool a_mn = a.a_mn, a_sym = a.a_sym, b_mn = a.b_mn, b_sym = a.b_sym;
+      for (int u = first; u < total && ok; u += stride) {
+        const int b = u < per ? 0 : (int)((unsigned)u / (unsigned)per);
         int mt, nt;
         tile_of(u - b * per, tiles_n, a.sym, g_tiles, RATIO, mt, nt);
-        const int blkA = mt * TM >> a.sym_log, blkB = nt * TN >> a.sym_log;
+        const int blkA = mt * TM >> sym_log, blkB = nt * TN >> sym_log;
         for (int c = 0; c < chunks && ok; ++c, ++acc_no) {
           const int slot = acc_no & 1;
           ok = mbar_spin_bounded(&tempty_bar[slot], (uint32_t)(((acc_no >> 1) & 1) ^ 1));
@@ -396,8 +403,8 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
           const uint32_t d = tmem_base + (uint32_t)(slot * TN);
           const int n = FULL ? (c == chunks - 1 ? nkb - c * a.chunk : a.chunk) : nkb;
           for (int kb = 0; kb < n && ok; ++kb) {
-            const int kblk = (kb0 + (FULL ? c * a.chunk : 0) + kb) * BK >> a.sym_log;
-            const bool mnA = a.a_mn || (a.a_sym && kblk < blkA), mnB = a.b_mn || (a.b_sym && kblk < blkB);
+            const int kblk = (kb0 + (FULL ? c * a.chunk : 0) + kb) * BK >> sym_log;
+            const bool mnA = a_mn || (a_sym && kblk < blkA), mnB = b_mn || (b_sym && kblk < blkB);
             const uint32_t idesc = IDESC | (mnA ? 1u << 15 : 0u) | (mnB ? 1u << 16 : 0u);
             const uint64_t ka = mnA ? 128u : 2u, kk_b = mnB ? 128u : 2u;  // descriptor step of 16 K values
             uint64_t da[2], db[2];
@@ -439,13 +446,13 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
     uint32_t fetched = 0;  // pieces fetched so far: the parity of the buffer's barrier
     bool ok = true;
     int acc_no = 0;
-    for (int i = 0; i < n_local; ++i) {
-      const int u = first + i * stride, b = u / per;
+    for (int u = first; u < total; u += stride) {
+      const int b = u < per ? 0 : (int)((unsigned)u / (unsigned)per);
       int mt, nt;
       tile_of(u - b * per, tiles_n, a.sym, g_tiles, RATIO, mt, nt);
       const int m0 = mt * TM + (PAIR ? rank * 128 : 0) + quad * 32, c0 = sub * WCOLS, n0 = nt * TN + c0;
       // the linear term does not depend on the products: the first piece's is on its way while those are formed
-      if (direct && a.src && lane == 0 && kept(a, m0, n0)) fetch_piece<PW>(&tmS, buf, bar, m0, n0, b);
+      if (direct && a.src && leader && kept(a, m0, n0)) fetch_piece<PW>(&tmS, buf, bar, m0, n0, b);
       const Coef k = coefficients(a, b);
       float sum[FULL ? WCOLS : 1];
       for (int c = 0; c < chunks; ++c, ++acc_no) {
@@ -487,19 +494,19 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
             }
             if (!kept(a, m0, n0 + q)) continue;
             if (a.src) {
-              if (q && lane == 0) fetch_piece<PW>(&tmS, buf, bar, m0, n0 + q, b);
+              if (q && leader) fetch_piece<PW>(&tmS, buf, bar, m0, n0 + q, b);
               ok = __all_sync(0xffffffffu, mbar_wait_bounded(bar, fetched++ & 1u));
               if (!ok) break;
             }
             float f[PW];
 #pragma unroll
             for (int j = 0; j < PW; ++j) f[j] = __uint_as_float(v[j]);
-            finish_piece<PW>(a, &tmD, k, buf, lane, m0, n0 + q, b, f);
+            finish_piece<PW>(a, &tmD, k, buf, lane, leader, m0, n0 + q, b, f);
           }
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) {
+        if (leader) {
           if (PAIR)
             mbar_arrive_cluster(cluster_map(smem_u32(&tempty_bar[slot]), 0));
           else
@@ -507,18 +514,18 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
         }
       }
     }
-    if (!ok && lane == 0) raise_error(a.err);
+    if (!ok && leader) raise_error(a.err);
   }
   if (!PAIR && csize > 1) {
     // One tile per cluster.  Its groups of 16 columns are dealt out to the CTAs, then to the four warps of a quadrant,
     // so a warp finishes one piece of 16 columns at most.
-    const int quad = warp & 3, c = 16 * (rank + ((warp - 2) >> 2) * csize), b = first / per;
+    const int quad = warp & 3, c = 16 * (rank + ((warp - 2) >> 2) * csize), b = first < per ? 0 : (int)((unsigned)first / (unsigned)per);
     int mt, nt;
     tile_of(first - b * per, tiles_n, a.sym, g_tiles, RATIO, mt, nt);
     const int m0 = mt * TM + quad * 32, n = nt * TN + c;
     const bool mine = warp >= 2 && c < TN && kept(a, m0, n);
     unsigned char* buf = tiles + (size_t)STAGES * STAGE_BYTES + (size_t)(warp - 2) * PIECE_BYTES;
-    if (mine && a.src && lane == 0) fetch_piece<16>(&tmS, buf, &src_bar[warp - 2], m0, n, b);
+    if (mine && a.src && leader) fetch_piece<16>(&tmS, buf, &src_bar[warp - 2], m0, n, b);
     // the partial tiles are complete (every stage had been consumed before they were written)
     __syncwarp();
     cluster_sync();
@@ -549,12 +556,12 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
       bool ok = true;
       if (a.src) ok = __all_sync(0xffffffffu, mbar_wait_bounded(&src_bar[warp - 2], 0));
       if (ok)
-        finish_piece<16>(a, &tmD, coefficients(a, b), buf, lane, m0, n, b, f);
-      else if (lane == 0)
+        finish_piece<16>(a, &tmD, coefficients(a, b), buf, lane, leader, m0, n, b, f);
+      else if (leader)
         raise_error(a.err);
     }
   }
-  if (warp >= 2 && lane == 0) bulk_wait();  // the results have left
+  if (warp >= 2 && leader) bulk_wait();  // the results have left
   tc_fence_before();
   __syncthreads();
   if (csize > 1) cluster_sync();  // nobody reads this CTA's shared or tensor memory any more
@@ -818,14 +825,17 @@ Shape choose_shape(int M, int N, int K, int sym, int g, int batch, int full, int
 
 cudaError_t launch_ns_gemm(const CUtensorMap& ta, const CUtensorMap& tb, NsGemm a, const Shape& s, int full, int sms,
                            cudaStream_t st) {
-  const long long tiles = shape_tiles(a.M, a.N, a.sym, a.sym_log - 7, a.batch, s.tn);
-  a.split = s.split;
   // The tensor cores cut each of a chunk's partial sums, an error that grows with their number and, like fp32's own
   // rounding, weighs less in longer sums.  Error of the result, time, with 4 / 2 / 1 blocks a chunk (fp32 arithmetic
   // 1.5e-6, 2.4e-6, 2.6e-6): 200 x 784 3.5e-6 2.2e-6 1.4e-6, 140 143 147 us; 1024 x 1024 2.6e-6 1.2e-6 0.6e-6,
   // 210 214 225 us; 4096 x 4096 1.2e-6 0.7e-6 0.5e-6, 4.0 4.4 6.0 ms.
-  a.chunk = a.K <= 512 ? 1 : a.K <= 2048 ? 2 : 4;
-  const long long room = s.tn == 256 ? sms / 2 : sms, want = tiles * a.split;
+  a.chunk_log = a.K <= 512 ? 0 : a.K <= 2048 ? 1 : 2;
+  a.chunk = 1 << a.chunk_log;
+  a.split = s.split;
+  a.tiles_n = (a.N + s.tn - 1) / s.tn;
+  a.per = (int)shape_tiles(a.M, a.N, a.sym, a.sym_log - 7, 1, s.tn);
+  a.total = a.per * a.batch;
+  const long long room = s.tn == 256 ? sms / 2 : sms, want = (long long)a.total * a.split;
   const int ctas = (int)(want < room ? want : room) * (s.tn == 256 ? 2 : 1);
   if (s.tn == 256) return full ? launch_shape<256, true>(ta, tb, a, ctas, st) : launch_shape<256, false>(ta, tb, a, ctas, st);
   if (s.tn == 128) return full ? launch_shape<128, true>(ta, tb, a, ctas, st) : launch_shape<128, false>(ta, tb, a, ctas, st);

@@ -571,9 +571,10 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
   const uint32_t tmem_base = tmem_base_sm;
   pdl_launch_dependents();
   pdl_wait();
+  const bool leader = elect_one();
 
   if (warp == 0) {
-    if (lane == 0) {
+    if (leader) {
       bool ok = true;
       int it = 0;
       for (int i = 0; i < n_local && ok; ++i) {
@@ -598,7 +599,7 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
       if (!ok) raise_error(p.err);
     }
   } else if (warp == 1) {
-    if (lane == 0 && (!PAIR || rank == 0)) {
+    if (leader && (!PAIR || rank == 0)) {
       // E2M1 operands (1 at bits 7 and 10), E8M0 scales (bit 23); bits 29 / 4: which pair of a column's four scale
       // bytes an instruction's two blocks take
       constexpr uint32_t IDESC =
@@ -661,7 +662,7 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
       tc_ld_wait();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) {
+      if (leader) {
         if (PAIR)
           mbar_arrive_cluster(cluster_map(smem_u32(&tempty_bar[slot]), 0));
         else
@@ -683,7 +684,7 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
         }
       }
     }
-    if (!ok && lane == 0) raise_error(p.err);
+    if (!ok && leader) raise_error(p.err);
   }
   if (!PAIR && csize > 1) {
     // one tile per cluster; every stage had been consumed before the partial tiles were written over them
