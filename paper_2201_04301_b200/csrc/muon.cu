@@ -133,7 +133,7 @@ __device__ __forceinline__ Coef coefficients(const NsGemm& a, int b) {
 // its warp: the linear term's hi and lo parts arrive there by a tensor copy, the results take their place and leave
 // the same way.  (With a thread reading and writing its own row in global memory every access of a warp touches 32
 // lines, and those 32 cycles each were what a short product spent most of its time on.)
-constexpr int PLANE_BYTES = 2048, PIECE_BYTES = 2 * PLANE_BYTES;
+constexpr int PIECE_BYTES = 4096;  // 32 columns' hi and lo parts; the lo part follows the hi part, PW * 64 bytes
 // Byte of 16-byte chunk `ch` of `row` in a plane as the copies lay it out (64- or 32-byte swizzle) ...
 template <int PW>
 __device__ __forceinline__ int plane_at(int row, int ch) {
@@ -154,8 +154,7 @@ template <int PW>
 __device__ __forceinline__ void fetch_piece(const CUtensorMap* tm, unsigned char* buf, uint64_t* bar, int m, int n, int b) {
   bulk_wait_read();
   mbar_expect_tx(bar, 2 * 32 * PW * 2);
-  tma_load_3d(buf, tm, n, m, 2 * b, bar);
-  tma_load_3d(buf + PLANE_BYTES, tm, n, m, 2 * b + 1, bar);
+  tma_load_3d(buf, tm, n, m, 2 * b, bar);  // both parts
 }
 
 __device__ __forceinline__ NsTarget target_of(const NsSink& s) { return s.at ? *s.at : s.to; }
@@ -168,7 +167,7 @@ __device__ __forceinline__ void finish_piece(const NsGemm& a, const CUtensorMap*
   for (int c = 0; c < PW / 8; ++c) {
     if (a.src) {
       const uint4 h = *reinterpret_cast<const uint4*>(buf + plane_at<PW>(lane, c));
-      const uint4 l = *reinterpret_cast<const uint4*>(buf + PLANE_BYTES + plane_at<PW>(lane, c));
+      const uint4 l = *reinterpret_cast<const uint4*>(buf + PW * 64 + plane_at<PW>(lane, c));
       const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, lw[4] = {l.x, l.y, l.z, l.w};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -203,13 +202,12 @@ __device__ __forceinline__ void finish_piece(const NsGemm& a, const CUtensorMap*
         l[j] = pack_half2(x - r.x, y - r.y);
       }
       *reinterpret_cast<uint4*>(buf + plane_at<PW>(lane, c)) = make_uint4(h[0], h[1], h[2], h[3]);
-      if (a.write_lo) *reinterpret_cast<uint4*>(buf + PLANE_BYTES + plane_at<PW>(lane, c)) = make_uint4(l[0], l[1], l[2], l[3]);
+      if (a.write_lo) *reinterpret_cast<uint4*>(buf + PW * 64 + plane_at<PW>(lane, c)) = make_uint4(l[0], l[1], l[2], l[3]);
     }
     fence_async_shared();
     __syncwarp();
     if (leader) {
-      tma_store_3d(tmD, buf, n, m0, 2 * b);
-      if (a.write_lo) tma_store_3d(tmD, buf + PLANE_BYTES, n, m0, 2 * b + 1);
+      tma_store_3d(tmD, buf, n, m0, 2 * b);  // with the lo part, if the map's boxes have two planes
       bulk_commit();
     }
     return;
@@ -710,14 +708,15 @@ __global__ void __launch_bounds__(256) ns_copy_kernel(const NsGemm a) {
 
 // ----------------------------------------------------------------- host
 // fp16 array [planes][rows][cols], row stride ld elements, zero fill outside; boxes of 64 columns x 64 rows with the
-// 128-byte swizzle (operands), or 32 or 16 columns x 32 rows with the 64- or 32-byte one (epilogue pieces).
+// 128-byte swizzle (operands), or 32 or 16 columns x 32 rows with the 64- or 32-byte one, hi and lo parts
+// in one box where `parts` is 2 (epilogue pieces).
 bool make_map_f16(CUtensorMap* tm, const void* base, long long cols, long long rows, long long planes, long long ld,
-                  long long plane, int width = 64) {
+                  long long plane, int width = 64, int parts = 1) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
   cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
   cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)plane * 2};
-  cuuint32_t box[3] = {(cuuint32_t)width, width == 64 ? 64u : 32u, 1};
+  cuuint32_t box[3] = {(cuuint32_t)width, width == 64 ? 64u : 32u, (cuuint32_t)parts};
   cuuint32_t es[3] = {1, 1, 1};
   return fn(tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(base), dims, strides, box, es,
             CU_TENSOR_MAP_INTERLEAVE_NONE,
@@ -774,8 +773,8 @@ cudaError_t launch_shape(const CUtensorMap& ta, const CUtensorMap& tb, const NsG
   CUtensorMap ts = ta, td = ta;  // the epilogue's pieces; not used where there is no linear term or a user's matrix
   constexpr bool PAIR = TN == 256;
   const int width = TN >= 128 && a.split == 1 ? 32 : 16;
-  if ((a.src && !make_map_f16(&ts, a.src, a.N, a.M, 2LL * a.batch, a.ld_src, a.src_plane, width)) ||
-      (a.out == OUT_SPLIT && !make_map_f16(&td, a.dst, a.N, a.M, 2LL * a.batch, a.ld_dst, a.dst_plane, width)))
+  if ((a.src && !make_map_f16(&ts, a.src, a.N, a.M, 2LL * a.batch, a.ld_src, a.src_plane, width, 2)) ||
+      (a.out == OUT_SPLIT && !make_map_f16(&td, a.dst, a.N, a.M, 2LL * a.batch, a.ld_dst, a.dst_plane, width, a.write_lo ? 2 : 1)))
     return cudaErrorInvalidValue;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)ctas);
