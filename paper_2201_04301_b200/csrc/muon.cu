@@ -339,8 +339,10 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
   tc_fence_after();
   const uint32_t tmem_base = tmem_base_sm;
   pdl_launch_dependents();
-  pdl_wait();
   const bool leader = elect_one();
+
+  // The previous product's result is waited for where it is first needed, which leaves the way there (whose first run
+  // of instructions and parameters costs as much as a copy) outside the wait.
 
   if (warp == 0) {
     if (leader) {
@@ -365,6 +367,7 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
             if (!PAIR || rank == 0) mbar_expect_tx(&full_bar[s], PAIR ? 2 * STAGE_USED : STAGE_USED);
             // a pair's copies are all counted by its first CTA, whose thread issues the products
             const uint32_t bar = PAIR ? cluster_map(smem_u32(&full_bar[s]), 0) : smem_u32(&full_bar[s]);
+            if (it == 0) pdl_wait();
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
               const int r = rA + j * 64;
@@ -437,6 +440,7 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
     }
   } else {
     // epilogue: warp w may touch TMEM lanes 32*(w%4) .. +31; the four warps of a quadrant split the columns
+    pdl_wait();
     const int quad = warp & 3, sub = (warp - 2) >> 2;
     unsigned char* buf = tiles + (size_t)STAGES * STAGE_BYTES + (size_t)(warp - 2) * PIECE_BYTES;
     uint64_t* bar = &src_bar[warp - 2];

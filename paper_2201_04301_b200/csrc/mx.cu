@@ -570,7 +570,6 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
   tc_fence_after();
   const uint32_t tmem_base = tmem_base_sm;
   pdl_launch_dependents();
-  pdl_wait();
   const bool leader = elect_one();
 
   if (warp == 0) {
@@ -587,6 +586,7 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
           unsigned char* sa = tiles + (size_t)s * T::STAGE_BYTES;
           if (!PAIR || rank == 0) mbar_expect_tx(&full_bar[s], (PAIR ? 2 : 1) * T::STAGE_BYTES);
           const uint32_t bar = PAIR ? cluster_map(smem_u32(&full_bar[s]), 0) : smem_u32(&full_bar[s]);
+          if (it == 0) pdl_wait();  // here and not earlier: the first run of what lies before costs as much as a copy
           tma_load_2d_to<PAIR>(sa, &tmA, kb * (KB / 2), rA, bar);
           tma_load_2d_to<PAIR>(sa + BM * (KB / 2), &tmB, kb * (KB / 2), rB, bar);
           // scale tiles are rows of their maps; one behind the end (its columns are not kept) arrives as zeros
@@ -645,6 +645,7 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
   } else {
     const int quad = warp & 3, sub = (warp - 2) >> 2;
     bool ok = true;
+    pdl_wait();
     for (int i = 0; i < n_local; ++i) {
       const int slot = i % T::ACC;
       const int u = first + i * stride, mt = u / tiles_n, nt = u - mt * tiles_n;
