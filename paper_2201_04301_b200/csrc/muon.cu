@@ -32,11 +32,21 @@ namespace {
 constexpr int TR = 128, BK = 64;                       // rows of an operand block; K values of a stage
 constexpr int BLK_BYTES = 64 * BK * 2;                 // one copy box: 64 x 64 fp16
 constexpr int OP_BYTES = TR * BK * 2;                  // one operand block: 16 KiB
-constexpr int STAGE_BYTES = 2 * OP_BYTES;
-constexpr int STAGES = 4;                              // even: a stage of hi parts is followed by its lo parts
 constexpr int EPI_WARPS = 16;                          // four to a quadrant of tensor memory's lanes
 constexpr int THREADS = 64 + 32 * EPI_WARPS;
-constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + EPI_WARPS * 4096 + 1024;
+constexpr int PW = 16;                                 // columns of an epilogue piece
+constexpr int PIECE_BYTES = PW * 128;
+// Shared memory: stages and an epilogue buffer a warp.  A stage holds a K block of A and B; FULL, its hi and its lo parts:
+// a stage costs the issuing thread 320 cycles beside its products (1024 x 1024 187 us with hi and lo parts apart, 174
+// so; two K blocks in HALF's stages gained nothing and made short products wait longer, 81 against 77 us at 200 x 784).
+template <int TN, bool FULL>
+struct Smem {
+  static constexpr int BLOCK_BYTES = OP_BYTES + (TN == 256 ? 128 : TN) * BK * 2, STAGE_BYTES = (FULL ? 2 : 1) * BLOCK_BYTES;
+  static constexpr int STAGES = (TN == 64 ? 8 : 6) / (FULL ? 2 : 1);
+  static constexpr int BYTES = STAGES * STAGE_BYTES + EPI_WARPS * PIECE_BYTES + 1024;
+  static_assert(BYTES <= 226 * 1024, "with the barriers, what an SM has");
+  static_assert(TN == 256 || TN * TR * 4 <= STAGES * STAGE_BYTES, "a partial tile lies in the stages");
+};
 constexpr float SCALE = 1024.f;                        // stored value = SCALE * matrix element
 constexpr float INV_SCALE = 1.f / 1024.f;
 constexpr int NORM_BLOCKS = 1184;                      // partial sums of a matrix's squared norm
@@ -133,16 +143,14 @@ __device__ __forceinline__ Coef coefficients(const NsGemm& a, int b) {
 // its warp: the linear term's hi and lo parts arrive there by a tensor copy, the results take their place and leave
 // the same way.  (With a thread reading and writing its own row in global memory every access of a warp touches 32
 // lines, and those 32 cycles each were what a short product spent most of its time on.)
-constexpr int PIECE_BYTES = 4096;  // 32 columns' hi and lo parts; the lo part follows the hi part, PW * 64 bytes
-// Byte of 16-byte chunk `ch` of `row` in a plane as the copies lay it out (64- or 32-byte swizzle) ...
-template <int PW>
+// The lo part follows the hi part, PW * 64 bytes.
+// Byte of 16-byte chunk `ch` of `row` in a part as the copies lay it out (32-byte swizzle) ...
 __device__ __forceinline__ int plane_at(int row, int ch) {
-  return PW == 32 ? row * 64 + ((ch ^ ((row >> 1) & 3)) << 4) : row * 32 + ((ch ^ ((row >> 2) & 1)) << 4);
+  return row * 32 + ((ch ^ ((row >> 2) & 1)) << 4);
 }
 // ... and in a piece of floats on its way to the user's matrix.
-template <int PW>
 __device__ __forceinline__ int float_at(int row, int ch) {
-  return PW == 32 ? row * 128 + ((ch ^ (row & 7)) << 4) : row * 64 + ((ch ^ ((row >> 1) & 3)) << 4);
+  return row * 64 + ((ch ^ ((row >> 1) & 3)) << 4);
 }
 
 __device__ __forceinline__ bool kept(const NsGemm& a, int m, int n) {  // whether a piece at (m, n) exists and is stored
@@ -150,7 +158,6 @@ __device__ __forceinline__ bool kept(const NsGemm& a, int m, int n) {  // whethe
 }
 
 // One lane: the hi and lo parts of the piece at (m, n) into the buffer, once what left it before has been read.
-template <int PW>
 __device__ __forceinline__ void fetch_piece(const CUtensorMap* tm, unsigned char* buf, uint64_t* bar, int m, int n, int b) {
   bulk_wait_read();
   mbar_expect_tx(bar, 2 * 32 * PW * 2);
@@ -160,14 +167,13 @@ __device__ __forceinline__ void fetch_piece(const CUtensorMap* tm, unsigned char
 __device__ __forceinline__ NsTarget target_of(const NsSink& s) { return s.at ? *s.at : s.to; }
 
 // A warp: f holds row m0 + lane, columns n .. n + PW - 1 of the products' sums.
-template <int PW>
 __device__ __forceinline__ void finish_piece(const NsGemm& a, const CUtensorMap* tmD, const Coef& k, unsigned char* buf, int lane,
                                              bool leader, int m0, int n, int b, float (&f)[PW]) {
 #pragma unroll
   for (int c = 0; c < PW / 8; ++c) {
     if (a.src) {
-      const uint4 h = *reinterpret_cast<const uint4*>(buf + plane_at<PW>(lane, c));
-      const uint4 l = *reinterpret_cast<const uint4*>(buf + PW * 64 + plane_at<PW>(lane, c));
+      const uint4 h = *reinterpret_cast<const uint4*>(buf + plane_at(lane, c));
+      const uint4 l = *reinterpret_cast<const uint4*>(buf + PW * 64 + plane_at(lane, c));
       const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, lw[4] = {l.x, l.y, l.z, l.w};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -201,8 +207,8 @@ __device__ __forceinline__ void finish_piece(const NsGemm& a, const CUtensorMap*
         const float2 r = unpack_half2(h[j]);
         l[j] = pack_half2(x - r.x, y - r.y);
       }
-      *reinterpret_cast<uint4*>(buf + plane_at<PW>(lane, c)) = make_uint4(h[0], h[1], h[2], h[3]);
-      if (a.write_lo) *reinterpret_cast<uint4*>(buf + PW * 64 + plane_at<PW>(lane, c)) = make_uint4(l[0], l[1], l[2], l[3]);
+      *reinterpret_cast<uint4*>(buf + plane_at(lane, c)) = make_uint4(h[0], h[1], h[2], h[3]);
+      if (a.write_lo) *reinterpret_cast<uint4*>(buf + PW * 64 + plane_at(lane, c)) = make_uint4(l[0], l[1], l[2], l[3]);
     }
     fence_async_shared();
     __syncwarp();
@@ -216,7 +222,7 @@ __device__ __forceinline__ void finish_piece(const NsGemm& a, const CUtensorMap*
   __syncwarp();
 #pragma unroll
   for (int c = 0; c < PW / 4; ++c)
-    *reinterpret_cast<float4*>(buf + float_at<PW>(lane, c)) = make_float4(f[4 * c], f[4 * c + 1], f[4 * c + 2], f[4 * c + 3]);
+    *reinterpret_cast<float4*>(buf + float_at(lane, c)) = make_float4(f[4 * c], f[4 * c + 1], f[4 * c + 2], f[4 * c + 3]);
   __syncwarp();
   constexpr int CH = PW / 4, RPP = 32 / CH;  // chunks of a row, rows of a pass
   const bool f32 = a.out == OUT_F32 || a.out == OUT_UPDATE_F32, upd = a.out == OUT_UPDATE_F32 || a.out == OUT_UPDATE_BF16;
@@ -226,7 +232,7 @@ __device__ __forceinline__ void finish_piece(const NsGemm& a, const CUtensorMap*
   for (int r0 = 0; r0 < 32; r0 += RPP) {
     const int row = r0 + lane / CH, m = m0 + row;
     if (m >= a.M || col >= a.N) continue;
-    const float4 v4 = *reinterpret_cast<const float4*>(buf + float_at<PW>(row, ch));
+    const float4 v4 = *reinterpret_cast<const float4*>(buf + float_at(row, ch));
     float v[4] = {v4.x, v4.y, v4.z, v4.w};
     const long long at = (long long)b * a.user.stride + (long long)m * a.user.ld + col;
     if (f32) {
@@ -271,31 +277,30 @@ __device__ __forceinline__ void finish_piece(const NsGemm& a, const CUtensorMap*
 }
 
 // One product.  Warp 0 copies operand blocks (128 rows or columns x 64 K values) into a ring of stages, warp 1
-// issues the tcgen05 products into one of two accumulators, eight warps finish the other one.
+// issues the tcgen05 products into one of two accumulators, sixteen warps finish the other one.
 //   PAIR (TN = 256): the two CTAs of a cluster work on one 256 x 256 tile (cta_group::2): each holds 128 rows of A, 128 of the
 //         256 columns of B and 128 rows of the result, so a stage of 32 KiB feeds 512 cycles of the tensor core: 64
 //         bytes a cycle, what an SM can take from L2.  (A single CTA's 128 x 256 tile needs 94.)
 //   else: a CTA has its own 128 x TN tile and, when there are fewer tiles than SMs, shares its K range with the
 //         other CTAs of its cluster: each leaves its partial tile in shared memory and adds up (in rank order) the
 //         columns that fall to it.
-// FULL: stages alternate between hi and lo parts, three products for each pair; the sum of `chunk` pairs moves to
-// registers, because the tensor cores cut (not round) each partial sum.
 //         Tiles of 64 columns leave an epilogue warp 16 of them instead of 32, and a K block costs 24 KiB: for results of
 //         so few tiles that it is their number that counts.
+// FULL: three products for each K block's pairs of parts; the sum of `chunk` blocks moves to registers, because the tensor
+// cores cut (not round) each partial sum.
 template <int TN, bool FULL>
 __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_constant__ CUtensorMap tmA,
                                                              const __grid_constant__ CUtensorMap tmB,
                                                              const __grid_constant__ CUtensorMap tmS,
                                                              const __grid_constant__ CUtensorMap tmD, const NsGemm a) {
+  constexpr int STAGES = Smem<TN, FULL>::STAGES, STAGE_BYTES = Smem<TN, FULL>::STAGE_BYTES, BLOCK_BYTES = Smem<TN, FULL>::BLOCK_BYTES;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   __shared__ uint64_t full_bar[STAGES], empty_bar[STAGES], tfull_bar[2], tempty_bar[2], src_bar[EPI_WARPS];
   __shared__ uint32_t tmem_base_sm;
   constexpr bool PAIR = TN == 256;
   constexpr int TM = PAIR ? 256 : 128, RATIO = TM / TN;
   constexpr int B_ROWS = PAIR ? 128 : TN;        // columns of B that this CTA copies
-  constexpr int STAGE_USED = OP_BYTES + B_ROWS * BK * 2;
   constexpr int WCOLS = TN / 4;                  // columns of an epilogue warp ...
-  constexpr int PW = WCOLS < 32 ? WCOLS : 32;    // ... and of a piece
   constexpr uint32_t TMEM_COLS = 2 * TN;
   unsigned char* tiles = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -347,7 +352,9 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
   if (warp == 0) {
     if (leader) {
       bool ok = true;
-      int it = 0;
+      bool waited = false;
+      int s = 0;  // the stage, and the parity of its turn
+      uint32_t ph = 0;
       const int sym_log = a.sym_log;
       const bool a_mn = a.a_mn, a_sym = a.a_sym, b_mn = a.b_mn, b_sym = a.b_sym;
       for (int u = first; u < total && ok; u += stride) {
@@ -355,19 +362,20 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
         int mt, nt;
         tile_of(u - b * per, tiles_n, a.sym, g_tiles, RATIO, mt, nt);
         const int rA = PAIR ? mt * 256 + rank * 128 : mt * 128, rB = PAIR ? nt * 256 + rank * 128 : nt * TN;
-        for (int kb = kb0; kb < kb1 && ok; ++kb) {
-          const int kblk = kb * BK >> sym_log;
+          for (int kb = kb0; kb < kb1; ++kb) {
+          const int kc = kb * BK, kblk = kc >> sym_log;
           const bool mnA = a_mn || (a_sym && kblk < rA >> sym_log), mnB = b_mn || (b_sym && kblk < rB >> sym_log);
+          ok = mbar_spin_bounded(&empty_bar[s], ph ^ 1u);
+          if (!ok) break;
+          if (!PAIR || rank == 0) mbar_expect_tx(&full_bar[s], (PAIR ? 2 : 1) * STAGE_BYTES);
+          // a pair's copies are all counted by its first CTA, whose thread issues the products
+          const uint32_t bar = PAIR ? cluster_map(smem_u32(&full_bar[s]), 0) : smem_u32(&full_bar[s]);
+          if (!waited) pdl_wait();
+          waited = true;
 #pragma unroll
-          for (int t = 0; t < (FULL ? 2 : 1); ++t, ++it) {  // plane 0 = hi, 1 = lo
-            const int s = it % STAGES, kc = kb * BK, z = 2 * b + t;
-            ok = mbar_spin_bounded(&empty_bar[s], (uint32_t)(((it / STAGES) & 1) ^ 1));
-            if (!ok) break;
-            unsigned char* sa = tiles + (size_t)s * STAGE_BYTES;
-            if (!PAIR || rank == 0) mbar_expect_tx(&full_bar[s], PAIR ? 2 * STAGE_USED : STAGE_USED);
-            // a pair's copies are all counted by its first CTA, whose thread issues the products
-            const uint32_t bar = PAIR ? cluster_map(smem_u32(&full_bar[s]), 0) : smem_u32(&full_bar[s]);
-            if (it == 0) pdl_wait();
+          for (int t = 0; t < (FULL ? 2 : 1); ++t) {
+            const int z = 2 * b + t;  // plane 0 = hi, 1 = lo
+            unsigned char* sa = tiles + (size_t)s * STAGE_BYTES + t * BLOCK_BYTES;
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
               const int r = rA + j * 64;
@@ -379,6 +387,7 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
               tma_load_3d_to<PAIR>(sa + OP_BYTES + j * BLK_BYTES, &tmB, mnB ? r : kc, mnB ? kc : r, z, bar);
             }
           }
+          if (++s == STAGES) s = 0, ph ^= 1u;
         }
       }
       if (!ok) raise_error(a.err);
@@ -388,7 +397,8 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
       // fp16 operands, fp32 sum
       constexpr uint32_t IDESC = (1u << 4) | ((uint32_t)(TN >> 3) << 17) | ((uint32_t)(TM >> 4) << 24);
       bool ok = true;
-      int it = 0, acc_no = 0;
+      int acc_no = 0, s = 0;
+      uint32_t ph = 0;
       const int sym_log = a.sym_log;
       const bool a_mn = a.a_mn, a_sym = a.a_sym, b_mn = a.b_mn, b_sym = a.b_sym;
       for (int u = first; u < total && ok; u += stride) {
@@ -403,35 +413,29 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
           tc_fence_after();
           const uint32_t d = tmem_base + (uint32_t)(slot * TN);
           const int n = FULL ? (c == chunks - 1 ? nkb - c * a.chunk : a.chunk) : nkb;
-          for (int kb = 0; kb < n && ok; ++kb) {
+          for (int kb = 0; kb < n; ++kb) {
             const int kblk = (kb0 + (FULL ? c * a.chunk : 0) + kb) * BK >> sym_log;
             const bool mnA = a_mn || (a_sym && kblk < blkA), mnB = b_mn || (b_sym && kblk < blkB);
             const uint32_t idesc = IDESC | (mnA ? 1u << 15 : 0u) | (mnB ? 1u << 16 : 0u);
             const uint64_t ka = mnA ? 128u : 2u, kk_b = mnB ? 128u : 2u;  // descriptor step of 16 K values
-            uint64_t da[2], db[2];
-            int st[2];
-#pragma unroll
-            for (int t = 0; t < (FULL ? 2 : 1); ++t, ++it) {
-              const int s = it % STAGES;
-              st[t] = s;
-              ok = ok && mbar_spin_bounded(&full_bar[s], (uint32_t)((it / STAGES) & 1));
-              const uint32_t sa = smem_u32(tiles + (size_t)s * STAGE_BYTES);
-              da[t] = mnA ? make_desc_mn(sa) : make_desc(sa);
-              db[t] = mnB ? make_desc_mn(sa + OP_BYTES) : make_desc(sa + OP_BYTES);
-            }
+            const uint32_t sa = smem_u32(tiles + (size_t)s * STAGE_BYTES);
+            const uint64_t da = mnA ? make_desc_mn(sa) : make_desc(sa);
+            const uint64_t db = mnB ? make_desc_mn(sa + OP_BYTES) : make_desc(sa + OP_BYTES);
+            ok = mbar_spin_bounded(&full_bar[s], ph);
             if (!ok) break;
             tc_fence_after();
             if (FULL) {  // the smallest products first
+              constexpr uint64_t LO = BLOCK_BYTES >> 4;  // from the hi to the lo part
 #pragma unroll
-              for (int kk = 0; kk < BK / 16; ++kk) tc_mma<PAIR>(d, da[1] + kk * ka, db[0] + kk * kk_b, idesc, (kb | kk) != 0 ? 1u : 0u);
+              for (int kk = 0; kk < BK / 16; ++kk) tc_mma<PAIR>(d, da + LO + kk * ka, db + kk * kk_b, idesc, (kb | kk) != 0 ? 1u : 0u);
 #pragma unroll
-              for (int kk = 0; kk < BK / 16; ++kk) tc_mma<PAIR>(d, da[0] + kk * ka, db[1] + kk * kk_b, idesc, 1u);
-              tc_commit_to<PAIR>(&empty_bar[st[1]]);
+              for (int kk = 0; kk < BK / 16; ++kk) tc_mma<PAIR>(d, da + kk * ka, db + LO + kk * kk_b, idesc, 1u);
             }
 #pragma unroll
             for (int kk = 0; kk < BK / 16; ++kk)
-              tc_mma<PAIR>(d, da[0] + kk * ka, db[0] + kk * kk_b, idesc, FULL || (kb | kk) != 0 ? 1u : 0u);
-            tc_commit_to<PAIR>(&empty_bar[st[0]]);
+              tc_mma<PAIR>(d, da + kk * ka, db + kk * kk_b, idesc, FULL || (kb | kk) != 0 ? 1u : 0u);
+            tc_commit_to<PAIR>(&empty_bar[s]);
+            if (++s == STAGES) s = 0, ph ^= 1u;
           }
           if (ok) tc_commit_to<PAIR>(&tfull_bar[slot]);
         }
@@ -454,7 +458,7 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
       tile_of(u - b * per, tiles_n, a.sym, g_tiles, RATIO, mt, nt);
       const int m0 = mt * TM + (PAIR ? rank * 128 : 0) + quad * 32, c0 = sub * WCOLS, n0 = nt * TN + c0;
       // the linear term does not depend on the products: the first piece's is on its way while those are formed
-      if (direct && a.src && leader && kept(a, m0, n0)) fetch_piece<PW>(&tmS, buf, bar, m0, n0, b);
+      if (direct && a.src && leader && kept(a, m0, n0)) fetch_piece(&tmS, buf, bar, m0, n0, b);
       const Coef k = coefficients(a, b);
       float sum[FULL ? WCOLS : 1];
       for (int c = 0; c < chunks; ++c, ++acc_no) {
@@ -483,10 +487,7 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
 #pragma unroll 1
           for (int q = 0; q < WCOLS; q += PW) {
             uint32_t v[PW];
-            if constexpr (PW == 32)
-              tc_ld32_issue(tbase + (uint32_t)q, v);
-            else
-              tc_ld16_issue(tbase + (uint32_t)q, v);
+            tc_ld16_issue(tbase + (uint32_t)q, v);
             tc_ld_wait();
             if (!direct) {
               float* part = reinterpret_cast<float*>(tiles) + (size_t)(c0 + q) * TR + quad * 32 + lane;
@@ -496,14 +497,14 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
             }
             if (!kept(a, m0, n0 + q)) continue;
             if (a.src) {
-              if (q && leader) fetch_piece<PW>(&tmS, buf, bar, m0, n0 + q, b);
+              if (q && leader) fetch_piece(&tmS, buf, bar, m0, n0 + q, b);
               ok = __all_sync(0xffffffffu, mbar_wait_bounded(bar, fetched++ & 1u));
               if (!ok) break;
             }
             float f[PW];
 #pragma unroll
             for (int j = 0; j < PW; ++j) f[j] = __uint_as_float(v[j]);
-            finish_piece<PW>(a, &tmD, k, buf, lane, leader, m0, n0 + q, b, f);
+            finish_piece(a, &tmD, k, buf, lane, leader, m0, n0 + q, b, f);
           }
         }
         tc_fence_before();
@@ -527,7 +528,7 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
     const int m0 = mt * TM + quad * 32, n = nt * TN + c;
     const bool mine = warp >= 2 && c < TN && kept(a, m0, n);
     unsigned char* buf = tiles + (size_t)STAGES * STAGE_BYTES + (size_t)(warp - 2) * PIECE_BYTES;
-    if (mine && a.src && leader) fetch_piece<16>(&tmS, buf, &src_bar[warp - 2], m0, n, b);
+    if (mine && a.src && leader) fetch_piece(&tmS, buf, &src_bar[warp - 2], m0, n, b);
     // the partial tiles are complete (every stage had been consumed before they were written)
     __syncwarp();
     cluster_sync();
@@ -558,7 +559,7 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
       bool ok = true;
       if (a.src) ok = __all_sync(0xffffffffu, mbar_wait_bounded(&src_bar[warp - 2], 0));
       if (ok)
-        finish_piece<16>(a, &tmD, coefficients(a, b), buf, lane, leader, m0, n, b, f);
+        finish_piece(a, &tmD, coefficients(a, b), buf, lane, leader, m0, n, b, f);
       else if (leader)
         raise_error(a.err);
     }
@@ -712,8 +713,8 @@ __global__ void __launch_bounds__(256) ns_copy_kernel(const NsGemm a) {
 
 // ----------------------------------------------------------------- host
 // fp16 array [planes][rows][cols], row stride ld elements, zero fill outside; boxes of 64 columns x 64 rows with the
-// 128-byte swizzle (operands), or 32 or 16 columns x 32 rows with the 64- or 32-byte one, hi and lo parts
-// in one box where `parts` is 2 (epilogue pieces).
+// 128-byte swizzle (operands), or 16 columns x 32 rows with the 32-byte one, hi and lo parts in one box where `parts` is 2
+// (epilogue pieces).
 bool make_map_f16(CUtensorMap* tm, const void* base, long long cols, long long rows, long long planes, long long ld,
                   long long plane, int width = 64, int parts = 1) {
   EncodeTiledFn fn = encode_fn();
@@ -724,7 +725,7 @@ bool make_map_f16(CUtensorMap* tm, const void* base, long long cols, long long r
   cuuint32_t es[3] = {1, 1, 1};
   return fn(tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(base), dims, strides, box, es,
             CU_TENSOR_MAP_INTERLEAVE_NONE,
-            width == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : width == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B,
+            width == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_32B,
             CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -762,12 +763,12 @@ NsLayout layout(int batch, int rows, int cols) {
 
 cudaError_t set_attributes() {
   const cudaFuncAttribute at = cudaFuncAttributeMaxDynamicSharedMemorySize;
-  cudaError_t e = cudaFuncSetAttribute(ns_gemm_kernel<256, true>, at, SMEM_BYTES);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<256, false>, at, SMEM_BYTES);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<128, true>, at, SMEM_BYTES);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<128, false>, at, SMEM_BYTES);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<64, true>, at, SMEM_BYTES);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<64, false>, at, SMEM_BYTES);
+  cudaError_t e = cudaFuncSetAttribute(ns_gemm_kernel<256, true>, at, Smem<256, true>::BYTES);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<256, false>, at, Smem<256, false>::BYTES);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<128, true>, at, Smem<128, true>::BYTES);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<128, false>, at, Smem<128, false>::BYTES);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<64, true>, at, Smem<64, true>::BYTES);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<64, false>, at, Smem<64, false>::BYTES);
   if (e == cudaSuccess) e = ns_cluster_set_attributes();
   return e;
 }
@@ -776,14 +777,13 @@ template <int TN, bool FULL>
 cudaError_t launch_shape(const CUtensorMap& ta, const CUtensorMap& tb, const NsGemm& a, int ctas, cudaStream_t st) {
   CUtensorMap ts = ta, td = ta;  // the epilogue's pieces; not used where there is no linear term or a user's matrix
   constexpr bool PAIR = TN == 256;
-  const int width = TN >= 128 && a.split == 1 ? 32 : 16;
-  if ((a.src && !make_map_f16(&ts, a.src, a.N, a.M, 2LL * a.batch, a.ld_src, a.src_plane, width, 2)) ||
-      (a.out == OUT_SPLIT && !make_map_f16(&td, a.dst, a.N, a.M, 2LL * a.batch, a.ld_dst, a.dst_plane, width, a.write_lo ? 2 : 1)))
+  if ((a.src && !make_map_f16(&ts, a.src, a.N, a.M, 2LL * a.batch, a.ld_src, a.src_plane, PW, 2)) ||
+      (a.out == OUT_SPLIT && !make_map_f16(&td, a.dst, a.N, a.M, 2LL * a.batch, a.ld_dst, a.dst_plane, PW, a.write_lo ? 2 : 1)))
     return cudaErrorInvalidValue;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)ctas);
   cfg.blockDim = dim3(THREADS);
-  cfg.dynamicSmemBytes = SMEM_BYTES;
+  cfg.dynamicSmemBytes = Smem<TN, FULL>::BYTES;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
