@@ -810,7 +810,7 @@ Shape choose_shape(int M, int N, int K, int sym, int g, int batch, int full, int
   const int kb = (K + BK - 1) / BK;
   const long long pairs = shape_tiles(M, N, sym, g, batch, 256);
   Shape s{256, 1};
-  double cost = (double)((pairs + sms / 2 - 1) / (sms / 2)) * kb * (full ? 3 : 1) + 14;
+  double cost = (double)((pairs + sms / 2 - 1) / (sms / 2)) * kb * (full ? 3 : 1) + (full ? 18 : 14);
   for (int tn = 128; tn >= 64; tn -= 64) {
     const long long t = shape_tiles(M, N, sym, g, batch, tn);
     const double block = (tn == 128 ? 1.0 : 0.75) * (full ? 2 : 1), ramp = tn == 128 ? 6 : 4;
