@@ -457,6 +457,83 @@ def test_product_streams_and_graphs():
     assert torch.equal(out, -2 * want)
 
 
+@pytest.mark.gpu
+def test_calls_on_two_streams_at_once():
+    """Chains of large and small calls side by side, each with its own work area, then two captured chains replayed
+    side by side: the same bits as one after the other."""
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    mats = [torch.randn(s, generator=gen, device="cuda").to(t) for s in ((300, 900), (40, 200), (2, 520, 260), (10, 90))
+            for t in (torch.float32, torch.bfloat16)]
+    x, w = torch.randn(200, 640, generator=gen, device="cuda"), torch.randn(333, 640, generator=gen, device="cuda")
+    b = binding.mx_quantize(w)
+
+    def chain(order, outs, works):
+        for i in order:
+            binding.orthogonalize(mats[i], out=outs[i], work=works[i])
+            binding.mx_gemm(binding.mx_quantize(x), b, out=outs[-1])
+
+    def buffers():
+        return ([torch.zeros_like(g) for g in mats] + [torch.zeros(200, 333, device="cuda")],
+                [torch.empty(binding.orthogonalize_work(g), dtype=torch.uint8, device="cuda") for g in mats])
+
+    want, works = buffers()
+    chain(range(len(mats)), want, works)
+    torch.cuda.synchronize()
+    sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+    orders = [list(range(len(mats))), list(reversed(range(len(mats))))]
+    places = [buffers(), buffers()]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for side, order, place in zip(sides, orders, places):
+            with torch.cuda.stream(side):
+                chain(order, *place)
+    torch.cuda.synchronize()
+    for outs, _ in places:
+        assert all(torch.equal(o, r) for o, r in zip(outs, want))
+    graphs = []
+    for order, (outs, works) in zip(orders, places):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            chain(order, outs, works)
+        for o in outs:
+            o.zero_()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for side, graph in zip(sides, graphs):
+            with torch.cuda.stream(side):
+                graph.replay()
+    torch.cuda.synchronize()
+    for outs, _ in places:
+        assert all(torch.equal(o, r) for o, r in zip(outs, want))
+    binding.check_operators()
+
+
+@pytest.mark.gpu
+def test_rows_whose_offsets_pass_32_bits():
+    rows, cols, ld = 70, 130, 36_000_000                       # the last row starts 2.5e9 elements behind the first
+    far = torch.empty(rows * ld, dtype=torch.bfloat16, device="cuda")
+    g = far.as_strided((rows, cols), (ld, 1))
+    out = far.as_strided((rows, cols), (ld, 1), 1001)
+    g.copy_(torch.from_numpy(spectrum(rows, cols, "gauss")))
+    near = g.contiguous()
+    binding.orthogonalize(g, out=out)
+    assert torch.equal(out, binding.orthogonalize(near))
+    q = binding.mx_quantize(near)
+    far_q = binding.mx_quantize(g)
+    assert torch.equal(far_q.codes, q.codes) and torch.equal(far_q.scales, q.scales)
+    assert torch.equal(binding.mx_quantize(g, transpose=True).codes, binding.mx_quantize(near, transpose=True).codes)
+    q.dequantize(out=out)
+    assert torch.equal(out, q.dequantize(torch.bfloat16))
+    binding.mx_gemm(q, q, out=far.as_strided((rows, rows), (ld, 1), 2000))
+    assert torch.equal(far.as_strided((rows, rows), (ld, 1), 2000), binding.mx_gemm(q, q, dtype=torch.bfloat16))
+    m = torch.zeros(rows, cols, device="cuda")
+    w, w2, m2 = out, out.contiguous(), m.clone()
+    binding.muon_update(w, m, g, lr=0.1)
+    binding.muon_update(w2, m2, near, lr=0.1)
+    assert torch.equal(w, w2) and torch.equal(m, m2)
+    binding.check_operators()
+
+
 # ------------------------------------------------------------------------------------------- together
 @pytest.mark.gpu
 def test_an_iteration_of_the_server():
