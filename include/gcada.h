@@ -353,7 +353,7 @@ gcada_status gcada_innovation_norms_noalloc(const float *fresh_dev, const float 
  * GCADA_EINVAL unless 0 <= steps <= 100, |a|, |b|, |c| <= 16, 1e-30 <= eps <= 1e30, rows, cols <= 2^20, batch <=
  * 65535, the results do not overlap, and work_dev is 256-byte aligned with at least the bytes that
  * gcada_orthogonalize_work gives (256 means that the area is not used: matrices with a short side of up to 64 stay
- * on chip while their long side fits).
+ * on chip while they and their batch are small).
  */
 gcada_status gcada_orthogonalize_work(int batch, int rows, int cols, size_t *bytes);
 gcada_status gcada_orthogonalize(const void *g_dev, void *o_dev, int type, int batch, int rows, int cols,

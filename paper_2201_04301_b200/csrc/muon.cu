@@ -279,8 +279,8 @@ __device__ __forceinline__ void finish_piece(const NsGemm& a, const CUtensorMap*
 // One product.  Warp 0 copies operand blocks (128 rows or columns x 64 K values) into a ring of stages, warp 1
 // issues the tcgen05 products into one of two accumulators, sixteen warps finish the other one.
 //   PAIR (TN = 256): the two CTAs of a cluster work on one 256 x 256 tile (cta_group::2): each holds 128 rows of A, 128 of the
-//         256 columns of B and 128 rows of the result, so a stage of 32 KiB feeds 512 cycles of the tensor core: 64
-//         bytes a cycle, what an SM can take from L2.  (A single CTA's 128 x 256 tile needs 94.)
+//         256 columns of B and 128 rows of the result, so a stage of 32 KiB feeds 512 cycles of the tensor core, 64
+//         bytes a cycle.  (A single CTA's 128 x 256 tile needs 94: 4096 x 4096 took 1.72 ms so, 1.24 in pairs at the time.)
 //   else: a CTA has its own 128 x TN tile and, when there are fewer tiles than SMs, shares its K range with the
 //         other CTAs of its cluster: each leaves its partial tile in shared memory and adds up (in rank order) the
 //         columns that fall to it.
@@ -300,7 +300,7 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
   constexpr bool PAIR = TN == 256;
   constexpr int TM = PAIR ? 256 : 128, RATIO = TM / TN;
   constexpr int B_ROWS = PAIR ? 128 : TN;        // columns of B that this CTA copies
-  constexpr int WCOLS = TN / 4;                  // columns of an epilogue warp ...
+  constexpr int WCOLS = TN / 4;                  // columns of an epilogue warp
   constexpr uint32_t TMEM_COLS = 2 * TN;
   unsigned char* tiles = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -796,9 +796,10 @@ cudaError_t launch_shape(const CUtensorMap& ta, const CUtensorMap& tb, const NsG
   return cudaLaunchKernelEx(&cfg, ns_gemm_kernel<TN, FULL>, ta, tb, ts, td, a);
 }
 
-// The shape with the least work in sequence, in units of 512 cycles, what 32 KiB from L2 take an SM: a K block of a
-// pair's tile or of 128 x 128 is one, of 128 x 64 three quarters (FULL twice that, and a pair's products, 1536 cycles a
-// block, then outlast its copies); filling and draining a tile, and adding up a split one, are counted as measured.
+// The shape with the least work in sequence, in units of 512 cycles: a K block of a pair's tile takes about one (measured
+// 530 to 580 cycles), as does one of 128 x 128 (410 to 580), one of 128 x 64 three quarters (390 to 490); FULL twice that
+// (1100 to 1400 and 940 to 1090), but three times for a pair, which its products then bound (1500 to 1700).  Filling and
+// draining a tile, and adding up a split one, are counted as measured.
 struct Shape {
   int tn, split;
 };
@@ -830,8 +831,8 @@ cudaError_t launch_ns_gemm(const CUtensorMap& ta, const CUtensorMap& tb, NsGemm 
                            cudaStream_t st) {
   // The tensor cores cut each of a chunk's partial sums, an error that grows with their number and, like fp32's own
   // rounding, weighs less in longer sums.  Error of the result, time, with 4 / 2 / 1 blocks a chunk (fp32 arithmetic
-  // 1.5e-6, 2.4e-6, 2.6e-6): 200 x 784 3.5e-6 2.2e-6 1.4e-6, 140 143 147 us; 1024 x 1024 2.6e-6 1.2e-6 0.6e-6,
-  // 210 214 225 us; 4096 x 4096 1.2e-6 0.7e-6 0.5e-6, 4.0 4.4 6.0 ms.
+  // 1.5e-6, 2.4e-6, 2.6e-6): 200 x 784 3.5e-6 2.2e-6 1.4e-6, 97 99 101 us; 1024 x 1024 2.6e-6 1.2e-6 0.6e-6,
+  // 165 174 190 us; 4096 x 4096 1.2e-6 0.7e-6 0.5e-6, 3.3 3.6 4.1 ms.
   a.chunk_log = a.K <= 512 ? 0 : a.K <= 2048 ? 1 : 2;
   a.chunk = 1 << a.chunk_log;
   a.split = s.split;
@@ -847,10 +848,13 @@ cudaError_t launch_ns_gemm(const CUtensorMap& ta, const CUtensorMap& tb, NsGemm 
 
 }  // namespace
 
-int ns_launches(int rows, int cols, int steps) { return ns_fits_cluster(rows, cols) ? 1 : 2 + (steps ? 3 * steps : 1); }
+int ns_launches(int rows, int cols, int steps, bool full) {
+  return ns_fits_cluster(1, rows, cols, full) ? 1 : 2 + (steps ? 3 * steps : 1);
+}
 
 size_t ns_work_bytes(int batch, int rows, int cols) {
-  return ns_fits_cluster(rows, cols) ? 256 : layout(batch, rows, cols).bytes;
+  // HALF leaves the chip first
+  return ns_fits_cluster(batch, rows, cols, false) ? 256 : layout(batch, rows, cols).bytes;
 }
 
 // Everything an orthogonalisation enqueues.  `why` names the step that failed.
@@ -873,9 +877,9 @@ cudaError_t ns_run(const NsProblem& p, void* work, cudaStream_t st, const char**
   s.rows = p.rows;
   s.cols = p.cols;
   const NsSink sink{{p.o, p.prev, (float)p.decay, (float)p.step}, p.ld_o, p.stride_o, p.o_bf16, p.w_update, p.at};
-  if (ns_fits_cluster(p.rows, p.cols)) {
+  if (ns_fits_cluster(p.batch, p.rows, p.cols, p.full)) {
     const float coef[3] = {(float)p.coef[0], (float)p.coef[1], (float)p.coef[2]};
-    if ((e = launch_ns_cluster(s, sink, p.batch, coef, p.steps, p.eps, st)) != cudaSuccess) *why = "kernel launch";
+    if ((e = launch_ns_cluster(s, sink, p.batch, p.full, coef, p.steps, p.eps, st)) != cudaSuccess) *why = "kernel launch";
     if (launches) *launches = 1;
     return e;
   }

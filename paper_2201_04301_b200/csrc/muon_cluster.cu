@@ -4,8 +4,8 @@
 // A step: every CTA forms its slice's share of A = X X^T; cluster barrier; A is added up from all shares through
 // distributed shared memory, in rank order (bitwise reproducible); every CTA forms b A + c A^2 for itself and applies
 // it to its slice.  Bound: latency - each phase is about a thousand cycles of dependent loads, FMAs and a barrier for
-// narrow matrices, some thousands for 64 rows.  As separate tensor-core launches the same steps cost 4 to 5 us per
-// product however small it is.
+// narrow matrices, some thousands for 64 rows.  As separate tensor-core launches the same steps cost 3 us and more
+// per product however small it is.
 #include <cuda_bf16.h>
 
 #include "common.cuh"
@@ -19,9 +19,11 @@ constexpr int NC_THREADS = 512;
 constexpr int NC_MAX_R = 64;
 static_assert(NC_MAX_R <= 64, "the tiles of A fit the smallest block that they are given");
 constexpr int NC_MAX_SMEM = 220 * 1024;
-// Multiply-adds of a product beyond which the tensor cores win in spite of their launches (here / there, us, fp32 and
-// bf16: 32 x 2048 59 / 85 71, 48 x 1500 79 / 86 73, 64 x 1024 94 / 82 72, 64 x 2048 151 / 90 75).
-constexpr long long NC_MAX_WORK = 3300000;
+// Multiply-adds of a product, for an eighth of them a CTA, beyond which the tensor cores win in spite of their launches
+// (here / there, us, in fp32 and bf16 accuracy: 64 x 512 60 / 77 55, 64 x 800 76 / 72 61, 48 x 1400 77 / 75 65, 32 x 3000
+// 73 / 77 65, 32 x 1024 38 / 67 60; batches, with fewer CTAs for a matrix: 40 of 64 x 512 149 / 98 76, 100 of 32 x 200
+// 42 / 90 77).
+constexpr long long NC_MAX_WORK_FULL = 3000000, NC_MAX_WORK_HALF = 2000000;
 
 struct NcArgs {
   int r, c, cs;   // short and long side; columns of the long side per CTA
@@ -257,12 +259,12 @@ __global__ void __launch_bounds__(NC_THREADS, 1) ns_cluster_kernel(const NsSourc
 // CTAs for a matrix.  One is fastest only while a barrier costs more than the work (16 x 16: 12 us with one, 15 with
 // eight; 16 x 64: 15 and 16); from there on eight (10 x 200: 17 and 15 us, 64 x 200: 111 and 40), but no more than let
 // all matrices of a batch run at once, and enough for the slices to fit.
-NcArgs plan(int batch, int rows, int cols, size_t* bytes) {
+NcArgs plan(int batch, int rows, int cols, bool full, size_t* bytes) {
   NcArgs n{};
   n.tall = rows > cols;
   n.r = n.tall ? cols : rows;
   n.c = n.tall ? rows : cols;
-  if (n.r > NC_MAX_R || (long long)n.r * n.r * n.c > NC_MAX_WORK) return n;
+  if (n.r > NC_MAX_R) return n;
   const int q = (n.r + 3) / 4;
   n.rp = 4 * (q | 1);
   n.direct = n.rp <= 20;  // at most 100 pieces of 16 bytes from each of eight CTAs
@@ -273,6 +275,7 @@ NcArgs plan(int batch, int rows, int cols, size_t* bytes) {
     n.csp = (n.cs + 3) / 4 * 4;
     const double size = sizeof(float) * ((double)2 * n.csp * n.rp + (double)(cs > 1 ? (n.direct ? 4 : 3) : 2) * n.rp * n.rp);
     if (size > NC_MAX_SMEM) continue;
+    if ((long long)n.r * n.r * n.c * (8 / cs) > (full ? NC_MAX_WORK_FULL : NC_MAX_WORK_HALF)) break;
     *bytes = (size_t)size;
     n.csize = cs;
     break;
@@ -282,19 +285,19 @@ NcArgs plan(int batch, int rows, int cols, size_t* bytes) {
 
 }  // namespace
 
-bool ns_fits_cluster(int rows, int cols) {
+bool ns_fits_cluster(int batch, int rows, int cols, bool full) {
   size_t bytes = 0;
-  return plan(1, rows, cols, &bytes).csize != 0;
+  return plan(batch, rows, cols, full, &bytes).csize != 0;
 }
 
 cudaError_t ns_cluster_set_attributes() {
   return cudaFuncSetAttribute(ns_cluster_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, NC_MAX_SMEM);
 }
 
-cudaError_t launch_ns_cluster(const NsSource& s, const NsSink& o, int batch, const float coef[3], int steps, double eps,
-                              cudaStream_t st) {
+cudaError_t launch_ns_cluster(const NsSource& s, const NsSink& o, int batch, bool full, const float coef[3], int steps,
+                              double eps, cudaStream_t st) {
   size_t bytes = 0;
-  NcArgs n = plan(batch, s.rows, s.cols, &bytes);
+  NcArgs n = plan(batch, s.rows, s.cols, full, &bytes);
   n.steps = steps;
   n.a = coef[0];
   n.b = coef[1];

@@ -458,6 +458,22 @@ def test_product_streams_and_graphs():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(1, 64, 486), (1, 64, 492), (1, 64, 733), (1, 740, 64), (16, 64, 480), (17, 64, 480), (64, 40, 300),
+                                   (65, 40, 300), (130, 64, 64), (200, 30, 500), (500, 12, 33), (300, 70, 64)])
+def test_orthogonalize_narrow_batches(shape):
+    """Both sides of what decides, by work and batch, whether a narrow matrix stays on chip."""
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    for t in ("f32", "bf16"):
+        g = torch.randn(shape, generator=gen, device="cuda").to(TYPES[t])
+        work = torch.empty(binding.orthogonalize_work(g), dtype=torch.uint8, device="cuda")
+        for precision, tol in (("full", FULL_TOL), ("half", HALF_TOL)):
+            o = binding.orthogonalize(g, precision=precision, work=work)
+            for i in sorted({0, shape[0] // 3, shape[0] - 1}):
+                assert rel(num(o[i]), om.newton_schulz(num(g[i]))) <= tol + OUT[t], (t, precision, i)
+    binding.check_operators()
+
+
+@pytest.mark.gpu
 def test_calls_on_two_streams_at_once():
     """Chains of large and small calls side by side, each with its own work area, then two captured chains replayed
     side by side: the same bits as one after the other."""
