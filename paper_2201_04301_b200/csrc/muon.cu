@@ -20,6 +20,7 @@
 #include <math.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "../../include/gcada.h"
 #include "common.cuh"
@@ -167,6 +168,7 @@ __device__ __forceinline__ void fetch_piece(const CUtensorMap* tm, unsigned char
 __device__ __forceinline__ NsTarget target_of(const NsSink& s) { return s.at ? *s.at : s.to; }
 
 // A warp: f holds row m0 + lane, columns n .. n + PW - 1 of the products' sums.
+template <bool USER>
 __device__ __forceinline__ void finish_piece(const NsGemm& a, const CUtensorMap* tmD, const Coef& k, unsigned char* buf, int lane,
                                              bool leader, int m0, int n, int b, float (&f)[PW]) {
 #pragma unroll
@@ -186,7 +188,7 @@ __device__ __forceinline__ void finish_piece(const NsGemm& a, const CUtensorMap*
       for (int j = 0; j < 8; ++j) f[8 * c + j] *= k.acc;
     }
   }
-  if (a.out == OUT_SPLIT) {
+  if (!USER) {
     const int d = m0 + lane - n;
     if (a.sym && m0 < n + PW && n < m0 + 32 && d >= 0 && d < PW) {
 #pragma unroll
@@ -288,7 +290,9 @@ __device__ __forceinline__ void finish_piece(const NsGemm& a, const CUtensorMap*
 //         so few tiles that it is their number that counts.
 // FULL: three products for each K block's pairs of parts; the sum of `chunk` blocks moves to registers, because the tensor
 // cores cut (not round) each partial sum.
-template <int TN, bool FULL>
+// USER: the result goes to the user's matrix; a kernel of its own, for its instructions would get in the other products' way
+// (they are fetched anew by every launch).
+template <int TN, bool FULL, bool USER>
 __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_constant__ CUtensorMap tmA,
                                                              const __grid_constant__ CUtensorMap tmB,
                                                              const __grid_constant__ CUtensorMap tmS,
@@ -504,7 +508,7 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
             float f[PW];
 #pragma unroll
             for (int j = 0; j < PW; ++j) f[j] = __uint_as_float(v[j]);
-            finish_piece(a, &tmD, k, buf, lane, leader, m0, n0 + q, b, f);
+            finish_piece<USER>(a, &tmD, k, buf, lane, leader, m0, n0 + q, b, f);
           }
         }
         tc_fence_before();
@@ -559,7 +563,7 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
       bool ok = true;
       if (a.src) ok = __all_sync(0xffffffffu, mbar_wait_bounded(&src_bar[warp - 2], 0));
       if (ok)
-        finish_piece(a, &tmD, coefficients(a, b), buf, lane, leader, m0, n, b, f);
+        finish_piece<USER>(a, &tmD, coefficients(a, b), buf, lane, leader, m0, n, b, f);
       else if (leader)
         raise_error(a.err);
     }
@@ -761,19 +765,24 @@ NsLayout layout(int batch, int rows, int cols) {
   return L;
 }
 
-cudaError_t set_attributes() {
+template <int TN, bool FULL>
+cudaError_t set_smem() {
   const cudaFuncAttribute at = cudaFuncAttributeMaxDynamicSharedMemorySize;
-  cudaError_t e = cudaFuncSetAttribute(ns_gemm_kernel<256, true>, at, Smem<256, true>::BYTES);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<256, false>, at, Smem<256, false>::BYTES);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<128, true>, at, Smem<128, true>::BYTES);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<128, false>, at, Smem<128, false>::BYTES);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<64, true>, at, Smem<64, true>::BYTES);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_gemm_kernel<64, false>, at, Smem<64, false>::BYTES);
+  const cudaError_t e = cudaFuncSetAttribute(ns_gemm_kernel<TN, FULL, true>, at, Smem<TN, FULL>::BYTES);
+  return e == cudaSuccess ? cudaFuncSetAttribute(ns_gemm_kernel<TN, FULL, false>, at, Smem<TN, FULL>::BYTES) : e;
+}
+cudaError_t set_attributes() {
+  cudaError_t e = set_smem<256, true>();
+  if (e == cudaSuccess) e = set_smem<256, false>();
+  if (e == cudaSuccess) e = set_smem<128, true>();
+  if (e == cudaSuccess) e = set_smem<128, false>();
+  if (e == cudaSuccess) e = set_smem<64, true>();
+  if (e == cudaSuccess) e = set_smem<64, false>();
   if (e == cudaSuccess) e = ns_cluster_set_attributes();
   return e;
 }
 
-template <int TN, bool FULL>
+template <int TN, bool FULL, bool USER>
 cudaError_t launch_shape(const CUtensorMap& ta, const CUtensorMap& tb, const NsGemm& a, int ctas, cudaStream_t st) {
   CUtensorMap ts = ta, td = ta;  // the epilogue's pieces; not used where there is no linear term or a user's matrix
   constexpr bool PAIR = TN == 256;
@@ -793,7 +802,7 @@ cudaError_t launch_shape(const CUtensorMap& ta, const CUtensorMap& tb, const NsG
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = PAIR || a.split > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, ns_gemm_kernel<TN, FULL>, ta, tb, ts, td, a);
+  return cudaLaunchKernelEx(&cfg, ns_gemm_kernel<TN, FULL, USER>, ta, tb, ts, td, a);
 }
 
 // The shape with the least work in sequence, in units of 512 cycles: a K block of a pair's tile takes about one (measured
@@ -841,9 +850,15 @@ cudaError_t launch_ns_gemm(const CUtensorMap& ta, const CUtensorMap& tb, NsGemm 
   a.total = a.per * a.batch;
   const long long room = s.tn == 256 ? sms / 2 : sms, want = (long long)a.total * a.split;
   const int ctas = (int)(want < room ? want : room) * (s.tn == 256 ? 2 : 1);
-  if (s.tn == 256) return full ? launch_shape<256, true>(ta, tb, a, ctas, st) : launch_shape<256, false>(ta, tb, a, ctas, st);
-  if (s.tn == 128) return full ? launch_shape<128, true>(ta, tb, a, ctas, st) : launch_shape<128, false>(ta, tb, a, ctas, st);
-  return full ? launch_shape<64, true>(ta, tb, a, ctas, st) : launch_shape<64, false>(ta, tb, a, ctas, st);
+  const bool user = a.out != OUT_SPLIT;
+  const auto launch = [&](auto tn, auto f) {
+    constexpr int TN = decltype(tn)::value;
+    constexpr bool FULL = decltype(f)::value;
+    return user ? launch_shape<TN, FULL, true>(ta, tb, a, ctas, st) : launch_shape<TN, FULL, false>(ta, tb, a, ctas, st);
+  };
+  const auto either = [&](auto tn) { return full ? launch(tn, std::true_type{}) : launch(tn, std::false_type{}); };
+  if (s.tn == 256) return either(std::integral_constant<int, 256>{});
+  return s.tn == 128 ? either(std::integral_constant<int, 128>{}) : either(std::integral_constant<int, 64>{});
 }
 
 }  // namespace
