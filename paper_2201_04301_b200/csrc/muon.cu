@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
   constexpr int WCOLS = TN / 4;                  // columns of an epilogue warp
   constexpr uint32_t TMEM_COLS = 2 * TN;
   unsigned char* tiles = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int csize = PAIR ? 2 : a.split;
   const int rank = csize > 1 ? (int)cluster_rank() : 0;
   const int first = (int)(blockIdx.x / (unsigned)csize), stride = (int)(gridDim.x / (unsigned)csize);
@@ -354,28 +354,30 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
   // of instructions and parameters costs as much as a copy) outside the wait.
 
   if (warp == 0) {
-    if (leader) {
-      bool ok = true;
-      bool waited = false;
-      int s = 0;  // the stage, and the parity of its turn
-      uint32_t ph = 0;
-      const int sym_log = a.sym_log;
-      const bool a_mn = a.a_mn, a_sym = a.a_sym, b_mn = a.b_mn, b_sym = a.b_sym;
-      for (int u = first; u < total && ok; u += stride) {
-        const int b = u < per ? 0 : (int)((unsigned)u / (unsigned)per);
-        int mt, nt;
-        tile_of(u - b * per, tiles_n, a.sym, g_tiles, RATIO, mt, nt);
-        const int rA = PAIR ? mt * 256 + rank * 128 : mt * 128, rB = PAIR ? nt * 256 + rank * 128 : nt * TN;
-          for (int kb = kb0; kb < kb1; ++kb) {
-          const int kc = kb * BK, kblk = kc >> sym_log;
-          const bool mnA = a_mn || (a_sym && kblk < rA >> sym_log), mnB = b_mn || (b_sym && kblk < rB >> sym_log);
-          ok = mbar_spin_bounded(&empty_bar[s], ph ^ 1u);
-          if (!ok) break;
+    // The warp runs the loop as a whole and elects a thread for the copies: what they take is uniform to the compiler then (the
+    // same for the products was slower).
+    bool ok = true;
+    bool waited = false;
+    int s = 0;  // the stage, and the parity of its turn
+    uint32_t ph = 0;
+    const int sym_log = a.sym_log;
+    const bool a_mn = a.a_mn, a_sym = a.a_sym, b_mn = a.b_mn, b_sym = a.b_sym;
+    for (int u = first; u < total && ok; u += stride) {
+      const int b = u < per ? 0 : (int)((unsigned)u / (unsigned)per);
+      int mt, nt;
+      tile_of(u - b * per, tiles_n, a.sym, g_tiles, RATIO, mt, nt);
+      const int rA = PAIR ? mt * 256 + rank * 128 : mt * 128, rB = PAIR ? nt * 256 + rank * 128 : nt * TN;
+      for (int kb = kb0; kb < kb1; ++kb) {
+        const int kc = kb * BK, kblk = kc >> sym_log;
+        const bool mnA = a_mn || (a_sym && kblk < rA >> sym_log), mnB = b_mn || (b_sym && kblk < rB >> sym_log);
+        ok = __all_sync(0xffffffffu, mbar_spin_bounded(&empty_bar[s], ph ^ 1u));
+        if (!ok) break;
+        if (!waited) pdl_wait();
+        waited = true;
+        if (elect_one()) {
           if (!PAIR || rank == 0) mbar_expect_tx(&full_bar[s], (PAIR ? 2 : 1) * STAGE_BYTES);
           // a pair's copies are all counted by its first CTA, whose thread issues the products
           const uint32_t bar = PAIR ? cluster_map(smem_u32(&full_bar[s]), 0) : smem_u32(&full_bar[s]);
-          if (!waited) pdl_wait();
-          waited = true;
 #pragma unroll
           for (int t = 0; t < (FULL ? 2 : 1); ++t) {
             const int z = 2 * b + t;  // plane 0 = hi, 1 = lo
@@ -391,11 +393,11 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
               tma_load_3d_to<PAIR>(sa + OP_BYTES + j * BLK_BYTES, &tmB, mnB ? r : kc, mnB ? kc : r, z, bar);
             }
           }
-          if (++s == STAGES) s = 0, ph ^= 1u;
         }
+        if (++s == STAGES) s = 0, ph ^= 1u;
       }
-      if (!ok) raise_error(a.err);
     }
+    if (!ok && leader) raise_error(a.err);
   } else if (warp == 1) {
     if (leader && (!PAIR || rank == 0)) {
       // fp16 operands, fp32 sum
