@@ -31,7 +31,6 @@ namespace gcada {
 namespace {
 
 constexpr int TR = 128, BK = 64;                       // rows of an operand block; K values of a stage
-constexpr int BLK_BYTES = 64 * BK * 2;                 // one copy box: 64 x 64 fp16
 constexpr int OP_BYTES = TR * BK * 2;                  // one operand block: 16 KiB
 constexpr int EPI_WARPS = 16;                          // four to a quadrant of tensor memory's lanes
 constexpr int THREADS = 64 + 32 * EPI_WARPS;
@@ -84,6 +83,11 @@ struct NsGemm {
   int out;               // OUT_*
   NsSink user;           // OUT_F32 ... : user's matrix
   int* err;
+};
+
+// An operand's maps: K contiguous, and M / N contiguous (either may stand in for the other where it is not used).
+struct OperandMaps {
+  CUtensorMap k, mn;
 };
 
 // Tiles of a result; of a symmetric one only those from the row's own block of 2^g row tiles on, a row tile being `r`
@@ -293,10 +297,11 @@ __device__ __forceinline__ void finish_piece(const NsGemm& a, const CUtensorMap*
 // USER: the result goes to the user's matrix; a kernel of its own, for its instructions would get in the other products' way
 // (they are fetched anew by every launch).
 template <int TN, bool FULL, bool USER>
-__global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_constant__ CUtensorMap tmA,
-                                                             const __grid_constant__ CUtensorMap tmB,
+__global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_constant__ OperandMaps tmA,
+                                                             const __grid_constant__ OperandMaps tmB,
                                                              const __grid_constant__ CUtensorMap tmS,
-                                                             const __grid_constant__ CUtensorMap tmD, const NsGemm a) {
+                                                             const __grid_constant__ CUtensorMap tmD,
+                                                             const __grid_constant__ NsGemm a) {
   constexpr int STAGES = Smem<TN, FULL>::STAGES, STAGE_BYTES = Smem<TN, FULL>::STAGE_BYTES, BLOCK_BYTES = Smem<TN, FULL>::BLOCK_BYTES;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   __shared__ uint64_t full_bar[STAGES], empty_bar[STAGES], tfull_bar[2], tempty_bar[2], src_bar[EPI_WARPS];
@@ -337,8 +342,10 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
   }
   if (warp == 1) tmem_alloc<PAIR>(&tmem_base_sm, TMEM_COLS);
   if (threadIdx.x == 64) {
-    prefetch_map(&tmA);
-    prefetch_map(&tmB);
+    prefetch_map(&tmA.k);
+    prefetch_map(&tmA.mn);
+    prefetch_map(&tmB.k);
+    prefetch_map(&tmB.mn);
     prefetch_map(&tmS);
     prefetch_map(&tmD);
   }
@@ -382,16 +389,8 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
           for (int t = 0; t < (FULL ? 2 : 1); ++t) {
             const int z = 2 * b + t;  // plane 0 = hi, 1 = lo
             unsigned char* sa = tiles + (size_t)s * STAGE_BYTES + t * BLOCK_BYTES;
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const int r = rA + j * 64;
-              tma_load_3d_to<PAIR>(sa + j * BLK_BYTES, &tmA, mnA ? r : kc, mnA ? kc : r, z, bar);
-            }
-#pragma unroll
-            for (int j = 0; j < B_ROWS / 64; ++j) {
-              const int r = rB + j * 64;
-              tma_load_3d_to<PAIR>(sa + OP_BYTES + j * BLK_BYTES, &tmB, mnB ? r : kc, mnB ? kc : r, z, bar);
-            }
+            tma_load_4d_to<PAIR>(sa, mnA ? &tmA.mn : &tmA.k, mnA ? 0 : kc, mnA ? kc : rA, mnA ? rA >> 6 : 0, z, bar);
+            tma_load_4d_to<PAIR>(sa + OP_BYTES, mnB ? &tmB.mn : &tmB.k, mnB ? 0 : kc, mnB ? kc : rB, mnB ? rB >> 6 : 0, z, bar);
           }
         }
         if (++s == STAGES) s = 0, ph ^= 1u;
@@ -718,23 +717,49 @@ __global__ void __launch_bounds__(256) ns_copy_kernel(const NsGemm a) {
 }
 
 // ----------------------------------------------------------------- host
-// fp16 array [planes][rows][cols], row stride ld elements, zero fill outside; boxes of 64 columns x 64 rows with the
-// 128-byte swizzle (operands), or 16 columns x 32 rows with the 32-byte one, hi and lo parts in one box where `parts` is 2
-// (epilogue pieces).
-bool make_map_f16(CUtensorMap* tm, const void* base, long long cols, long long rows, long long planes, long long ld,
-                  long long plane, int width = 64, int parts = 1) {
-  EncodeTiledFn fn = encode_fn();
-  if (!fn) return false;
-  cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
-  cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)plane * 2};
-  cuuint32_t box[3] = {(cuuint32_t)width, width == 64 ? 64u : 32u, (cuuint32_t)parts};
-  cuuint32_t es[3] = {1, 1, 1};
-  return fn(tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(base), dims, strides, box, es,
-            CU_TENSOR_MAP_INTERLEAVE_NONE,
-            width == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_32B,
-            CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
+// The arrays of a run, [planes][rows][cols] of fp16 with row stride ld (a multiple of 64), and the forms in which they are
+// copied, each encoded once:
+//   K128, K64   128 or 64 rows x 64 columns under the 128-byte swizzle: an operand whose K is the contiguous index
+//   MN128, MN64 64 rows (K) x 128 or 64 columns, as blocks of 64 columns one behind the other, under the same swizzle.  Blocks of
+//               64 columns are a dimension of the map, so one copy takes two of them; columns behind the last are whatever the
+//               padding holds and reach only results that are not kept
+//   PIECE2, 1   32 rows x 16 columns under the 32-byte swizzle, of the hi and lo planes or of the hi plane
+enum { ARR_X0, ARR_X1, ARR_A, ARR_Q };
+enum { FORM_K128, FORM_K64, FORM_MN128, FORM_MN64, FORM_PIECE2, FORM_PIECE1 };
+struct NsArrays {
+  struct {
+    const __half* p;
+    long long cols, rows, ld, plane;
+  } arr[4];
+  long long planes;
+  CUtensorMap maps[4][6];
+  bool made[4][6] = {};
+
+  const CUtensorMap* get(int i, int form) {
+    CUtensorMap* tm = &maps[i][form];
+    if (made[i][form]) return tm;
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return nullptr;
+    const auto& a = arr[i];
+    const bool mn = form == FORM_MN128 || form == FORM_MN64, piece = form >= FORM_PIECE2;
+    const cuuint64_t ld = (cuuint64_t)a.ld * 2, plane = (cuuint64_t)a.plane * 2;
+    const cuuint64_t planes = (cuuint64_t)this->planes;
+    const cuuint64_t d3[3] = {(cuuint64_t)a.cols, (cuuint64_t)a.rows, planes}, s3[2] = {ld, plane};
+    const cuuint64_t dk[4] = {(cuuint64_t)a.cols, (cuuint64_t)a.rows, 1, planes}, sk[3] = {ld, plane, plane};
+    const cuuint64_t dm[4] = {64, (cuuint64_t)a.rows, (cuuint64_t)a.ld / 64, planes}, sm[3] = {ld, 128, plane};
+    const cuuint32_t b3[3] = {PW, 32, form == FORM_PIECE2 ? 2u : 1u}, bk[4] = {64, form == FORM_K128 ? 128u : 64u, 1, 1};
+    const cuuint32_t bm[4] = {64, 64, form == FORM_MN128 ? 2u : 1u, 1}, es[4] = {1, 1, 1, 1};
+    made[i][form] = fn(tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, piece ? 3 : 4, const_cast<__half*>(a.p), piece ? d3 : mn ? dm : dk,
+                       piece ? s3 : mn ? sm : sk, piece ? b3 : mn ? bm : bk, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                       piece ? CU_TENSOR_MAP_SWIZZLE_32B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return made[i][form] ? tm : nullptr;
+  }
+};
+// Which of them a product reads and writes.
+struct NsUse {
+  int a, b, src, dst;
+};
 
 struct NsLayout {
   int r, c;                // short and long side
@@ -747,9 +772,9 @@ NsLayout layout(int batch, int rows, int cols) {
   NsLayout L{};
   L.r = rows < cols ? rows : cols;
   L.c = rows < cols ? cols : rows;
-  L.ld_x = (cols + 15) / 16 * 16;  // rows of whole 32-byte sectors
+  L.ld_x = (cols + 63) / 64 * 64;  // rows of whole copy blocks
   L.plane_x = L.ld_x * rows;
-  L.ld_s = (L.r + 15) / 16 * 16;
+  L.ld_s = (L.r + 63) / 64 * 64;
   L.plane_s = L.ld_s * L.r;
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -785,12 +810,19 @@ cudaError_t set_attributes() {
 }
 
 template <int TN, bool FULL, bool USER>
-cudaError_t launch_shape(const CUtensorMap& ta, const CUtensorMap& tb, const NsGemm& a, int ctas, cudaStream_t st) {
-  CUtensorMap ts = ta, td = ta;  // the epilogue's pieces; not used where there is no linear term or a user's matrix
+cudaError_t launch_shape(NsArrays& arrays, const NsUse& use, const NsGemm& a, int ctas, cudaStream_t st) {
   constexpr bool PAIR = TN == 256;
-  if ((a.src && !make_map_f16(&ts, a.src, a.N, a.M, 2LL * a.batch, a.ld_src, a.src_plane, PW, 2)) ||
-      (a.out == OUT_SPLIT && !make_map_f16(&td, a.dst, a.N, a.M, 2LL * a.batch, a.ld_dst, a.dst_plane, PW, a.write_lo ? 2 : 1)))
-    return cudaErrorInvalidValue;
+  const CUtensorMap* ak = a.a_mn ? nullptr : arrays.get(use.a, FORM_K128);
+  const CUtensorMap* am = a.a_mn || a.a_sym ? arrays.get(use.a, FORM_MN128) : ak;
+  const CUtensorMap* bk = a.b_mn ? nullptr : arrays.get(use.b, TN == 64 ? FORM_K64 : FORM_K128);
+  const CUtensorMap* bm = a.b_mn || a.b_sym ? arrays.get(use.b, TN == 64 ? FORM_MN64 : FORM_MN128) : bk;
+  if (a.a_mn) ak = am;
+  if (a.b_mn) bk = bm;
+  if (!ak || !am || !bk || !bm) return cudaErrorInvalidValue;
+  // the pieces' are not used where there is no linear term, or a user's matrix
+  const CUtensorMap* ts = a.src ? arrays.get(use.src, FORM_PIECE2) : ak;
+  const CUtensorMap* td = a.out == OUT_SPLIT ? arrays.get(use.dst, a.write_lo ? FORM_PIECE2 : FORM_PIECE1) : ak;
+  if (!ts || !td) return cudaErrorInvalidValue;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)ctas);
   cfg.blockDim = dim3(THREADS);
@@ -804,7 +836,7 @@ cudaError_t launch_shape(const CUtensorMap& ta, const CUtensorMap& tb, const NsG
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = PAIR || a.split > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, ns_gemm_kernel<TN, FULL, USER>, ta, tb, ts, td, a);
+  return cudaLaunchKernelEx(&cfg, ns_gemm_kernel<TN, FULL, USER>, OperandMaps{*ak, *am}, OperandMaps{*bk, *bm}, *ts, *td, a);
 }
 
 // The shape with the least work in sequence, in units of 512 cycles: a K block of a pair's tile takes about one (measured
@@ -838,8 +870,7 @@ Shape choose_shape(int M, int N, int K, int sym, int g, int batch, int full, int
   return s;
 }
 
-cudaError_t launch_ns_gemm(const CUtensorMap& ta, const CUtensorMap& tb, NsGemm a, const Shape& s, int full, int sms,
-                           cudaStream_t st) {
+cudaError_t launch_ns_gemm(NsArrays& arrays, const NsUse& use, NsGemm a, const Shape& s, int full, int sms, cudaStream_t st) {
   // The tensor cores cut each of a chunk's partial sums, an error that grows with their number and, like fp32's own
   // rounding, weighs less in longer sums.  Error of the result, time, with 4 / 2 / 1 blocks a chunk (fp32 arithmetic
   // 1.5e-6, 2.4e-6, 2.6e-6): 200 x 784 3.5e-6 2.2e-6 1.4e-6, 97 99 101 us; 1024 x 1024 2.6e-6 1.2e-6 0.6e-6,
@@ -856,7 +887,7 @@ cudaError_t launch_ns_gemm(const CUtensorMap& ta, const CUtensorMap& tb, NsGemm 
   const auto launch = [&](auto tn, auto f) {
     constexpr int TN = decltype(tn)::value;
     constexpr bool FULL = decltype(f)::value;
-    return user ? launch_shape<TN, FULL, true>(ta, tb, a, ctas, st) : launch_shape<TN, FULL, false>(ta, tb, a, ctas, st);
+    return user ? launch_shape<TN, FULL, true>(arrays, use, a, ctas, st) : launch_shape<TN, FULL, false>(arrays, use, a, ctas, st);
   };
   const auto either = [&](auto tn) { return full ? launch(tn, std::true_type{}) : launch(tn, std::false_type{}); };
   if (s.tn == 256) return either(std::integral_constant<int, 256>{});
@@ -907,11 +938,12 @@ cudaError_t ns_run(const NsProblem& p, void* work, cudaStream_t st, const char**
   __half* X[2] = {reinterpret_cast<__half*>(base + L.x0), reinterpret_cast<__half*>(base + L.x1)};
   __half* A = reinterpret_cast<__half*>(base + L.s0);
   __half* Q = reinterpret_cast<__half*>(base + L.s1);
-  CUtensorMap tx[2], ta, tq;
-  bool ok = make_map_f16(&ta, A, L.r, L.r, 2LL * p.batch, L.ld_s, L.plane_s) &&
-            make_map_f16(&tq, Q, L.r, L.r, 2LL * p.batch, L.ld_s, L.plane_s);
-  for (int i = 0; i < 2 && ok; ++i) ok = make_map_f16(&tx[i], X[i], p.cols, p.rows, 2LL * p.batch, L.ld_x, L.plane_x);
-  if (!ok) return *why = "tensor map creation failed for this shape", cudaErrorInvalidValue;
+  NsArrays arrays;
+  arrays.planes = 2LL * p.batch;
+  for (int i = 0; i < 2; ++i) {
+    arrays.arr[ARR_X0 + i] = {X[i], p.cols, p.rows, L.ld_x, L.plane_x};
+    arrays.arr[ARR_A + i] = {i ? Q : A, L.r, L.r, L.ld_s, L.plane_s};
+  }
 
   const long long chunks = (long long)((p.cols + 7) / 8) * p.rows;
   const long long want = (chunks + 255) / 256;
@@ -973,7 +1005,7 @@ cudaError_t ns_run(const NsProblem& p, void* work, cudaStream_t st, const char**
     g.ld_dst = L.ld_s;
     g.dst_plane = L.plane_s;
     g.write_lo = 1;
-    if ((e = launch_ns_gemm(tx[cur], tx[cur], g, gram, p.full, sms, st)) != cudaSuccess) return *why = "kernel launch", e;
+    if ((e = launch_ns_gemm(arrays, {cur, cur, 0, ARR_A}, g, gram, p.full, sms, st)) != cudaSuccess) return *why = "kernel launch", e;
     // b A + c A^2
     g.prod = PROD_POLY;
     g.K = L.r;
@@ -988,7 +1020,7 @@ cudaError_t ns_run(const NsProblem& p, void* work, cudaStream_t st, const char**
     g.diag = shift_a && !shift_p ? (cb + cc) * SCALE : 0.f;
     g.dst = Q;
     g.write_lo = p.full;
-    if ((e = launch_ns_gemm(ta, ta, g, poly, p.full, sms, st)) != cudaSuccess) return *why = "kernel launch", e;
+    if ((e = launch_ns_gemm(arrays, {ARR_A, ARR_A, ARR_A, ARR_Q}, g, poly, p.full, sms, st)) != cudaSuccess) return *why = "kernel launch", e;
     // a X + (.) X, or a X + X (.) for a tall matrix
     NsGemm h = last ? f : g;
     h.prod = last ? PROD_LAST : PROD_APPLY;
@@ -1016,7 +1048,7 @@ cudaError_t ns_run(const NsProblem& p, void* work, cudaStream_t st, const char**
       h.dst_plane = L.plane_x;
       h.write_lo = 1;
     }
-    if ((e = launch_ns_gemm(tall ? tx[cur] : tq, tall ? tq : tx[cur], h, apply, p.full, sms, st)) != cudaSuccess)
+    if ((e = launch_ns_gemm(arrays, {tall ? cur : ARR_Q, tall ? ARR_Q : cur, cur, cur ^ 1}, h, apply, p.full, sms, st)) != cudaSuccess)
       return *why = "kernel launch", e;
     n += 3;
   }

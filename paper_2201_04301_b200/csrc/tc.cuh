@@ -214,18 +214,18 @@ __device__ __forceinline__ void tmem_dealloc(uint32_t base, uint32_t cols) {
 }
 // `bar` is an address in the cluster's window; with PAIR it may be the other CTA's.
 template <bool PAIR>
-__device__ __forceinline__ void tma_load_3d_to(void* dst, const CUtensorMap* tm, int c0, int c1, int c2, uint32_t bar) {
+__device__ __forceinline__ void tma_load_4d_to(void* dst, const CUtensorMap* tm, int c0, int c1, int c2, int c3, uint32_t bar) {
   if (PAIR)
     asm volatile(
-        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
+        "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(
             smem_u32(dst)),
-        "l"(tm), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
+        "l"(tm), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
         : "memory");
   else
     asm volatile(
-        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(
             smem_u32(dst)),
-        "l"(tm), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
+        "l"(tm), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
         : "memory");
 }
 template <bool PAIR>
