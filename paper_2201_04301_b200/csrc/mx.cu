@@ -535,7 +535,7 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
   __shared__ uint64_t full_bar[STAGES], empty_bar[STAGES], tfull_bar[2], tempty_bar[2];
   __shared__ uint32_t tmem_base_sm;
   unsigned char* tiles = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int csize = PAIR ? 2 : split;
   const int rank = csize > 1 ? (int)cluster_rank() : 0;
   const int first = (int)blockIdx.x / csize, stride = (int)gridDim.x / csize;
@@ -573,20 +573,21 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
   const bool leader = elect_one();
 
   if (warp == 0) {
-    if (leader) {
-      bool ok = true;
-      int it = 0;
-      for (int i = 0; i < n_local && ok; ++i) {
-        const int u = first + i * stride, mt = u / tiles_n, nt = u - mt * tiles_n;
-        const int rA = mt * T::TM + (PAIR ? rank * 128 : 0), rB = nt * T::TN + (PAIR ? rank * 128 : 0);
-        for (int kb = kb0; kb < kb1; ++kb, ++it) {
-          const int s = it % STAGES;
-          ok = mbar_spin_bounded(&empty_bar[s], (uint32_t)(((it / STAGES) & 1) ^ 1));
-          if (!ok) break;
+    // the warp runs the loop as a whole and elects a thread for the copies: what they take is uniform to the compiler then
+    bool ok = true;
+    int it = 0;
+    for (int i = 0; i < n_local && ok; ++i) {
+      const int u = first + i * stride, mt = u / tiles_n, nt = u - mt * tiles_n;
+      const int rA = mt * T::TM + (PAIR ? rank * 128 : 0), rB = nt * T::TN + (PAIR ? rank * 128 : 0);
+      for (int kb = kb0; kb < kb1; ++kb, ++it) {
+        const int s = it % STAGES;
+        ok = __all_sync(0xffffffffu, mbar_spin_bounded(&empty_bar[s], (uint32_t)(((it / STAGES) & 1) ^ 1)));
+        if (!ok) break;
+        if (it == 0) pdl_wait();  // here and not earlier: the first run of what lies before costs as much as a copy
+        if (elect_one()) {
           unsigned char* sa = tiles + (size_t)s * T::STAGE_BYTES;
           if (!PAIR || rank == 0) mbar_expect_tx(&full_bar[s], (PAIR ? 2 : 1) * T::STAGE_BYTES);
           const uint32_t bar = PAIR ? cluster_map(smem_u32(&full_bar[s]), 0) : smem_u32(&full_bar[s]);
-          if (it == 0) pdl_wait();  // here and not earlier: the first run of what lies before costs as much as a copy
           tma_load_2d_to<PAIR>(sa, &tmA, kb * (KB / 2), rA, bar);
           tma_load_2d_to<PAIR>(sa + BM * (KB / 2), &tmB, kb * (KB / 2), rB, bar);
           // scale tiles are rows of their maps; one behind the end (its columns are not kept) arrives as zeros
@@ -596,8 +597,8 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
             tma_load_2d_to<PAIR>(sa + T::CODE_BYTES + (1 + j) * 1024, &tmSB, 0, ((nt * T::TN >> 7) + j) * (int)p.b.col_tiles + kb, bar);
         }
       }
-      if (!ok) raise_error(p.err);
     }
+    if (!ok && leader) raise_error(p.err);
   } else if (warp == 1) {
     if (leader && (!PAIR || rank == 0)) {
       // E2M1 operands (1 at bits 7 and 10), E8M0 scales (bit 23); bits 29 / 4: which pair of a column's four scale
