@@ -7,6 +7,7 @@ missing or cannot be loaded: there is no fallback implementation.
 import ctypes as C
 import functools
 import os
+import threading
 
 import numpy as np
 
@@ -375,12 +376,15 @@ def _matrix(t, what, dims=(2,)):
     return stride[-2]
 
 
+_messages = threading.local()
+
+
 class _Launch:
     """Device, stream and message buffer of one operator call on `first`'s device."""
 
     def __init__(self, first, others, stream):
         import torch
-        self.torch, self.device, self.lib = torch, first.device, _lib or load()
+        self.torch, self.first, self.device, self.lib = torch, first, first.device, _lib or load()
         for t in others:
             if t is not None and t.device != self.device:
                 raise ValueError("tensors on different devices: %s and %s" % (self.device, t.device))
@@ -394,7 +398,7 @@ class _Launch:
                 self.other = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(self.raw, self.device)
 
     def fresh(self, *shape, dtype):
-        t = self.torch.empty(shape, dtype=dtype, device=self.device)
+        t = self.first.new_empty(shape, dtype=dtype)
         if self.other is not None:  # the caching allocator may hand out memory that the current stream still uses
             self.other.wait_stream(self.torch.cuda.current_stream(self.device))
             t.record_stream(self.other)
@@ -410,7 +414,9 @@ class _Launch:
         return w.data_ptr()
 
     def call(self, fn, args, tensors):
-        buf = C.create_string_buffer(256)
+        buf = getattr(_messages, "buf", None)
+        if buf is None:
+            buf = _messages.buf = C.create_string_buffer(256)   # one a thread
         if self.torch._C._cuda_getDevice() == self.index:
             st = fn(*args, self.raw, buf, 256)
         else:
