@@ -412,11 +412,12 @@ __global__ void __launch_bounds__(256) mx_upload_product_kernel(const MxView a, 
 // ----------------------------------------------------------------- product
 // Warp 0 copies the operands' codes (128-byte rows of 256 elements, 128-byte swizzle) and scales into a ring of
 // stages, warp 1 copies a stage's scales into tensor memory and issues the block-scaled products (64 K values each),
-// sixteen warps write the result.  As in the fp16 products of muon.cu there are two shapes:
-//   PAIR: two CTAs on a 256 x 256 tile (cta_group::2), persistent.  A CTA holds 128 rows of A and of the result, 128 of
-//         the 256 columns of B, and the scales of its rows and of all columns.  The accumulator takes 256 of the 512
-//         columns of tensor memory and the stages' scales most of the rest, so there is only one: the epilogue first
-//         moves it to registers (64 a thread), which frees it for the next tile.
+// sixteen warps write the result.  As in the fp16 products of muon.cu there are two kinds of shapes:
+//   PAIR: two CTAs on a 256 x BN tile (cta_group::2), persistent.  A CTA holds 128 rows of A and of the result, half of
+//         the columns of B, and the scales of its rows and of all columns.  BN = 256 needs the fewest bytes; its accumulator
+//         takes 256 of the 512 columns of tensor memory and the stages' scales most of the rest, so there is only one, and
+//         the epilogue first moves it to registers (64 a thread), which frees it for the next tile.  BN = 192 leaves room
+//         for two, so that the epilogue of a tile runs beside the products of the next: faster where K is short.
 //   else: a CTA on a 128 x BN tile; with fewer tiles than SMs the CTAs of a cluster share the K range and add up
 //         their partial tiles through distributed shared memory in rank order.
 constexpr int BM = 128, KB = 256;
@@ -425,14 +426,15 @@ constexpr int THREADS = 64 + 32 * EPI_WARPS;
 
 template <bool PAIR, int BN>
 struct MxTile {
-  static constexpr int TM = PAIR ? 256 : 128, TN = PAIR ? 256 : BN;  // the tile
-  static constexpr int ROWS_B = PAIR ? 128 : BN;                     // rows of B that this CTA copies
-  static constexpr int NB = TN < 128 ? 1 : TN / 128;                 // row tiles of B's scales that the tile touches
-  static constexpr int ACC = PAIR ? 1 : 2;                           // accumulators in tensor memory
+  static constexpr int TM = PAIR ? 256 : 128, TN = BN;  // the tile
+  static constexpr int ROWS_B = PAIR ? BN / 2 : BN;     // rows of B that this CTA copies
+  static constexpr int NB = (TN + 127) / 128;           // row tiles of B's scales that the tile touches
+  static constexpr int ACC = TN == 256 ? 1 : 2;         // accumulators in tensor memory
   static constexpr int CODE_BYTES = (BM + ROWS_B) * (KB / 2);
   static constexpr int STAGE_BYTES = CODE_BYTES + (1 + NB) * 1024;
-  static constexpr int STAGES = PAIR || BN == 128 ? 6 : 7;
-  static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + 1024;
+  static constexpr int STAGES = BN == 64 ? 7 : 5;
+  static constexpr int PIECE_BYTES = 32 * 64;  // a warp's 32 rows of 64 bytes of a result on their way out
+  static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + EPI_WARPS * PIECE_BYTES + 1024;
   static constexpr int SF_COL = ACC * TN;                 // first tensor-memory column of the scales
   static constexpr int SF_COLS = 8 + 8 * NB;              // per stage: A 2 x 4, B 2 x 4 NB
   static constexpr int TMEM_COLS = SF_COL + STAGES * SF_COLS <= 256 ? 256 : 512;
@@ -523,6 +525,73 @@ __device__ __forceinline__ void mx_finish16(const MxGemm& p, int m, int n, float
   }
 }
 
+// A warp's 32 rows x W columns from (m0, n) on, a lane a row: through shared memory in pieces of 64 bytes a row, so that four
+// lanes write a row's and an instruction meets 8 lines instead of 32 (8192 x 4096 x 1024, fp32: 60 -> 33 us).
+template <int W>
+__device__ __forceinline__ void mx_finish_rows(const MxGemm& p, unsigned char* buf, int lane, int m0, int n, const uint32_t (&v)[W / 16][16]) {
+  const int M = (int)p.a.rows, N = (int)p.b.rows;
+  const bool even = ((reinterpret_cast<uintptr_t>(p.d) | (uintptr_t)(p.ld * (p.d_bf16 ? 2 : 4))) & 15) == 0;
+#pragma unroll
+  for (int j = 0; j < W / 16; ++j) {
+    const int nj = n + 16 * j;
+    if (nj >= N) continue;
+    // a piece: 16 columns in fp32, in bf16 32, taken together with the even sixteen
+    const bool whole = even && (p.d_bf16 ? p.beta == 0.f && (j | 1) < W / 16 && n + 16 * (j | 1) + 16 <= N : nj + 16 <= N);
+    if (whole && p.d_bf16 && (j & 1)) continue;
+    float f[16];
+#pragma unroll
+    for (int t = 0; t < 16; ++t) f[t] = __uint_as_float(v[j][t]);
+    if (!whole) {
+      if (m0 + lane < M) mx_finish16(p, m0 + lane, nj, f);
+      continue;
+    }
+    uint4 x[4];
+#pragma unroll
+    for (int t = 0; t < 16; ++t) f[t] = p.alpha * f[t] + (p.bias ? p.bias[nj + t] : 0.f);
+    if (!p.d_bf16) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        x[c] = make_uint4(__float_as_uint(f[4 * c]), __float_as_uint(f[4 * c + 1]), __float_as_uint(f[4 * c + 2]), __float_as_uint(f[4 * c + 3]));
+    } else {
+      constexpr int LAST = W / 16 - 1;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        if (c == 2) {
+#pragma unroll
+          for (int t = 0; t < 16; ++t)
+            f[t] = p.alpha * __uint_as_float(v[j < LAST ? j + 1 : j][t]) + (p.bias ? p.bias[nj + 16 + t] : 0.f);
+        }
+        uint32_t w[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const __nv_bfloat162 b2 = __floats2bfloat162_rn(f[8 * (c & 1) + 2 * t], f[8 * (c & 1) + 2 * t + 1]);
+          w[t] = *reinterpret_cast<const uint32_t*>(&b2);
+        }
+        x[c] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+    const int ch = lane & 3;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) *reinterpret_cast<uint4*>(buf + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = x[c];
+    __syncwarp();
+#pragma unroll
+    for (int r0 = 0; r0 < 32; r0 += 8) {
+      const int r = r0 + (lane >> 2), m = m0 + r;
+      uint4 y = *reinterpret_cast<const uint4*>(buf + r * 64 + ((ch ^ ((r >> 1) & 3)) << 4));
+      if (m < M) {
+        uint4* o = reinterpret_cast<uint4*>(static_cast<char*>(p.d) + ((long long)m * p.ld + nj) * (p.d_bf16 ? 2 : 4)) + ch;
+        if (p.beta != 0.f) {  // (fp32)
+          const float4 d = *reinterpret_cast<const float4*>(o);
+          y = make_uint4(__float_as_uint(__uint_as_float(y.x) + p.beta * d.x), __float_as_uint(__uint_as_float(y.y) + p.beta * d.y),
+                         __float_as_uint(__uint_as_float(y.z) + p.beta * d.z), __float_as_uint(__uint_as_float(y.w) + p.beta * d.w));
+        }
+        *o = y;
+      }
+    }
+    __syncwarp();
+  }
+}
+
 template <bool PAIR, int BN>
 __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_constant__ CUtensorMap tmA,
                                                              const __grid_constant__ CUtensorMap tmB,
@@ -578,7 +647,8 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
     int it = 0;
     for (int i = 0; i < n_local && ok; ++i) {
       const int u = first + i * stride, mt = u / tiles_n, nt = u - mt * tiles_n;
-      const int rA = mt * T::TM + (PAIR ? rank * 128 : 0), rB = nt * T::TN + (PAIR ? rank * 128 : 0);
+      const int rank_b = PAIR ? rank * T::ROWS_B : 0;
+      const int rA = mt * T::TM + (PAIR ? rank * 128 : 0), rB = nt * T::TN + rank_b;
       for (int kb = kb0; kb < kb1; ++kb, ++it) {
         const int s = it % STAGES;
         ok = __all_sync(0xffffffffu, mbar_spin_bounded(&empty_bar[s], (uint32_t)(((it / STAGES) & 1) ^ 1)));
@@ -628,8 +698,8 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
               tc_copy_scales<PAIR>(sf + 8 + h * 4 * T::NB + j * 4, sa + T::CODE_BYTES + (1 + j) * 1024 + h * 512);
           }
           const uint64_t da = make_desc(sa), db = make_desc(sa + BM * (KB / 2));
-          // a tile narrower than a scale tile starts at one of its groups of 32 rows = one of the four columns
-          const uint32_t sub = T::TN < 128 ? (uint32_t)((nt * T::TN & 127) >> 5) : 0u;
+          // a tile may start in the middle of a scale tile, at one of its groups of 32 rows = one of the four columns
+          const uint32_t sub = T::TN % 128 ? (uint32_t)((nt * T::TN & 127) >> 5) : 0u;
 #pragma unroll
           for (int kk = 0; kk < 4; ++kk) {
             const uint32_t id = (uint32_t)(kk & 1) * 2u;
@@ -645,12 +715,13 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
     }
   } else {
     const int quad = warp & 3, sub = (warp - 2) >> 2;
+    unsigned char* buf = tiles + (size_t)STAGES * T::STAGE_BYTES + (size_t)(warp - 2) * T::PIECE_BYTES;
     bool ok = true;
     pdl_wait();
     for (int i = 0; i < n_local; ++i) {
       const int slot = i % T::ACC;
       const int u = first + i * stride, mt = u / tiles_n, nt = u - mt * tiles_n;
-      const int m = mt * T::TM + (PAIR ? rank * 128 : 0) + quad * 32 + lane, c0 = sub * WCOLS, n0 = nt * T::TN + c0;
+      const int m0 = mt * T::TM + (PAIR ? rank * 128 : 0) + quad * 32, c0 = sub * WCOLS, n0 = nt * T::TN + c0;
       if (ok) {
         ok = mbar_wait_bounded(&tfull_bar[slot], (uint32_t)((i / T::ACC) & 1));
         ok = __all_sync(0xffffffffu, ok);
@@ -674,16 +745,8 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
         float* part = reinterpret_cast<float*>(tiles) + (size_t)c0 * BM + quad * 32 + lane;
 #pragma unroll
         for (int j = 0; j < WCOLS; ++j) part[j * BM] = __uint_as_float(v[j >> 4][j & 15]);
-      } else if (m < M) {
-#pragma unroll
-        for (int j = 0; j < WCOLS; j += 16) {
-          if (n0 + j < N) {
-            float f[16];
-#pragma unroll
-            for (int t = 0; t < 16; ++t) f[t] = __uint_as_float(v[j >> 4][t]);
-            mx_finish16(p, m, n0 + j, f);
-          }
-        }
+      } else {
+        mx_finish_rows<WCOLS>(p, buf, lane, m0, n0, v);
       }
     }
     if (!ok && leader) raise_error(p.err);
@@ -759,6 +822,7 @@ bool make_map_scales(CUtensorMap* tm, const MxView& v) {
 cudaError_t set_attributes() {
   const cudaFuncAttribute at = cudaFuncAttributeMaxDynamicSharedMemorySize;
   cudaError_t e = cudaFuncSetAttribute(mx_gemm_kernel<true, 256>, at, MxTile<true, 256>::SMEM_BYTES);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(mx_gemm_kernel<true, 192>, at, MxTile<true, 192>::SMEM_BYTES);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(mx_gemm_kernel<false, 128>, at, MxTile<false, 128>::SMEM_BYTES);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(mx_gemm_kernel<false, 64>, at, MxTile<false, 64>::SMEM_BYTES);
   return e;
@@ -827,19 +891,28 @@ cudaError_t mx_gemm(const MxGemm& p, cudaStream_t st, const char** why) {
   int sms = 0;
   cudaError_t e = device_ready(known, set_attributes, &sms, why);
   if (e != cudaSuccess) return e;
-  // The shape whose CTAs have the least to copy in sequence: a K block costs 35 KiB in a pair, 34 and 26 KiB in the
-  // single shapes (units of 32 KiB below); `ramp` is what filling and draining costs, a cluster's sum included.
+  // The shape with the least work in sequence, in units of 0.34 us = 32 KiB on their way to an SM: a K block costs 35 and 31
+  // KiB in the pairs' shapes, 34 and 26 in the single ones; what a round of tiles, the filling and draining and a cluster's
+  // sum cost beside that is measured.  (fp32 results, us, with 256 / 192 / 128 / 64 columns: 4096 x 4096 x 32768 210 / 232 /
+  // 284 / 400, 4096 x 4096 x 4096 38 / 34 / 40 / 56, 3000 x 3000 x 2048 17 / 17 / 15 / 20, 8192 x 4096 x 1024 41 / 44 / 36 /
+  // 40, 1024 x 1024 x 4096 13 / 10 / 10 / 8.)
   const int kb = (int)p.a.col_tiles;
   auto tiles = [&](int tm, int tn) { return ((p.a.rows + tm - 1) / tm) * ((p.b.rows + tn - 1) / tn); };
-  const long long pairs = tiles(256, 256), t128 = tiles(128, 128), t64 = tiles(128, 64);
+  const long long pairs = tiles(256, 256), p192 = tiles(256, 192), t128 = tiles(128, 128), t64 = tiles(128, 64);
   int bn = 256, split = 1;
-  double cost = (double)((pairs + sms / 2 - 1) / (sms / 2)) * (kb * 1.1 + 4) + 8;
+  auto rounds = [](long long n, int places) { return (double)((n + places - 1) / places); };
+  double cost = rounds(pairs, sms / 2) * (kb * 1.1 + 8) + 17;
+  const double c192 = rounds(p192, sms / 2) * (kb * 1.02 + 2 > 12.5 ? kb * 1.02 + 2 : 12.5) + 9;
+  if (c192 < cost) {
+    cost = c192;
+    bn = 192;
+  }
   for (int w = 128; w >= 64; w -= 64) {
     const long long t = w == 128 ? t128 : t64;
-    const double unit = w == 128 ? 1.06 : 0.8;
+    const double unit = w == 128 ? 1.06 : 0.8, ramp = w == 128 ? 6 : 4;
     for (int k = 1; k <= 8 && k <= kb; ++k) {
       if (k > 1 && (t * k > sms || k * t > (long long)max_clusters(k, sms) * k)) break;
-      const double c = (k == 1 ? (double)((t + sms - 1) / sms) : 1.0) * ((kb + k - 1) / k) * unit + 6 + (k > 1 ? 3 : 0);
+      const double c = (k == 1 ? rounds(t, sms) : 1.0) * (((kb + k - 1) / k) * unit + 1) + (k > 1 ? 2 : 1) * ramp;
       if (c < cost) {
         cost = c;
         bn = w;
@@ -847,6 +920,7 @@ cudaError_t mx_gemm(const MxGemm& p, cudaStream_t st, const char** why) {
       }
     }
   }
+  if (bn == 192) return launch_shape<true, 192>(p, 1, 2 * (p192 < sms / 2 ? p192 : sms / 2), st, why);
   if (bn == 256) return launch_shape<true, 256>(p, 1, 2 * (pairs < sms / 2 ? pairs : sms / 2), st, why);
   const long long t = bn == 128 ? t128 : t64, want = t * split, ctas = want < sms ? want : sms;
   if (bn == 128) return launch_shape<false, 128>(p, split, ctas, st, why);
