@@ -339,7 +339,8 @@ gcada_status gcada_innovation_norms_noalloc(const float *fresh_dev, const float 
 
 /* How the products of an orthogonalisation are formed.  Both keep the iterate in 22 bits and accumulate in fp32.
  * FULL: operands of 22 bits, the accuracy of fp32 arithmetic (three tensor-core products for one).
- * HALF: operands of 11 bits; the result is within about 2e-3 of its norm, below the rounding to bfloat16. */
+ * HALF: operands of 11 bits; the result is within about 2e-3 of its norm (4e-3 for a short side below 100; matrices with
+ * a short side of up to 64 are formed as with FULL). */
 #define GCADA_PRECISION_FULL 0
 #define GCADA_PRECISION_HALF 1
 

@@ -53,12 +53,13 @@ struct NsProblem {
   int* err = nullptr;   // device error word, or null
 };
 // Narrow matrices, all steps on chip (muon_cluster.cu).
-bool ns_fits_cluster(int batch, int rows, int cols, bool full);
+constexpr int NS_NARROW = 64;  // short side
+bool ns_fits_cluster(int batch, int rows, int cols);
 cudaError_t ns_cluster_set_attributes();
-cudaError_t launch_ns_cluster(const NsSource& s, const NsSink& o, int batch, bool full, const float coef[3], int steps,
-                              double eps, cudaStream_t st);
+cudaError_t launch_ns_cluster(const NsSource& s, const NsSink& o, int batch, const float coef[3], int steps, double eps,
+                              cudaStream_t st);
 
-int ns_launches(int rows, int cols, int steps, bool full);  // kernels that ns_run enqueues
+int ns_launches(int rows, int cols, int steps);  // kernels that ns_run enqueues
 size_t ns_work_bytes(int batch, int rows, int cols);
 cudaError_t ns_run(const NsProblem& p, void* work, cudaStream_t st, const char** why, int* launches);
 

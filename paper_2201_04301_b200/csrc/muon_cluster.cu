@@ -16,14 +16,13 @@ namespace gcada {
 namespace {
 
 constexpr int NC_THREADS = 512;
-constexpr int NC_MAX_R = 64;
+constexpr int NC_MAX_R = NS_NARROW;
 static_assert(NC_MAX_R <= 64, "the tiles of A fit the smallest block that they are given");
 constexpr int NC_MAX_SMEM = 220 * 1024;
 // Multiply-adds of a product, for an eighth of them a CTA, beyond which the tensor cores win in spite of their launches
-// (here / there, us, in fp32 and bf16 accuracy: 64 x 512 60 / 77 55, 64 x 800 76 / 72 61, 48 x 1400 77 / 75 65, 32 x 3000
-// 73 / 77 65, 32 x 1024 38 / 67 60; batches, with fewer CTAs for a matrix: 40 of 64 x 512 149 / 98 76, 100 of 32 x 200
-// 42 / 90 77).
-constexpr long long NC_MAX_WORK_FULL = 3000000, NC_MAX_WORK_HALF = 2000000;
+// (here / there, us: 64 x 512 60 / 77, 64 x 800 76 / 72, 48 x 1400 77 / 75, 32 x 3000 73 / 77, 32 x 1024 38 / 67; batches,
+// with fewer CTAs for a matrix: 40 of 64 x 512 149 / 98, 100 of 32 x 200 42 / 90).
+constexpr long long NC_MAX_WORK = 3000000;
 
 struct NcArgs {
   int r, c, cs;   // short and long side; columns of the long side per CTA
@@ -259,7 +258,7 @@ __global__ void __launch_bounds__(NC_THREADS, 1) ns_cluster_kernel(const NsSourc
 // CTAs for a matrix.  One is fastest only while a barrier costs more than the work (16 x 16: 12 us with one, 15 with
 // eight; 16 x 64: 15 and 16); from there on eight (10 x 200: 17 and 15 us, 64 x 200: 111 and 40), but no more than let
 // all matrices of a batch run at once, and enough for the slices to fit.
-NcArgs plan(int batch, int rows, int cols, bool full, size_t* bytes) {
+NcArgs plan(int batch, int rows, int cols, size_t* bytes) {
   NcArgs n{};
   n.tall = rows > cols;
   n.r = n.tall ? cols : rows;
@@ -275,7 +274,7 @@ NcArgs plan(int batch, int rows, int cols, bool full, size_t* bytes) {
     n.csp = (n.cs + 3) / 4 * 4;
     const double size = sizeof(float) * ((double)2 * n.csp * n.rp + (double)(cs > 1 ? (n.direct ? 4 : 3) : 2) * n.rp * n.rp);
     if (size > NC_MAX_SMEM) continue;
-    if ((long long)n.r * n.r * n.c * (8 / cs) > (full ? NC_MAX_WORK_FULL : NC_MAX_WORK_HALF)) break;
+    if ((long long)n.r * n.r * n.c * (8 / cs) > NC_MAX_WORK) break;
     *bytes = (size_t)size;
     n.csize = cs;
     break;
@@ -285,19 +284,19 @@ NcArgs plan(int batch, int rows, int cols, bool full, size_t* bytes) {
 
 }  // namespace
 
-bool ns_fits_cluster(int batch, int rows, int cols, bool full) {
+bool ns_fits_cluster(int batch, int rows, int cols) {
   size_t bytes = 0;
-  return plan(batch, rows, cols, full, &bytes).csize != 0;
+  return plan(batch, rows, cols, &bytes).csize != 0;
 }
 
 cudaError_t ns_cluster_set_attributes() {
   return cudaFuncSetAttribute(ns_cluster_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, NC_MAX_SMEM);
 }
 
-cudaError_t launch_ns_cluster(const NsSource& s, const NsSink& o, int batch, bool full, const float coef[3], int steps,
-                              double eps, cudaStream_t st) {
+cudaError_t launch_ns_cluster(const NsSource& s, const NsSink& o, int batch, const float coef[3], int steps, double eps,
+                              cudaStream_t st) {
   size_t bytes = 0;
-  NcArgs n = plan(batch, s.rows, s.cols, full, &bytes);
+  NcArgs n = plan(batch, s.rows, s.cols, &bytes);
   n.steps = steps;
   n.a = coef[0];
   n.b = coef[1];

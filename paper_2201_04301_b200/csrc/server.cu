@@ -118,7 +118,7 @@ size_t muon_work_bytes(const MlpPlan& pl) {
 
 int muon_kernels(const MlpPlan& pl, const MuonPlan& m) {
   int n = 2;
-  for (int l = 1; l <= pl.n_layers; ++l) n += ns_launches(pl.dims[l], pl.dims[l - 1], m.steps, pl.compute == 0);
+  for (int l = 1; l <= pl.n_layers; ++l) n += ns_launches(pl.dims[l], pl.dims[l - 1], m.steps);
   return n;
 }
 

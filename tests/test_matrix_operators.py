@@ -470,6 +470,8 @@ def test_orthogonalize_narrow_batches(shape):
             o = binding.orthogonalize(g, precision=precision, work=work)
             for i in sorted({0, shape[0] // 3, shape[0] - 1}):
                 assert rel(num(o[i]), om.newton_schulz(num(g[i]))) <= tol + OUT[t], (t, precision, i)
+            if min(shape[1:]) <= 64:                              # narrow matrices have fp32 accuracy either way
+                assert rel(num(o[0]), om.newton_schulz(num(g[0]))) <= FULL_TOL + OUT[t], (t, precision)
     binding.check_operators()
 
 
