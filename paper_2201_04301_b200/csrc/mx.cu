@@ -361,6 +361,14 @@ __global__ void __launch_bounds__(128) mx_quantize_uploads_kernel(const Params P
     for (int j = 0; j < 32; ++j)
       v[j] = T::make(r < q.rows ? p[(long long)j * ld] : (__nv_bfloat16)0.f, r + 1 < q.rows ? p[(long long)j * ld + 1] : (__nv_bfloat16)0.f);
   }
+  // behind the minibatch's end the factor holds what the network makes of a row of zeros (activations relu(b)): no part of
+  // the upload, and it must not decide the scale of a block that it shares with samples
+  const int samples = P.B - b0 - w * 32;
+  if (samples < 32) {
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+      if (j >= samples) v[j] = 0;
+  }
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     uint32_t top = 0;

@@ -189,6 +189,33 @@ def test_uploads_in_four_bits(kw):
     full.close()
 
 
+@pytest.mark.parametrize("batch", [200, 129, 31])
+def test_padding_rows_take_no_part_in_an_uploads_scales(batch):
+    """A minibatch that ends inside a block of 32 rows: the block's scale is that of its own rows.  The kernels pad a
+    minibatch with zero features, whose activations are relu(b); here those are far above every sample's, and in the later
+    steps the biases are what the updates have made of them."""
+    w = workload(dict(ODD16, batch=batch))
+    dims, n_g = w["dims"], w["N"] // (w["M"] // w["M_G"])
+    w["X"][:, :dims[0]] = w["X"][:, :dims[0]].abs()
+    rows, cols, W, b = layers(dims)[0]
+    w["theta0"][W] = -w["theta0"][W].abs()
+    x = w["X"][:, :cols].double()
+    drop = (x @ w["theta0"][W].view(rows, cols).double().T).max(dim=0).values      # the sample that is lowered least
+    w["theta0"][b] = (-drop + 0.02 * drop.abs()).float()                           # a little above zero, for that one
+    model, X = MLP(dims, bf16=True), w["X"][:, :dims[0]].float().numpy().astype(np.float64)
+    g = binding.from_workload(to_cuda(w), stream=torch.cuda.Stream(), options={binding.OPT_UPLOAD: binding.UPLOAD_MXFP4})
+    for k in range(3):
+        theta = np.asarray(g.get_theta(), dtype=np.float64)
+        g.step_forced(np.ones((1, g.G), dtype=np.uint8))
+        uploads = np.asarray(g.get_debug(binding.DBG_GLAST), dtype=np.float64)
+        for grp in range(g.G):
+            pick = batch_indices(w["seed"], k, grp, batch, n_g)
+            for (n_out, n_in, W, b), (dz, act) in zip(layers(dims), factors(model, theta, X[pick], w["y"].numpy()[pick])):
+                want = (four_bits(dz).T @ four_bits(act)).ravel()
+                assert rel_l2(uploads[grp][W], want) < TOL_BF16, (k, grp, n_out, n_in, rel_l2(uploads[grp][W], want))
+    g.close()
+
+
 def test_refusals():
     lin = binding.from_workload(to_cuda(make_workload("cfg1", rows=300)), stream=torch.cuda.Stream())
     fp32 = binding.from_workload(to_cuda(workload(FP32)), stream=torch.cuda.Stream())
