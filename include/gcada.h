@@ -339,8 +339,11 @@ gcada_status gcada_innovation_norms_noalloc(const float *fresh_dev, const float 
 
 /* How the products of an orthogonalisation are formed.  Both keep the iterate in 22 bits and accumulate in fp32.
  * FULL: operands of 22 bits, the accuracy of fp32 arithmetic (three tensor-core products for one).
- * HALF: operands of 11 bits; the result is within about 2e-3 of its norm (4e-3 for a short side below 100; matrices with
- * a short side of up to 64 are formed as with FULL). */
+ * HALF: operands of 11 bits, for callers to whom speed matters more.  Five steps with the default coefficients: within
+ * 2e-3 of the result's norm for random matrices with a short side of 100 and more, 4e-3 from 65 on, where roundings
+ * average out; where many singular values are alike (a multiple of a permutation, an orthogonal or an identity matrix)
+ * they do not, and the error can reach 4e-2 (half a step of bf16 is 4e-3).  More steps than five amplify it: 0.1 at
+ * seven.  Matrices with a short side of up to 64 are formed as with FULL. */
 #define GCADA_PRECISION_FULL 0
 #define GCADA_PRECISION_HALF 1
 

@@ -445,9 +445,9 @@ def check_operators(device=None):
 _coef_arrays = {}
 
 
-def _steps(steps, coef, eps, precision, narrow):
+def _steps(steps, coef, eps, precision):
     if precision is None:
-        precision = "half" if narrow else "full"
+        precision = "full"
     if precision not in PRECISIONS:
         raise ValueError("precision must be 'full' or 'half', not %r" % (precision,))
     array = _coef_arrays.get(coef) if type(coef) is tuple else None
@@ -485,8 +485,9 @@ def _ns_work(run, batch, rows, cols, work):
 
 def orthogonalize(g, out=None, steps=5, coef=MUON_COEF, eps=1e-7, precision=None, work=None, stream=None):
     """`g` ([rows, cols] or [batch, rows, cols], float32 or bfloat16) after `steps` Newton-Schulz steps: a matrix of
-    the same singular vectors whose singular values are near one.  See gcada_orthogonalize.  `precision`: "full" or
-    "half", by default "full" for float32 and "half" for bfloat16.  `out` may be `g`.  `work`: a tensor of at least
+    the same singular vectors whose singular values are near one.  See gcada_orthogonalize.  `precision`: "full" (the
+    default, for either type) or "half", up to three times as fast but with an error that can be above half a step of
+    bfloat16 (GCADA_PRECISION_HALF).  `out` may be `g`.  `work`: a tensor of at least
     orthogonalize_work(g) bytes to use as the work area, by default taken from torch's allocator."""
     kind, ld_g = _compute_type(g, "g"), _matrix(g, "g", (2, 3))
     run = _Launch(g, (out, work), stream)
@@ -498,7 +499,7 @@ def orthogonalize(g, out=None, steps=5, coef=MUON_COEF, eps=1e-7, precision=None
     ld_o = _matrix(out, "out", (2, 3))
     rows, cols = shape[-2:]
     batch, stride_g, stride_o = (shape[0], g.stride(0), out.stride(0)) if len(shape) == 3 else (1, 0, 0)
-    precision, steps, coef, eps = _steps(steps, coef, eps, precision, kind == COMPUTE_BF16)
+    precision, steps, coef, eps = _steps(steps, coef, eps, precision)
     work, ptr, size = _ns_work(run, batch, rows, cols, work)
     run.call(run.lib.gcada_orthogonalize,
              (g.data_ptr(), out.data_ptr(), kind, batch, rows, cols, ld_g, stride_g, ld_o, stride_o, precision, steps,
@@ -515,8 +516,8 @@ def orthogonalize_work(g):
 def muon_update(w, m, g, lr, beta=0.95, nesterov=True, weight_decay=0.0, scale=None, steps=5, coef=MUON_COEF,
                 eps=1e-7, precision=None, work=None, stream=None):
     """One optimiser step of the weight matrix `w`, in place with its momentum `m` (float32); `g` is the gradient.
-    See gcada_muon_update.  `scale`: by default sqrt(max(1, rows / cols)).  `precision`: by default "full" for
-    float32 weights and "half" for bfloat16 ones."""
+    See gcada_muon_update.  `scale`: by default sqrt(max(1, rows / cols)).  `precision`: "full" (the default) or
+    "half", see orthogonalize."""
     w_kind, g_kind = _compute_type(w, "w"), _compute_type(g, "g")
     ld_w, ld_m, ld_g = _matrix(w, "w"), _matrix(m, "m"), _matrix(g, "g")
     if _compute_type(m, "m") != COMPUTE_FP32:
@@ -527,7 +528,7 @@ def muon_update(w, m, g, lr, beta=0.95, nesterov=True, weight_decay=0.0, scale=N
     run = _Launch(w, (m, g, work), stream)
     if scale is None:
         scale = max(1.0, rows / max(1, cols)) ** 0.5
-    precision, steps, coef, eps = _steps(steps, coef, eps, precision, w_kind == COMPUTE_BF16)
+    precision, steps, coef, eps = _steps(steps, coef, eps, precision)
     work, ptr, size = _ns_work(run, 1, rows, cols, work)
     run.call(run.lib.gcada_muon_update,
              (w.data_ptr(), w_kind, m.data_ptr(), g.data_ptr(), g_kind, rows, cols, ld_w, ld_m, ld_g, float(lr),

@@ -11,6 +11,9 @@
 //     3.44^4 = 140-fold; the products' own roundings only reach directions whose singular values are already of
 //     order one.  (Simulated error after 5 steps, spectra i^-2 / rank 10 / Gaussian: 2e-4 / 4e-4 / 1.7e-3 of the
 //     result's norm; with X kept in 11 bits 2e-2 / 4e-2 / 1.4e-3; in bf16 2e-1 / 3e-1 / 1.3e-2.)
+//     That is the average of many roundings.  Where all singular values are alike they agree: a multiple of an identity
+//     matrix is off by up to 1.3e-2 (51 x 51; 8e-3 at 151), a single singular value by up to 4e-2, because the polynomial's
+//     slope reaches 4.2 at 1.21.  So nothing takes HALF that did not ask for it.
 //   - precision FULL: each product is lo*hi' + hi*lo' + hi*hi' (the smallest terms first), which is fp32 accuracy
 //     (simulated 4e-7 .. 8e-6 of the result's norm on the same spectra, fp32 arithmetic itself 6e-6 .. 3e-5).
 // A and b A + c A^2 are symmetric: only blocks on and above the diagonal are computed and stored.  An operand block
@@ -906,8 +909,8 @@ size_t ns_work_bytes(int batch, int rows, int cols) {
 // Everything an orthogonalisation enqueues.  `why` names the step that failed.
 cudaError_t ns_run(const NsProblem& problem, void* work, cudaStream_t st, const char** why, int* launches) {
   NsProblem p = problem;
-  // HALF's roundings do not average out over few singular values that are all alike (error 5e-3 at 33 x 997, 3e-3 at 66 x
-  // 700, 1.7e-3 from 100 on), and for narrow matrices the products are not what takes the time.
+  // For narrow matrices the products are not what takes the time, and HALF's roundings average out over few singular values
+  // least of all (error of Gaussian ones 5e-3 at 33 x 997, 3e-3 at 66 x 700, 1.7e-3 from 100 on).
   if ((p.rows < p.cols ? p.rows : p.cols) <= NS_NARROW) p.full = 1;
   *why = "";
   static std::atomic<int> known[MAX_DEVICES];

@@ -573,3 +573,83 @@ def test_an_iteration_of_the_server():
         assert (np.abs(num(agg) - ra) <= (rows / 32 + 3) * 2.0 ** -23 * (np.abs(da) @ np.abs(db).T)).all()
         rw, rm = om.muon(rw, rm, ra, 0.02, 0.95, True, 0.01, 1.0)
     assert np.linalg.norm(num(w) - rw) <= 3 * (FULL_TOL * 0.02 * 1.3 * math.sqrt(n_out) + 2.0 ** -22 * np.linalg.norm(rw))
+
+
+# ------------------------------------------------------------------------------------------- accuracy
+def even_spectrum(kind, rows, cols, seed=0):
+    """Matrices whose singular values are all alike: nothing averages their roundings out."""
+    gen = np.random.default_rng(seed)
+    r = min(rows, cols)
+    if kind == "identity":
+        return np.eye(rows, cols)
+    if kind == "permutation":
+        x = np.zeros((rows, cols))
+        x[gen.permutation(rows)[:r], gen.permutation(cols)[:r]] = gen.choice([-1.0, 1.0], r)
+        return x
+    u = np.linalg.qr(gen.standard_normal((max(rows, cols), r)))[0]
+    return u if rows >= cols else np.ascontiguousarray(u.T)
+
+
+def even_bound(r, operand, kept, steps=5):
+    """First-order bound of the relative error where all r singular values are s_0 = r^-1/2.  A step rounds what it keeps (X, A,
+    the polynomial's terms: `kept`, relative) and its products' operands (`operand`): with q = b A + c A^2
+        dA <= 2 operand A,   dq <= |b + 2 c A| dA + 2 operand |c| A^2 + operand max(|q|, |q - b - c|)
+        dx <= s (dq + operand |q| + kept (|a| + |b| A + |c| A^2 + 2))
+    An error of a multiple of an orthogonal matrix grows by |p'(s)| in its symmetric and by p(s) / s in its other part."""
+    a, b, c = om.COEF
+    s, e = 1 / math.sqrt(r), 0.0
+    for _ in range(steps):
+        worst = max(max(abs(a + 3 * b * t * t + 5 * c * t ** 4), abs(a + b * t * t + c * t ** 4)) for t in (s - e, s, s + e))
+        A = s * s
+        q = b * A + c * A * A
+        dq = abs(b + 2 * c * A) * 2 * operand * A + 2 * operand * abs(c) * A * A + operand * max(abs(q), abs(q - b - c))
+        e = worst * e + s * (dq + operand * abs(q) + kept * (a + abs(b) * A + abs(c) * A * A + 2))
+        s = s * (a + q)
+    return e / s
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["identity", "permutation", "orthogonal"])
+@pytest.mark.parametrize("shape", [(65, 65), (92, 92), (100, 180), (151, 151), (308, 308), (500, 398), (400, 400), (1024, 1024)])
+def test_accuracy_where_all_singular_values_are_alike(shape, kind):
+    """The accuracy that a caller gets without asking is that of fp32 arithmetic, whatever the type and the matrix: below
+    half a step of bf16 too, which the products of 11-bit operands can miss by more than its half."""
+    x = even_spectrum(kind, *shape)
+    for t in ("f32", "bf16"):
+        g = torch.from_numpy(x * 0.5).to(TYPES[t]).cuda()
+        want = om.newton_schulz(num(g))
+        # (a rounded orthogonal matrix has singular values within 2^-8 of each other: the bound's slope hardly moves)
+        full = 1.1 * even_bound(min(shape), 2.0 ** -22, 2.0 ** -22) + OUT[t]
+        assert rel(num(binding.orthogonalize(g)), want) <= full, t
+        assert rel(num(binding.orthogonalize(g, precision="full")), want) <= full, t
+        assert rel(num(binding.orthogonalize(g, precision="half")), want) <= 1.1 * even_bound(min(shape), 2.0 ** -11, 2.0 ** -22) + OUT[t], t
+        assert rel(num(binding.orthogonalize(g, precision="half")), want) <= 0.04 + OUT[t], t      # what the header says
+    w, m = torch.zeros(shape, dtype=torch.bfloat16, device="cuda"), torch.zeros(shape, device="cuda")
+    binding.muon_update(w, m, g, lr=-1.0, beta=0.0, scale=1.0)
+    assert rel(num(w), want) <= full
+    binding.check_operators()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(66, 700), (100, 150), (200, 784), (513, 520), (700, 300)])
+def test_accuracy_of_either_precision_for_spread_spectra(shape):
+    """The figures that the header gives for random matrices."""
+    for kind in ("gauss", "power"):
+        g = torch.from_numpy(spectrum(*shape, kind, seed=4)).float().cuda()
+        want = om.newton_schulz(num(g))
+        assert rel(num(binding.orthogonalize(g, precision="half")), want) <= (2e-3 if min(shape) >= 100 else 4e-3), kind
+        assert rel(num(binding.orthogonalize(g, precision="full")), want) <= 2e-5, kind
+
+
+@pytest.mark.gpu
+def test_the_precision_is_full_unless_half_is_asked_for():
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    for t in TYPES.values():
+        g = torch.randn(130, 300, generator=gen, device="cuda").to(t)
+        assert torch.equal(binding.orthogonalize(g), binding.orthogonalize(g, precision="full"))
+        results = []
+        for precision in (None, "full", "half"):
+            w, m = torch.zeros(130, 300, dtype=t, device="cuda"), torch.zeros(130, 300, device="cuda")
+            binding.muon_update(w, m, g, lr=0.1, precision=precision)
+            results.append(w)
+        assert torch.equal(results[0], results[1]) and not torch.equal(results[0], results[2])
