@@ -97,6 +97,8 @@ typedef struct {
                                   was uploaded, i.e. the products of the quantised factors */
 #define GCADA_UPLOAD_FULL 0
 #define GCADA_UPLOAD_MXFP4 1
+#define GCADA_OPT_SERVER_PRECISION 9 /* MLP: how server rule Muon orthogonalises, GCADA_PRECISION_FULL (default: weights and
+                                        momentum are fp32, whatever the network computes in) or GCADA_PRECISION_HALF */
 #define GCADA_OPT_PERSISTENT 7     /* 1 (default) = logistic / quadratic models with d <= 256, at most 64 groups and
                                       1024 workers run free-running steps of the default rule as ONE launch of a
                                       single thread-block cluster per gcada_step call, whatever n_iters is (the
@@ -197,7 +199,7 @@ gcada_status gcada_set_step_schedule(gcada_ctx *ctx, int kind, double a, double 
  *     H <- beta1 H + (1 - beta1) A   (Eq. 8a),   U = nesterov ? beta1 H + (1 - beta1) A : H,
  *     W <- (1 - alpha^k weight_decay) W - alpha^k scale sqrt(max(1, rows / cols)) O,
  *   O = U orthogonalised by `steps` Newton-Schulz steps (gcada_orthogonalize with its default coefficients and eps
- *   1e-7; GCADA_PRECISION_FULL for the fp32 MLP, _HALF for the bf16 one); the biases keep Eq. (8a)-(8c).  The step
+ *   1e-7, in the precision that GCADA_OPT_SERVER_PRECISION names); the biases keep Eq. (8a)-(8c).  The step
  *   norms of Eq. (9) are those of the whole parameter vector, whatever the rule.  GCADA_EINVAL for logistic / quadratic
  *   models and unless weight_decay >= 0, scale > 0, 1 <= steps <= 100.  Like options, the rule is not part of a
  *   checkpoint. */

@@ -19,7 +19,7 @@ OK, EINVAL, ENOMEM, ECUDA, ESTATE, ETIMEOUT = range(6)
 MODEL_LOGISTIC, MODEL_MLP, MODEL_QUADRATIC = 0, 1, 2
 COMPUTE_FP32, COMPUTE_BF16 = 0, 1
 (OPT_RULE, OPT_REDUCTION, OPT_HISTORY, OPT_KEEP_STALE, OPT_GRAPH, OPT_TIMING, _OPT_UNUSED,
- OPT_PERSISTENT, OPT_UPLOAD) = range(9)
+ OPT_PERSISTENT, OPT_UPLOAD, OPT_SERVER_PRECISION) = range(10)
 UPLOAD_FULL, UPLOAD_MXFP4 = 0, 1
 (DBG_FRESH, DBG_STALE, DBG_LHS, DBG_RHS, DBG_TAU, DBG_AGG, DBG_H, DBG_VHAT, DBG_TGROUP, DBG_GLAST,
  DBG_SRING) = range(11)

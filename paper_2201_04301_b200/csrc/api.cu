@@ -62,6 +62,7 @@ struct gcada_ctx {
   MlpPlan mlp{};
   int server_rule = GCADA_SERVER_AMSGRAD;
   int upload = GCADA_UPLOAD_FULL;
+  int server_precision = GCADA_PRECISION_FULL;
   MuonPlan muon{};
   unsigned char* forced_dev = nullptr;
   size_t forced_cap = 0;
@@ -318,6 +319,7 @@ gcada_status make_plans(gcada_ctx* ctx) {
       TRY(dev_alloc(ctx, &work, muon_work_bytes(ctx->mlp)));
       ctx->muon.work = work;
       ctx->muon.beta = ctx->beta1;
+      ctx->muon.full = ctx->server_precision == GCADA_PRECISION_FULL;
     }
   }
   if (ctx->rule == 1) {
@@ -765,6 +767,11 @@ gcada_status gcada_set_option(gcada_ctx* ctx, int key, double value) {
       if (value != GCADA_UPLOAD_FULL && value != GCADA_UPLOAD_MXFP4) return fail(ctx, GCADA_EINVAL, "upload must be 0 (full) or 1 (MXFP4)");
       if (value == GCADA_UPLOAD_MXFP4 && !factored(ctx)) return fail(ctx, GCADA_EINVAL, "4-bit uploads need the bf16 MLP (the other models upload gradients, not factors)");
       ctx->upload = (int)value;
+      break;
+    case GCADA_OPT_SERVER_PRECISION:
+      if (value != GCADA_PRECISION_FULL && value != GCADA_PRECISION_HALF) return fail(ctx, GCADA_EINVAL, "server precision must be 0 (full) or 1 (half)");
+      if (is_linear(ctx)) return fail(ctx, GCADA_EINVAL, "the server precision is that of rule Muon: an MLP");
+      ctx->server_precision = (int)value;
       break;
     case GCADA_OPT_PERSISTENT:
       ctx->persistent = value != 0;

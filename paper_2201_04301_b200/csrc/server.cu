@@ -159,7 +159,7 @@ cudaError_t launch_muon_update(const Params& P, const MlpPlan& pl, const MuonPla
     p.coef[1] = -4.7750;
     p.coef[2] = 2.0315;
     p.eps = 1e-7;
-    p.full = pl.compute == 0;  // fp32 model: fp32 accuracy
+    p.full = m.full;
     p.err = &P.st->err;
     const char* why = "";
     int n = 0;

@@ -11,6 +11,7 @@ namespace gcada {
 struct MuonPlan {
   double beta = 0, weight_decay = 0, scale = 1;
   int nesterov = 1, steps = 5;
+  int full = 1;                 // 0: products of 11-bit operands
   NsTarget* targets = nullptr;  // [n_layers + 1] device: where layer l's weights come from and go to this iteration
   void* work = nullptr;
 };

@@ -77,6 +77,38 @@ def test_muon_steps(kw, rule):
     g.close()
 
 
+@pytest.mark.parametrize("kw", [BF16, ODD16, WIDE], ids=["bf16", "bf16-odd", "fp32-wide"])
+def test_the_rule_s_precision_is_full_unless_half_is_asked_for(kw):
+    """The first step from the same iterate: weights, momentum and aggregate are fp32, so fp32 accuracy is what a network gets
+    without asking, whatever its own products round to."""
+    w = workload(kw)
+    theta = w["theta0"].numpy().astype(np.float64)
+    moved = {}
+    for name, options in (("default", {}), ("full", {binding.OPT_SERVER_PRECISION: 0}), ("half", {binding.OPT_SERVER_PRECISION: 1})):
+        g = binding.from_workload(to_cuda(w), stream=torch.cuda.Stream(), options=options, server_rule=dict(rule="muon"))
+        g.step(1)
+        moved[name], h, vh, agg = state(g)
+        g.close()
+        for rows, cols, W, b in layers(w["dims"]):
+            s = math.sqrt(max(1.0, rows / cols))
+            want, _ = om.muon(theta[W].reshape(rows, cols), np.zeros((rows, cols)), agg[W].reshape(rows, cols), w["alpha"],
+                              w["beta1"], True, 0.0, s)
+            err = np.linalg.norm(moved[name][W].reshape(rows, cols) - want)
+            tol = HALF_TOL if name == "half" else FULL_TOL
+            assert err <= tol * w["alpha"] * s * 1.3 * math.sqrt(min(rows, cols)) + 2.0 ** -22 * np.linalg.norm(want), (name, rows, cols)
+    assert np.array_equal(moved["default"], moved["full"]) and not np.array_equal(moved["full"], moved["half"])
+    g = binding.from_workload(to_cuda(w), stream=torch.cuda.Stream())
+    for bad in (2, -1, 0.5):
+        with pytest.raises(binding.GCadaError) as e:
+            g.set_option(binding.OPT_SERVER_PRECISION, bad)
+        assert e.value.status == binding.EINVAL
+    g.close()
+    lin = binding.from_workload(to_cuda(make_workload("cfg1", rows=300)), stream=torch.cuda.Stream())
+    with pytest.raises(binding.GCadaError) as e:
+        lin.set_option(binding.OPT_SERVER_PRECISION, 1)
+    assert e.value.status == binding.EINVAL
+    lin.close()
+
 @pytest.mark.parametrize("kw", [FP32, BF16], ids=["fp32", "bf16"])
 def test_the_aggregate_under_muon_is_the_sum_of_uploads(kw):
     w = workload(kw)
