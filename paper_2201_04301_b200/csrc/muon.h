@@ -52,6 +52,12 @@ struct NsProblem {
   int full;             // 1: products of hi / lo pairs (fp32 accuracy), 0: of the hi parts
   int* err = nullptr;   // device error word, or null
 };
+// Exponent of the smallest power of two that is at least max(1, |a|): what a step multiplies a tiny iterate by.
+inline int ns_growth(double a) {
+  int g = 0;
+  while ((double)(1 << g) < (a < 0 ? -a : a)) ++g;
+  return g;
+}
 // Narrow matrices, all steps on chip (muon_cluster.cu).
 constexpr int NS_NARROW = 64;  // short side
 bool ns_fits_cluster(int batch, int rows, int cols);

@@ -28,6 +28,7 @@ struct NcArgs {
   int r, c, cs;   // short and long side; columns of the long side per CTA
   int rp, csp;    // padded row length (4 x odd: rows start in different banks) and slice length (multiple of 4)
   int tall, csize, steps;
+  int growth;     // see ns_growth
   int direct;     // every CTA reads all shares of A
   float a, b, cc;
   double eps;
@@ -146,7 +147,11 @@ __global__ void __launch_bounds__(NC_THREADS, 1) ns_cluster_kernel(const NsSourc
     ss += n.csize > 1 ? cluster_load_f64(cluster_map(smem_u32(share + w), (uint32_t)p)) : share[w];
   }
   ss = warp_sum(ss);
-  const double inv = 1.0 / (sqrt(ss) + n.eps);
+  // A norm far below eps would leave X_0 to fp32's subnormal numbers: the iterate is then kept times 2^-rho, rho as in
+  // muon.cu (0 for all others, and every factor that follows from it 1)
+  const double size = sqrt(ss) / (sqrt(ss) + n.eps);
+  int rho = size > 0.0 && size < 0x1p-60 ? ilogb(size) : 0;
+  const double inv = ldexp(1.0 / (sqrt(ss) + n.eps), -rho);
   for (int e = tid; e < kn * rp; e += threads) X[e] = (float)((double)X[e] * inv);
   __syncthreads();
 
@@ -186,8 +191,11 @@ __global__ void __launch_bounds__(NC_THREADS, 1) ns_cluster_kernel(const NsSourc
     } else {
       __syncthreads();
     }
-    symmetric_product(poly, A, n.r, rp, Q, A, n.b, n.cc);
+    symmetric_product(poly, A, n.r, rp, Q, A, ldexpf(n.b, 2 * rho), ldexpf(n.cc, 4 * rho));
     __syncthreads();
+    const int next = min(rho + n.growth, 0);
+    const float grown = ldexpf(1.f, rho - next), an = n.a * grown;
+    rho = next;
     // Y = a X + X Q: 4 columns of the slice x 4 rows a thread
     for (int base = 0; base < items << lk; base += threads) {
       const int id = base + tid, item = id >> lk, p = id & ((1 << lk) - 1);
@@ -227,7 +235,7 @@ __global__ void __launch_bounds__(NC_THREADS, 1) ns_cluster_kernel(const NsSourc
         for (int t = 0; t < 4; ++t) {
           const float4 v = *reinterpret_cast<const float4*>(x + t * rp + 4 * ti);
           *reinterpret_cast<float4*>(Y + (size_t)(kg * 4 + t) * rp + 4 * ti) =
-              make_float4(n.a * v.x + acc[t][0], n.a * v.y + acc[t][1], n.a * v.z + acc[t][2], n.a * v.w + acc[t][3]);
+              make_float4(an * v.x + grown * acc[t][0], an * v.y + grown * acc[t][1], an * v.z + grown * acc[t][2], an * v.w + grown * acc[t][3]);
         }
       }
     }
@@ -243,7 +251,7 @@ __global__ void __launch_bounds__(NC_THREADS, 1) ns_cluster_kernel(const NsSourc
     const int i = n.tall ? w : q, k = n.tall ? q : w;
     const long long row = n.tall ? k0 + k : i, col = n.tall ? i : k0 + k;
     const long long at = (long long)b * o.stride + row * o.ld + col;
-    const float v = X[k * rp + i];
+    const float v = ldexpf(X[k * rp + i], rho);
     if (o.bf16)
       static_cast<__nv_bfloat16*>(to.o)[at] = __float2bfloat16_rn(
           o.update ? to.decay * __bfloat162float(static_cast<const __nv_bfloat16*>(to.prev)[at]) - to.step * v : v);
@@ -301,6 +309,7 @@ cudaError_t launch_ns_cluster(const NsSource& s, const NsSink& o, int batch, con
   n.a = coef[0];
   n.b = coef[1];
   n.cc = coef[2];
+  n.growth = ns_growth(coef[0]);
   n.eps = eps;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(batch * n.csize));

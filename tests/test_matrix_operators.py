@@ -653,3 +653,22 @@ def test_the_precision_is_full_unless_half_is_asked_for():
             binding.muon_update(w, m, g, lr=0.1, precision=precision)
             results.append(w)
         assert torch.equal(results[0], results[1]) and not torch.equal(results[0], results[2])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(100, 150), (150, 100), (300, 300), (10, 200), (60, 40), (4, 4)])
+def test_norms_far_below_eps(shape):
+    """The largest eps with matrices so small that X_0 is beyond fp32's range: results of the formula's size, not NaN, and no
+    digits lost on the way to results that are in range again."""
+    g = torch.from_numpy(spectrum(*shape, "gauss")).float().cuda()
+    grow = (1.875, -1.25, 0.375)                                # a tiny iterate grows 1.875-fold a step, 2e27-fold in a hundred
+    for factor, eps in ((1e-20, 1e30), (1e-30, 1e20), (1e-38, 1e30), (1e-12, 1e30), (1.0, 1e30), (1e-38, 1e-7), (1e-25, 1e-20)):
+        h = g * factor
+        for steps, coef in ((0, om.COEF), (1, om.COEF), (5, om.COEF), (100, grow)):
+            o = num(binding.orthogonalize(h, steps=steps, coef=coef, eps=eps))
+            want = om.newton_schulz(num(h), steps, coef, eps)
+            # every step rounds the iterate to 22 bits; numbers below fp32's normal range have its smallest step, 2^-149, and a
+            # last factor in that range 2^-149 of 1.2e-38 / 2^10
+            tol = (FULL_TOL + steps * 2.0 ** -21) * np.linalg.norm(want) + 2.0 ** -138 * np.sqrt(want.size)
+            assert np.linalg.norm(o - want) <= tol, (factor, eps, steps)
+    binding.check_operators()
