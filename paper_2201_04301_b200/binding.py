@@ -430,13 +430,20 @@ class _Launch:
                     t.record_stream(self.other)
 
 
+def _status_word(index):
+    """The device's status word as a tensor, or None if no operator has run there."""
+    return _status_words.get(index)
+
+
 def check_operators(device=None):
-    """Waits for the device and raises (GCADA_ETIMEOUT) if a kernel of the matrix operators ever gave up a wait
-    there since the last check."""
+    """Waits for the device (by default, and for "cuda", the current one) and raises (GCADA_ETIMEOUT) if a kernel of the
+    matrix operators ever gave up a wait there since the last check."""
     import torch
-    index = torch.cuda.current_device() if device is None else torch.device(device).index
+    index = device if isinstance(device, int) else None if device is None else torch.device(device).index
+    if index is None:
+        index = torch.cuda.current_device()
     torch.cuda.synchronize(index)
-    w = _status_words.get(index)
+    w = _status_word(index)
     if w is not None and int(w.item()):
         w.zero_()
         raise GCadaError(ETIMEOUT, "a bounded device-side wait of a matrix operator gave up")

@@ -672,3 +672,17 @@ def test_norms_far_below_eps(shape):
             tol = (FULL_TOL + steps * 2.0 ** -21) * np.linalg.norm(want) + 2.0 ** -138 * np.sqrt(want.size)
             assert np.linalg.norm(o - want) <= tol, (factor, eps, steps)
     binding.check_operators()
+
+
+# ------------------------------------------------------------------------------------------- status, memory, autograd
+@pytest.mark.gpu
+@pytest.mark.parametrize("device", [None, "cuda", 0, "cuda:0"])
+def test_a_wait_that_gave_up_is_reported_once(device):
+    """The word is set from the host; no wait runs out."""
+    binding.orthogonalize(torch.ones(4, 4, device="cuda"))
+    binding.check_operators(device)
+    binding._status_word(0).fill_(1)
+    with pytest.raises(binding.GCadaError) as e:
+        binding.check_operators(device if device is None or isinstance(device, int) else torch.device(device))
+    assert e.value.status == binding.ETIMEOUT
+    binding.check_operators(device)
