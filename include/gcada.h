@@ -339,6 +339,10 @@ gcada_status gcada_innovation_norms_noalloc(const float *fresh_dev, const float 
  * throws or aborts.
  */
 
+/* A status word for callers who keep none: the library's own on the current device, zero when the library is loaded, at one
+ * address for the life of the process.  It may be asked for while a graph is captured. */
+gcada_status gcada_operator_status(int **word_dev);
+
 /* How the products of an orthogonalisation are formed.  Both keep the iterate in 22 bits and accumulate in fp32.
  * FULL: operands of 22 bits, the accuracy of fp32 arithmetic (three tensor-core products for one).
  * HALF: operands of 11 bits, for callers to whom speed matters more.  Five steps with the default coefficients: within

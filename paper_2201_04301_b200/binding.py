@@ -70,6 +70,7 @@ SIGNATURES = {
     "gcada_get_launch_count": (C.c_int, [_VP, _ULLP]),
     "gcada_get_kernel_times": (C.c_int, [_VP, C.POINTER(C.c_double), C.POINTER(C.c_int)]),
     "gcada_innovation_norms_noalloc": (C.c_int, [_VP, _VP, C.c_int, _LL, _LL, _VP, _VP, C.c_char_p, C.c_size_t]),
+    "gcada_operator_status": (C.c_int, [C.POINTER(_VP)]),
     "gcada_orthogonalize_work": (C.c_int, [C.c_int, C.c_int, C.c_int, C.POINTER(C.c_size_t)]),
     "gcada_orthogonalize": (C.c_int, [_VP, _VP] + [C.c_int] * 4 + [_LL] * 4 + [C.c_int] * 2 +
                             [C.POINTER(C.c_double), C.c_double, _VP, C.c_size_t, _VP, _VP, C.c_char_p, C.c_size_t]),
@@ -347,7 +348,7 @@ PRECISIONS = {"full": 0, "half": 1}
 MUON_COEF = (3.4445, -4.7750, 2.0315)
 _NO_WORK = 256       # a work area of this size is asked for, but not used (narrow matrices stay on chip)
 _unused_work = {}    # device index -> one such area, shared by every call
-_status_words = {}   # device index -> an int32 tensor that a kernel whose bounded wait gave up makes non-zero
+_status_words = {}   # device index -> address of the word that a kernel whose bounded wait gave up makes non-zero
 
 
 def _compute_type(t, what):
@@ -407,11 +408,13 @@ class _Launch:
     def status(self):
         w = _status_words.get(self.index)
         if w is None:
-            if self.torch.cuda.is_current_stream_capturing():
-                return None   # a word made now would belong to the graph being captured
-            w = _status_words[self.index] = self.torch.zeros(1, dtype=self.torch.int32, device=self.device)
-            self.torch.cuda.current_stream(self.device).synchronize()
-        return w.data_ptr()
+            word = _VP()
+            with self.torch.cuda.device(self.index):
+                st = self.lib.gcada_operator_status(C.byref(word))
+            if st != OK:
+                raise GCadaError(st, "no status word on device %d" % self.index)
+            w = _status_words[self.index] = word.value
+        return w
 
     def call(self, fn, args, tensors):
         buf = getattr(_messages, "buf", None)
@@ -430,14 +433,23 @@ class _Launch:
                     t.record_stream(self.other)
 
 
+class _Word:
+    """One int32 at a device address, for torch.as_tensor."""
+
+    def __init__(self, address):
+        self.__cuda_array_interface__ = dict(shape=(1,), typestr="<i4", data=(address, False), version=2)
+
+
 def _status_word(index):
     """The device's status word as a tensor, or None if no operator has run there."""
-    return _status_words.get(index)
+    import torch
+    w = _status_words.get(index)
+    return None if w is None else torch.as_tensor(_Word(w), device=torch.device("cuda", index))
 
 
 def check_operators(device=None):
     """Waits for the device (by default, and for "cuda", the current one) and raises (GCADA_ETIMEOUT) if a kernel of the
-    matrix operators ever gave up a wait there since the last check."""
+    matrix operators ever gave up a wait there since the last check, in the replay of a graph too."""
     import torch
     index = device if isinstance(device, int) else None if device is None else torch.device(device).index
     if index is None:

@@ -37,6 +37,8 @@ bool aligned_to(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p
 
 constexpr long long MAX_SIDE = 1 << 20;  // rows or columns of a matrix
 
+__device__ int own_status_word;  // gcada_operator_status: zero when the library is loaded, one on every device
+
 const double DEFAULT_COEF[3] = {3.4445, -4.7750, 2.0315};
 
 gcada_status check_steps(int precision, int steps, const double* coef, double eps, char* errbuf, size_t errbuf_len) {
@@ -50,6 +52,14 @@ gcada_status check_steps(int precision, int steps, const double* coef, double ep
 }  // namespace
 
 extern "C" {
+
+gcada_status gcada_operator_status(int** word_dev) {
+  if (!word_dev) return GCADA_EINVAL;
+  void* p = nullptr;
+  if (cudaGetSymbolAddress(&p, own_status_word) != cudaSuccess) return *word_dev = nullptr, GCADA_ECUDA;
+  *word_dev = static_cast<int*>(p);
+  return GCADA_OK;
+}
 
 gcada_status gcada_orthogonalize_work(int batch, int rows, int cols, size_t* bytes) {
   if (!bytes || batch < 0 || rows < 0 || cols < 0 || rows > MAX_SIDE || cols > MAX_SIDE) return GCADA_EINVAL;

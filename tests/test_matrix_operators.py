@@ -686,3 +686,42 @@ def test_a_wait_that_gave_up_is_reported_once(device):
         binding.check_operators(device if device is None or isinstance(device, int) else torch.device(device))
     assert e.value.status == binding.ETIMEOUT
     binding.check_operators(device)
+
+
+FIRST_CALL_CAPTURED = """
+import sys
+sys.path.insert(0, {root!r})
+import torch
+from paper_2201_04301_b200 import binding
+x = torch.randn(130, 200, device="cuda")
+n = torch.randn(10, 90, device="cuda")
+out, small, prod = torch.zeros_like(x), torch.zeros_like(n), torch.zeros(130, 130, device="cuda")
+graph = torch.cuda.CUDAGraph()
+torch.cuda.synchronize()
+with torch.cuda.graph(graph):
+    binding.orthogonalize(n, out=small)
+    binding.orthogonalize(x, out=out)
+    q = binding.mx_quantize(x)
+    binding.mx_gemm(q, q, out=prod)
+graph.replay()
+torch.cuda.synchronize()
+binding.check_operators("cuda")
+word = binding._status_words[0]
+assert word, "the captured kernels have no status word"
+assert torch.equal(out, binding.orthogonalize(x)) and torch.equal(small, binding.orthogonalize(n))
+q = binding.mx_quantize(x)
+assert torch.equal(prod, binding.mx_gemm(q, q))
+assert binding._status_words[0] == word
+print("same")
+"""
+
+
+@pytest.mark.gpu
+def test_the_first_calls_of_a_process_may_be_captured():
+    """... and their kernels know the status word that check_operators reads."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALL_CAPTURED.format(root=root)], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "same" in r.stdout, r.stderr[-2000:]
