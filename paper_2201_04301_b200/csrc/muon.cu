@@ -404,6 +404,8 @@ __global__ void __launch_bounds__(THREADS, 1) ns_gemm_kernel(const __grid_consta
     if (!ok && leader) raise_error(a.err);
   } else if (warp == 1) {
     if (leader && (!PAIR || rank == 0)) {
+      // its bounded waits count from here: a predecessor that let this kernel start early may run for any time
+      pdl_wait();
       // fp16 operands, fp32 sum
       constexpr uint32_t IDESC = (1u << 4) | ((uint32_t)(TN >> 3) << 17) | ((uint32_t)(TM >> 4) << 24);
       bool ok = true;

@@ -679,6 +679,8 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
     if (!ok && leader) raise_error(p.err);
   } else if (warp == 1) {
     if (leader && (!PAIR || rank == 0)) {
+      // its bounded waits count from here: a predecessor that let this kernel start early may run for any time
+      pdl_wait();
       // E2M1 operands (1 at bits 7 and 10), E8M0 scales (bit 23); bits 29 / 4: which pair of a column's four scale
       // bytes an instruction's two blocks take
       constexpr uint32_t IDESC =

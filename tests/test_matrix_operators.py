@@ -725,3 +725,45 @@ def test_the_first_calls_of_a_process_may_be_captured():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", FIRST_CALL_CAPTURED.format(root=root)], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "same" in r.stdout, r.stderr[-2000:]
+
+
+BUSY = """
+// Lets the kernels behind it start at once, then keeps one thread asleep for `ns` nanoseconds (ten seconds at most).
+__global__ void busy_kernel(long long ns) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  long long t0, t;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
+  do {
+    __nanosleep(1000);
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+  } while (t - t0 < ns && t - t0 < 10000000000LL);
+}
+extern "C" int busy(void* stream, long long ns) {
+  busy_kernel<<<1, 1, 0, static_cast<cudaStream_t>(stream)>>>(ns);
+  return (int)cudaGetLastError();
+}
+"""
+
+
+@pytest.mark.gpu
+def test_a_long_predecessor_that_lets_them_start_early(tmp_path):
+    """The kernels' bounded waits (a second or so) begin when their predecessor has finished: one that runs for longer, but lets
+    the next kernels become resident meanwhile, is no failure."""
+    import subprocess
+    from paper_2201_04301_b200 import build
+    src, so = tmp_path / "busy.cu", tmp_path / "busy.so"
+    src.write_text(BUSY)
+    subprocess.run(["nvcc", *build.NVCC_FLAGS, "-shared", "-o", str(so), str(src)], check=True, capture_output=True)
+    busy = binding.C.CDLL(str(so)).busy
+    busy.argtypes = [binding.C.c_void_p, binding.C.c_longlong]
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    mats = [torch.randn(s, generator=gen, device="cuda") for s in ((130, 300), (600, 700), (10, 200))]
+    a, b = (binding.mx_quantize(torch.randn(s, generator=gen, device="cuda")) for s in ((300, 4000), (500, 4000)))
+    calls = [lambda g=g: binding.orthogonalize(g) for g in mats] + [lambda: binding.mx_gemm(a, b)]
+    want = [f() for f in calls]
+    binding.check_operators()
+    for f, w in zip(calls, want):
+        assert busy(torch.cuda.current_stream().cuda_stream, 2_500_000_000) == 0
+        o = f()
+        binding.check_operators()
+        assert torch.equal(o, w)
