@@ -344,6 +344,15 @@ gcada_status make_plans(gcada_ctx* ctx) {
   return GCADA_OK;
 }
 
+// Back to iteration 0 of the same theta^0, with no plans: for settings that change what the plans allocate.
+gcada_status rebuild(gcada_ctx* ctx) {
+  DeviceGuard dg(ctx->device);
+  std::vector<float> th((size_t)ctx->p);
+  CK(cudaStreamSynchronize(ctx->stream));
+  CK(cudaMemcpy(th.data(), ctx->P.theta_ring, sizeof(float) * ctx->p, cudaMemcpyDeviceToHost));
+  return make_ready(ctx, th.data(), 0);
+}
+
 // The server's update (the last kernels of an iteration); its launches are counted.
 gcada_status enqueue_update(gcada_ctx* ctx, const Params& P) {
   int n = 1;
@@ -691,9 +700,8 @@ gcada_status gcada_set_lag_weights(gcada_ctx* ctx, const double* c_d, int D) {
       if (!(c_d[d] >= 0)) return fail(ctx, GCADA_EINVAL, "lag weights must be non-negative");
     ctx->c_d.assign(c_d, c_d + D);
   }
-  ctx->ready = false;  // the device copy is made with the plans
   drop_graphs(ctx);
-  return GCADA_OK;
+  return ctx->ready ? rebuild(ctx) : GCADA_OK;  // the device copy is made with the plans
 }
 
 gcada_status gcada_set_step_schedule(gcada_ctx* ctx, int kind, double a, double b) {
@@ -733,9 +741,8 @@ gcada_status gcada_set_server_rule(gcada_ctx* ctx, int rule, double weight_decay
     ctx->muon.steps = steps;
   }
   ctx->server_rule = rule;
-  ctx->ready = false;  // the work area is made with the plans
   drop_graphs(ctx);
-  return GCADA_OK;
+  return ctx->ready ? rebuild(ctx) : GCADA_OK;  // the work area is made with the plans
 }
 
 gcada_status gcada_set_option(gcada_ctx* ctx, int key, double value) {
@@ -784,14 +791,7 @@ gcada_status gcada_set_option(gcada_ctx* ctx, int key, double value) {
       return fail(ctx, GCADA_EINVAL, "unknown option %d", key);
   }
   // options change buffer shapes: rebuild lazily at the next set_theta
-  if (ctx->have_theta) {
-    DeviceGuard dg(ctx->device);
-    std::vector<float> th((size_t)ctx->p);
-    CK(cudaStreamSynchronize(ctx->stream));
-    CK(cudaMemcpy(th.data(), ctx->P.theta_ring, sizeof(float) * ctx->p, cudaMemcpyDeviceToHost));
-    return make_ready(ctx, th.data(), 0);
-  }
-  return GCADA_OK;
+  return ctx->have_theta ? rebuild(ctx) : GCADA_OK;
 }
 
 gcada_status gcada_set_smoothness(gcada_ctx* ctx, const double* L, int G) {
@@ -802,9 +802,8 @@ gcada_status gcada_set_smoothness(gcada_ctx* ctx, const double* L, int G) {
   if (ctx->k_host > 0) return fail(ctx, GCADA_ESTATE, "the smoothness constants are fixed once stepping has begun");
   ctx->L2.resize(G);
   for (int g = 0; g < G; ++g) ctx->L2[g] = L[g] * L[g];
-  ctx->ready = false;  // the device copy is made with the plans
   drop_graphs(ctx);
-  return GCADA_OK;
+  return ctx->ready ? rebuild(ctx) : GCADA_OK;  // the device copy is made with the plans
 }
 
 static gcada_status run_iterations(gcada_ctx* ctx, int n_iters, const unsigned char* mask) {

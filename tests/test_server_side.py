@@ -248,6 +248,28 @@ def test_padding_rows_take_no_part_in_an_uploads_scales(batch):
     g.close()
 
 
+def test_settings_made_after_the_plans_leave_no_second_set_of_buffers():
+    """Timing the gradient builds the plans; a rule, lag weights or smoothness constants set then replace them."""
+    w = to_cuda(workload(dict(BF16, rows=64 * 300, dims=(256, 1024, 1024, 40), M=64, M_G=1, batch=256)))
+    g = binding.from_workload(w, stream=torch.cuda.Stream())
+    theta = g.get_theta()
+    g.time_gradient(1)
+    free = []
+    for setting in (lambda: g.set_server_rule("muon"), lambda: g.set_lag_weights([0.3] * w["D"]), lambda: g.set_smoothness([1.0] * g.G),
+                    lambda: g.set_server_rule("muon", scale=0.5), lambda: g.set_server_rule("amsgrad"), lambda: g.set_server_rule("muon", scale=0.5)):
+        setting()
+        g.time_gradient(1)
+        torch.cuda.synchronize()
+        free.append(torch.cuda.mem_get_info()[0])
+    assert free[0] - min(free) < 64 << 20, free               # the plans' buffers are 0.6 GB
+    assert np.array_equal(g.get_theta(), theta)
+    g.step(2)
+    other = binding.from_workload(w, stream=torch.cuda.Stream(), server_rule=dict(rule="muon", scale=0.5))
+    other.step(2)
+    assert np.array_equal(g.get_theta(), other.get_theta())
+    g.close()
+    other.close()
+
 def test_refusals():
     lin = binding.from_workload(to_cuda(make_workload("cfg1", rows=300)), stream=torch.cuda.Stream())
     fp32 = binding.from_workload(to_cuda(workload(FP32)), stream=torch.cuda.Stream())
