@@ -496,7 +496,9 @@ def _ns_work(run, batch, rows, cols, work):
         else:
             work = _unused_work.get(run.index)
             if work is None:
-                work = _unused_work[run.index] = run.fresh(_NO_WORK, dtype=run.torch.uint8)
+                work = run.fresh(_NO_WORK, dtype=run.torch.uint8)
+                if not run.torch.cuda.is_current_stream_capturing():   # (a graph's own memory goes with the graph)
+                    _unused_work[run.index] = work
     elif not work.is_contiguous():
         raise ValueError("work must be contiguous")
     return work, work.data_ptr(), work.numel() * work.element_size()

@@ -767,3 +767,38 @@ def test_a_long_predecessor_that_lets_them_start_early(tmp_path):
         o = f()
         binding.check_operators()
         assert torch.equal(o, w)
+
+
+NOTHING_KEPT_OF_A_CAPTURE = """
+import sys
+sys.path.insert(0, {root!r})
+import torch
+from paper_2201_04301_b200 import binding
+x = torch.randn(10, 90, device="cuda")
+out, graph = torch.zeros_like(x), torch.cuda.CUDAGraph()
+torch.cuda.synchronize()
+with torch.cuda.graph(graph):
+    binding.orthogonalize(x, out=out)
+    binding.muon_update(torch.zeros_like(x), torch.zeros_like(x), x, lr=0.1)
+graph.replay()
+torch.cuda.synchronize()
+private = [s for s in torch.cuda.memory_snapshot() if tuple(s["segment_pool_id"]) != (0, 0)]
+assert private, "the capture had no memory of its own"
+del graph
+torch.cuda.empty_cache()
+assert not [s for s in torch.cuda.memory_snapshot() if tuple(s["segment_pool_id"]) != (0, 0)], "a part of the graph's memory is held"
+first = binding.orthogonalize(x)
+assert torch.equal(first, out) and binding._unused_work
+print("same")
+"""
+
+
+@pytest.mark.gpu
+def test_nothing_of_a_graph_s_memory_outlives_it():
+    """The area that narrow matrices hand over but do not use is kept for later calls, unless a graph's memory pool made it."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", NOTHING_KEPT_OF_A_CAPTURE.format(root=root)], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "same" in r.stdout, r.stderr[-2000:]
