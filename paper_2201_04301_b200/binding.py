@@ -342,7 +342,11 @@ def innovation_norms_noalloc(fresh, stale, lhs_out, stream=None):
 # ---------------------------------------------------------------------------
 # Matrix operators (gcada_orthogonalize, gcada_muon_update, gcada_mx_*).  Tensors live on one CUDA device, which
 # need not be the current one; their last dimension is contiguous.  stream: a torch.cuda.Stream, a raw cudaStream_t
-# integer, or None for torch's current stream of that device.
+# integer, or None for torch's current stream of that device.  On another stream than the current one the caller orders the
+# inputs' writers before the call; what the call itself takes from torch's allocator (a result without `out`, a work area
+# without `work`) makes that stream wait for all that the current one holds, so calls that are to run beside it bring both.
+# None of them is differentiable: results carry no gradient, whatever the inputs require.  Tensors that a call writes
+# have their version counters raised, as by torch's own in-place operations.
 # ---------------------------------------------------------------------------
 PRECISIONS = {"full": 0, "half": 1}
 MUON_COEF = (3.4445, -4.7750, 2.0315)
@@ -416,7 +420,8 @@ class _Launch:
             w = _status_words[self.index] = word.value
         return w
 
-    def call(self, fn, args, tensors):
+    def call(self, fn, args, tensors, written=()):
+        """`written`: what the caller gave to be written."""
         buf = getattr(_messages, "buf", None)
         if buf is None:
             buf = _messages.buf = C.create_string_buffer(256)   # one a thread
@@ -427,6 +432,8 @@ class _Launch:
                 st = fn(*args, self.raw, buf, 256)
         if st != OK:
             raise GCadaError(st, buf.value.decode())
+        if written:
+            self.torch.autograd.graph.increment_version(written)
         if self.other is not None:
             for t in tensors:
                 if t is not None:
@@ -512,7 +519,7 @@ def orthogonalize(g, out=None, steps=5, coef=MUON_COEF, eps=1e-7, precision=None
     orthogonalize_work(g) bytes to use as the work area, by default taken from torch's allocator."""
     kind, ld_g = _compute_type(g, "g"), _matrix(g, "g", (2, 3))
     run = _Launch(g, (out, work), stream)
-    shape = g.shape
+    shape, written = g.shape, () if out is None else (out,)
     if out is None:
         out = run.torch.empty_like(g) if run.other is None and g.is_contiguous() else run.fresh(*shape, dtype=g.dtype)
     elif out.shape != shape or out.dtype != g.dtype:
@@ -524,7 +531,7 @@ def orthogonalize(g, out=None, steps=5, coef=MUON_COEF, eps=1e-7, precision=None
     work, ptr, size = _ns_work(run, batch, rows, cols, work)
     run.call(run.lib.gcada_orthogonalize,
              (g.data_ptr(), out.data_ptr(), kind, batch, rows, cols, ld_g, stride_g, ld_o, stride_o, precision, steps,
-              coef, eps, ptr, size, run.status()), (g, out, work))
+              coef, eps, ptr, size, run.status()), (g, out, work), written)
     return out
 
 
@@ -554,7 +561,7 @@ def muon_update(w, m, g, lr, beta=0.95, nesterov=True, weight_decay=0.0, scale=N
     run.call(run.lib.gcada_muon_update,
              (w.data_ptr(), w_kind, m.data_ptr(), g.data_ptr(), g_kind, rows, cols, ld_w, ld_m, ld_g, float(lr),
               float(beta), int(bool(nesterov)), float(weight_decay), float(scale), precision, steps, coef, eps, ptr,
-              size, run.status()), (w, m, g, work))
+              size, run.status()), (w, m, g, work), (w, m))
 
 
 @functools.lru_cache(maxsize=256)
@@ -602,7 +609,7 @@ class MxMatrix:
 
     def dequantize(self, dtype=None, out=None, stream=None):
         """The values as a float32 (default) or bfloat16 tensor.  See gcada_mx_dequantize."""
-        run = _Launch(self._parts[0], (out,), stream)
+        run, written = _Launch(self._parts[0], (out,), stream), () if out is None else (out,)
         if out is None:
             out = run.fresh(self.rows, self.cols, dtype=dtype or run.torch.float32)
         elif tuple(out.shape) != (self.rows, self.cols) or (dtype is not None and out.dtype != dtype):
@@ -610,7 +617,7 @@ class MxMatrix:
         ld = _matrix(out, "out")
         run.call(run.lib.gcada_mx_dequantize,
                  (*self._where, self.rows, self.cols, out.data_ptr(), _compute_type(out, "out"), ld),
-                 (*self._parts, out))
+                 (*self._parts, out), written)
         return out
 
 
@@ -620,13 +627,14 @@ def mx_quantize(x, transpose=False, out=None, stream=None):
     kind, ld = _compute_type(x, "x"), _matrix(x, "x")
     rows, cols = x.shape
     shape = (cols, rows) if transpose else (rows, cols)
-    run = _Launch(x, () if out is None else out._parts, stream)
+    written = () if out is None else out._parts
+    run = _Launch(x, written, stream)
     if out is None:
         out = MxMatrix._fresh(run, *shape)
     elif (out.rows, out.cols) != shape:
         raise ValueError("out must be %d x %d" % shape)
     run.call(run.lib.gcada_mx_quantize,
-             (x.data_ptr(), kind, rows, cols, ld, 1 if transpose else 0, *out._where), (x, *out._parts))
+             (x.data_ptr(), kind, rows, cols, ld, 1 if transpose else 0, *out._where), (x, *out._parts), written)
     return out
 
 
@@ -635,7 +643,7 @@ def mx_gemm(a, b, out=None, dtype=None, alpha=1.0, beta=0.0, bias=None, stream=N
     tensor.  See gcada_mx_gemm.  `bias`: float32, n values."""
     if a.cols != b.cols:
         raise ValueError("a has %d columns and b %d" % (a.cols, b.cols))
-    run = _Launch(a._parts[0], (b._parts[0], out, bias), stream)
+    run, written = _Launch(a._parts[0], (b._parts[0], out, bias), stream), () if out is None else (out,)
     if out is None:
         if beta != 0:
             raise ValueError("beta needs out")
@@ -648,7 +656,7 @@ def mx_gemm(a, b, out=None, dtype=None, alpha=1.0, beta=0.0, bias=None, stream=N
     run.call(run.lib.gcada_mx_gemm,
              (*a._where, a.rows, *b._where, b.rows, a.cols, out.data_ptr(), _compute_type(out, "out"), ld, float(alpha),
               float(beta), None if bias is None else bias.data_ptr(), run.status()),
-             (*a._parts, *b._parts, out, bias))
+             (*a._parts, *b._parts, out, bias), written)
     return out
 
 

@@ -802,3 +802,40 @@ def test_nothing_of_a_graph_s_memory_outlives_it():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", NOTHING_KEPT_OF_A_CAPTURE.format(root=root)], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "same" in r.stdout, r.stderr[-2000:]
+
+
+@pytest.mark.gpu
+def test_written_tensors_have_their_versions_raised():
+    """Autograd then refuses a backward pass through a tensor that an operator has overwritten meanwhile."""
+    x = torch.randn(20, 40, device="cuda")
+    w = torch.randn(20, 40, device="cuda", requires_grad=True)
+    m, before = torch.zeros_like(x), w._version
+    loss = w.square().sum()                                     # keeps w for its backward pass
+    binding.muon_update(w, m, x, lr=0.1)
+    assert w._version > before and m._version > 0
+    with pytest.raises(RuntimeError, match="inplace operation"):
+        loss.backward()
+    q = binding.mx_quantize(x)
+    other = binding.MxMatrix(20, 40, q.codes.clone(), q.scales.clone())
+    for out, call in ((torch.zeros_like(x), lambda o: binding.orthogonalize(x, out=o)), (torch.zeros_like(x), lambda o: q.dequantize(out=o)),
+                      (torch.zeros(20, 20, device="cuda"), lambda o: binding.mx_gemm(q, q, out=o))):
+        version, of_x = out._version, x._version
+        call(out)
+        assert out._version > version and x._version == of_x
+    versions = other.codes._version, other.scales._version
+    binding.mx_quantize(x, out=other)
+    assert other.codes._version > versions[0] and other.scales._version > versions[1]
+    codes = q.codes._version
+    binding.mx_quantize(x, out=q)
+    assert q.codes._version > codes
+    with torch.inference_mode():                                # tensors without a version counter
+        y = torch.zeros(20, 40, device="cuda")
+        assert torch.equal(binding.orthogonalize(x, out=y), binding.orthogonalize(x))
+
+
+@pytest.mark.gpu
+def test_results_carry_no_gradient():
+    x = torch.randn(20, 40, device="cuda", requires_grad=True)
+    q = binding.mx_quantize(x)
+    for r in (binding.orthogonalize(x), binding.orthogonalize(x.T.contiguous()), q.codes, q.dequantize(), binding.mx_gemm(q, q)):
+        assert not r.requires_grad and r.grad_fn is None
