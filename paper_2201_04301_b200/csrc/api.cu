@@ -5,6 +5,7 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <memory>
 #include <new>
 #include <string>
 #include <vector>
@@ -347,10 +348,11 @@ gcada_status make_plans(gcada_ctx* ctx) {
 // Back to iteration 0 of the same theta^0, with no plans: for settings that change what the plans allocate.
 gcada_status rebuild(gcada_ctx* ctx) {
   DeviceGuard dg(ctx->device);
-  std::vector<float> th((size_t)ctx->p);
+  const std::unique_ptr<float[]> th(new (std::nothrow) float[(size_t)ctx->p]);  // (no exception leaves a C entry)
+  if (!th) return fail(ctx, GCADA_ENOMEM, "out of host memory");
   CK(cudaStreamSynchronize(ctx->stream));
-  CK(cudaMemcpy(th.data(), ctx->P.theta_ring, sizeof(float) * ctx->p, cudaMemcpyDeviceToHost));
-  return make_ready(ctx, th.data(), 0);
+  CK(cudaMemcpy(th.get(), ctx->P.theta_ring, sizeof(float) * ctx->p, cudaMemcpyDeviceToHost));
+  return make_ready(ctx, th.get(), 0);
 }
 
 // The server's update (the last kernels of an iteration); its launches are counted.
