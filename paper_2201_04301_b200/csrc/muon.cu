@@ -58,8 +58,8 @@ enum { OUT_SPLIT = 0, OUT_F32 = 1, OUT_BF16 = 2, OUT_UPDATE_F32 = 3, OUT_UPDATE_
 
 // A matrix whose norm is far below eps starts from an X_0 far below one, which fp16 pairs could not hold.  The stored
 // iterate is then SCALE * X_j / rho_j with powers of two rho_0 ~ ||X_0||, rho_{j+1} = min(1, rho_j g), g >= |a|: an
-// iterate that small grows by |a| a step.  For every other matrix all rho are 1.  They are kept as exponents: with the
-// largest eps and the smallest matrices rho_0 is 2^-250.
+// iterate that small grows by |a| a step.  For every other matrix all rho are 1.  With the largest eps and the smallest
+// matrices rho_0 is 2^-250, so what the steps need of it is formed from its exponent, each factor for itself.
 constexpr int MAX_STEPS = 100;
 enum { PROD_GRAM = 0, PROD_POLY = 1, PROD_APPLY = 2, PROD_LAST = 3 };
 
@@ -77,7 +77,8 @@ struct NsGemm {
   float diag;            // symmetric results: added on the diagonal (see ns_run on the shifted form)
   float c_src_shift;     // PROD_APPLY / PROD_LAST in the shifted form: added to c_src
   float c_src_plain;     // PROD_POLY in the shifted form: c_src where the form does not apply
-  const int* rho;        // [batch][MAX_STEPS + 1] log2 rho; entry step_no is that of the iterate the step starts from
+  const float4* rho;     // [batch][MAX_STEPS + 1] rho_j, rho_j^2, rho_j^4, rho_j / rho_{j+1}; entry step_no is that of the
+                         // iterate the step starts from
   int step_no;
   const __half* src;     // [batch][2][M][ld_src] hi / lo planes, or null
   long long ld_src, src_plane;
@@ -128,24 +129,20 @@ struct Coef {
 };
 __device__ __forceinline__ Coef coefficients(const NsGemm& a, int b) {
   Coef r;
-  const int* rho = a.rho + (long long)b * (MAX_STEPS + 1) + a.step_no;
-  const int r0 = rho[0];
-  const bool plain = r0 == 0;
+  const float4 rho = a.rho[(long long)b * (MAX_STEPS + 1) + a.step_no];
+  const bool plain = rho.x == 1.f;
   r.src = a.c_src;
   r.acc = a.c_acc;
-  r.diag = a.diag;
-  if (plain) {
-    if (a.prod >= PROD_APPLY) r.src += a.c_src_shift;
-    return r;
-  }
-  r.diag = 0.f;
+  r.diag = plain ? a.diag : 0.f;
   if (a.prod == PROD_POLY) {
-    r.src = ldexpf(a.c_src_plain, 2 * r0);
-    r.acc = ldexpf(r.acc, 4 * r0);
+    if (!plain) r.src = a.c_src_plain;
+    r.src *= rho.y;
+    r.acc *= rho.z;
   } else if (a.prod != PROD_GRAM) {
-    const int k = a.prod == PROD_APPLY ? r0 - rho[1] : r0;
-    r.src = ldexpf(r.src, k);
-    r.acc = ldexpf(r.acc, k);
+    const float k = a.prod == PROD_APPLY ? rho.w : rho.x;
+    if (plain) r.src += a.c_src_shift;
+    r.src *= k;
+    r.acc *= k;
   }
   return r;
 }
@@ -673,7 +670,7 @@ __global__ void __launch_bounds__(256) ns_norm_kernel(const NsSource s, double* 
 
 // X_0 = source / (norm + eps), stored as SCALE * X_0 / rho_0 = hi + lo; and the rho_j.
 __global__ void __launch_bounds__(256) ns_scale_kernel(const NsSource s, const double* part, int n_part, double eps,
-                                                       int growth, int steps, int* rho, __half* x, long long ld,
+                                                       int growth, int steps, float4* rho, __half* x, long long ld,
                                                        long long plane) {
   __shared__ double scratch[40];
   pdl_launch_dependents();
@@ -687,7 +684,11 @@ __global__ void __launch_bounds__(256) ns_scale_kernel(const NsSource s, const d
   const int rho0 = size > 0.0 && size < 0.0625 ? ilogb(size) : 0;
   const double k = ldexp((double)SCALE / (norm + eps), -rho0);
   if (blockIdx.x == 0 && threadIdx.x == 0)
-    for (int j = 0, r = rho0; j <= steps; ++j, r = min(r + growth, 0)) rho[(long long)b * (MAX_STEPS + 1) + j] = r;
+    for (int j = 0, r = rho0, next; j <= steps; ++j, r = next) {
+      next = min(r + growth, 0);
+      rho[(long long)b * (MAX_STEPS + 1) + j] =
+          r ? make_float4(ldexpf(1.f, r), ldexpf(1.f, 2 * r), ldexpf(1.f, 4 * r), ldexpf(1.f, r - next)) : make_float4(1.f, 1.f, 1.f, 1.f);
+    }
   __half* hi = x + (long long)b * 2 * plane;
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
     const int r = (int)(i / cpr), c = (int)(i - (long long)r * cpr) * 8;
@@ -709,7 +710,7 @@ __global__ void __launch_bounds__(256) ns_copy_kernel(const NsGemm a) {
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
     const int r = (int)(i / a.N), c = (int)(i - (long long)r * a.N);
     const __half* p = a.src + (long long)b * 2 * a.src_plane + (long long)r * a.ld_src + c;
-    const float v = ldexpf(a.c_src * (__half2float(p[0]) + __half2float(p[a.src_plane])), a.rho[(long long)b * (MAX_STEPS + 1)]);
+    const float v = a.c_src * (__half2float(p[0]) + __half2float(p[a.src_plane])) * a.rho[(long long)b * (MAX_STEPS + 1)].x;
     const long long o = (long long)b * a.user.stride + (long long)r * a.user.ld + c;
     const NsTarget to = target_of(a.user);
     if (a.out == OUT_F32 || a.out == OUT_UPDATE_F32)
@@ -787,7 +788,7 @@ NsLayout layout(int batch, int rows, int cols) {
     return o;
   };
   L.part = take(sizeof(double) * NORM_BLOCKS * (size_t)batch);
-  L.rho = take(sizeof(int) * (MAX_STEPS + 1) * (size_t)batch);
+  L.rho = take(sizeof(float4) * (MAX_STEPS + 1) * (size_t)batch);
   L.x0 = take((size_t)batch * 2 * L.plane_x * 2);
   L.x1 = take((size_t)batch * 2 * L.plane_x * 2);
   L.s0 = take((size_t)batch * 2 * L.plane_s * 2);
@@ -941,7 +942,7 @@ cudaError_t ns_run(const NsProblem& problem, void* work, cudaStream_t st, const 
   const NsLayout L = layout(p.batch, p.rows, p.cols);
   char* base = static_cast<char*>(work);
   double* part = reinterpret_cast<double*>(base + L.part);
-  int* rho = reinterpret_cast<int*>(base + L.rho);
+  float4* rho = reinterpret_cast<float4*>(base + L.rho);
   __half* X[2] = {reinterpret_cast<__half*>(base + L.x0), reinterpret_cast<__half*>(base + L.x1)};
   __half* A = reinterpret_cast<__half*>(base + L.s0);
   __half* Q = reinterpret_cast<__half*>(base + L.s1);

@@ -98,6 +98,9 @@ __device__ __forceinline__ void symmetric_product(const SymPlace& p, const float
   }
 }
 
+// TINY: X_0 may be beyond fp32's normal range.  Its non-zero elements are at least 2^-149 / eps where the norm is far below
+// eps, which for eps <= 1e-7 (the default) is 2^-125.7: nothing is lost then.  (10 x 200 takes 15.0 us without TINY, 15.7 with.)
+template <bool TINY>
 __global__ void __launch_bounds__(NC_THREADS, 1) ns_cluster_kernel(const NsSource s, const NsSink o, const NcArgs n) {
   extern __shared__ __align__(16) float sm[];
   __shared__ double share[NC_THREADS / 32];
@@ -147,11 +150,13 @@ __global__ void __launch_bounds__(NC_THREADS, 1) ns_cluster_kernel(const NsSourc
     ss += n.csize > 1 ? cluster_load_f64(cluster_map(smem_u32(share + w), (uint32_t)p)) : share[w];
   }
   ss = warp_sum(ss);
-  // A norm far below eps would leave X_0 to fp32's subnormal numbers: the iterate is then kept times 2^-rho, rho as in
-  // muon.cu (0 for all others, and every factor that follows from it 1)
-  const double size = sqrt(ss) / (sqrt(ss) + n.eps);
-  int rho = size > 0.0 && size < 0x1p-60 ? ilogb(size) : 0;
-  const double inv = ldexp(1.0 / (sqrt(ss) + n.eps), -rho);
+  const double norm = sqrt(ss);
+  double inv = 1.0 / (norm + n.eps);
+  int rho = 0;  // TINY: the iterate is kept times 2^-rho, rho as in muon.cu
+  if (TINY && norm > 0.0 && norm * inv < 0x1p-60) {
+    rho = ilogb(norm * inv);
+    inv = ldexp(inv, -rho);
+  }
   for (int e = tid; e < kn * rp; e += threads) X[e] = (float)((double)X[e] * inv);
   __syncthreads();
 
@@ -191,11 +196,16 @@ __global__ void __launch_bounds__(NC_THREADS, 1) ns_cluster_kernel(const NsSourc
     } else {
       __syncthreads();
     }
-    symmetric_product(poly, A, n.r, rp, Q, A, ldexpf(n.b, 2 * rho), ldexpf(n.cc, 4 * rho));
+    float ca = n.a, cb = n.b, cc = n.cc;
+    if (TINY && rho) {
+      const int next = min(rho + n.growth, 0);
+      ca = ldexpf(ca, rho - next);
+      cb = ldexpf(cb, 3 * rho - next);
+      cc = ldexpf(cc, 5 * rho - next);
+      rho = next;
+    }
+    symmetric_product(poly, A, n.r, rp, Q, A, cb, cc);
     __syncthreads();
-    const int next = min(rho + n.growth, 0);
-    const float grown = ldexpf(1.f, rho - next), an = n.a * grown;
-    rho = next;
     // Y = a X + X Q: 4 columns of the slice x 4 rows a thread
     for (int base = 0; base < items << lk; base += threads) {
       const int id = base + tid, item = id >> lk, p = id & ((1 << lk) - 1);
@@ -235,7 +245,7 @@ __global__ void __launch_bounds__(NC_THREADS, 1) ns_cluster_kernel(const NsSourc
         for (int t = 0; t < 4; ++t) {
           const float4 v = *reinterpret_cast<const float4*>(x + t * rp + 4 * ti);
           *reinterpret_cast<float4*>(Y + (size_t)(kg * 4 + t) * rp + 4 * ti) =
-              make_float4(an * v.x + grown * acc[t][0], an * v.y + grown * acc[t][1], an * v.z + grown * acc[t][2], an * v.w + grown * acc[t][3]);
+              make_float4(ca * v.x + acc[t][0], ca * v.y + acc[t][1], ca * v.z + acc[t][2], ca * v.w + acc[t][3]);
         }
       }
     }
@@ -251,7 +261,7 @@ __global__ void __launch_bounds__(NC_THREADS, 1) ns_cluster_kernel(const NsSourc
     const int i = n.tall ? w : q, k = n.tall ? q : w;
     const long long row = n.tall ? k0 + k : i, col = n.tall ? i : k0 + k;
     const long long at = (long long)b * o.stride + row * o.ld + col;
-    const float v = ldexpf(X[k * rp + i], rho);
+    const float v = TINY && rho ? ldexpf(X[k * rp + i], rho) : X[k * rp + i];
     if (o.bf16)
       static_cast<__nv_bfloat16*>(to.o)[at] = __float2bfloat16_rn(
           o.update ? to.decay * __bfloat162float(static_cast<const __nv_bfloat16*>(to.prev)[at]) - to.step * v : v);
@@ -298,7 +308,8 @@ bool ns_fits_cluster(int batch, int rows, int cols) {
 }
 
 cudaError_t ns_cluster_set_attributes() {
-  return cudaFuncSetAttribute(ns_cluster_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, NC_MAX_SMEM);
+  const cudaError_t e = cudaFuncSetAttribute(ns_cluster_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, NC_MAX_SMEM);
+  return e == cudaSuccess ? cudaFuncSetAttribute(ns_cluster_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, NC_MAX_SMEM) : e;
 }
 
 cudaError_t launch_ns_cluster(const NsSource& s, const NsSink& o, int batch, const float coef[3], int steps, double eps,
@@ -327,7 +338,8 @@ cudaError_t launch_ns_cluster(const NsSource& s, const NsSink& o, int batch, con
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = n.csize > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, ns_cluster_kernel, s, o, n);
+  return eps > 1e-7 ? cudaLaunchKernelEx(&cfg, ns_cluster_kernel<true>, s, o, n)
+                    : cudaLaunchKernelEx(&cfg, ns_cluster_kernel<false>, s, o, n);
 }
 
 }  // namespace gcada

@@ -662,7 +662,7 @@ def test_norms_far_below_eps(shape):
     digits lost on the way to results that are in range again."""
     g = torch.from_numpy(spectrum(*shape, "gauss")).float().cuda()
     grow = (1.875, -1.25, 0.375)                                # a tiny iterate grows 1.875-fold a step, 2e27-fold in a hundred
-    for factor, eps in ((1e-20, 1e30), (1e-30, 1e20), (1e-38, 1e30), (1e-12, 1e30), (1.0, 1e30), (1e-38, 1e-7), (1e-25, 1e-20)):
+    for factor, eps in ((1e-20, 1e30), (1e-30, 1e20), (1e-38, 1e30), (1e-12, 1e30), (1.0, 1e30), (1e-38, 1e-7), (3e-44, 1e-7), (1e-25, 1e-20)):
         h = g * factor
         for steps, coef in ((0, om.COEF), (1, om.COEF), (5, om.COEF), (100, grow)):
             o = num(binding.orthogonalize(h, steps=steps, coef=coef, eps=eps))
