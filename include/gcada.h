@@ -359,7 +359,7 @@ gcada_status gcada_operator_status(int **word_dev);
  * which drive the singular values towards one.  coef = {a, b, c} (host; NULL: 3.4445, -4.7750, 2.0315, for which
  * five steps take singular values above 0.01 of the norm to between 0.68 and 1.21).  The iterates' singular values
  * have to stay below 7.  A matrix of zeros gives zeros; one that holds an infinity or NaN gives NaN
- * everywhere (after one step at least).  o may be g, in the same layout.
+ * everywhere (after one step at least).  o may be g, in the same layout (another one is refused for batches).
  * GCADA_EINVAL unless 0 <= steps <= 100, |a|, |b|, |c| <= 16, 1e-30 <= eps <= 1e30, rows, cols <= 2^20, batch <=
  * 65535, the results do not overlap, and work_dev is 256-byte aligned with at least the bytes that
  * gcada_orthogonalize_work gives (256 means that the area is not used: matrices with a short side of up to 64 stay

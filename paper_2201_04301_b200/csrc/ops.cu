@@ -82,6 +82,8 @@ gcada_status gcada_orthogonalize(const void* g_dev, void* o_dev, int type, int b
   REFUSE(!aligned_to(g_dev, type_bytes(type)) || !aligned_to(o_dev, type_bytes(type)), "a matrix pointer is not aligned to its type");
   REFUSE(ld_g < cols || ld_o < cols, "a row stride is smaller than cols");
   REFUSE(batch > 1 && (stride_g < 0 || stride_o < ld_o * (rows - 1) + cols), "matrix strides: need stride_g >= 0 and results that do not overlap");
+  // a matrix of the batch may be written before another has been read
+  REFUSE(batch > 1 && o_dev == g_dev && (stride_o != stride_g || (rows > 1 && ld_o != ld_g)), "a batch takes its results in place in the same layout only");
   const size_t need = gcada::ns_work_bytes(batch, rows, cols);
   REFUSE(!work_dev || !aligned_to(work_dev, 256) || work_bytes < need, "need a 256-byte aligned work area of %zu bytes", need);
   gcada::NsProblem p{};

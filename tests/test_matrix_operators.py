@@ -62,6 +62,13 @@ def test_orthogonalize_refuses(lib, bad):
     assert st == binding.EINVAL and text
 
 
+@pytest.mark.parametrize("bad", [dict(sg=0), dict(sg=17), dict(ld_g=5, sg=20), dict(ld_o=5, so=20, sg=20)])
+def test_orthogonalize_refuses_batches_in_place_of_another_layout(lib, bad):
+    """One matrix, three times, with the first result in its place: the others might read the result."""
+    st, text = c_orth(lib, **{**dict(batch=3, g=8192, o=8192, sg=16, so=16), **bad})
+    assert st == binding.EINVAL and "layout" in text
+
+
 def test_empty_matrices_are_no_error(lib):
     for kw in (dict(batch=0), dict(rows=0), dict(cols=0)):
         assert c_orth(lib, g=0, o=0, work=0, bytes=0, **kw)[0] == binding.OK
